@@ -1,7 +1,7 @@
 """Binding of libbsr_actprune.so -- argument marshalling only.
 
 Every function here has the name of the C entry point it calls (see
-``include/bsr_actprune.h``) and does nothing but turn torch tensors into device
+``include/bsr_actprune.h`` and, for the token operators, ``include/bsr_token_step.h``) and does nothing but turn torch tensors into device
 pointers, sizes and the current HIP stream, allocate missing output buffers
 with torch, and raise on a non-zero status.  The single-tensor calls do that in
 native code (``csrc/torch_calls.cpp``: they are short, and marshalling in Python
@@ -25,6 +25,7 @@ BSR_OP_AFFINE_SCALE_GRAD = 4
 BSR_OK = 0
 BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_DTYPE, BSR_ERR_KEEP = -1, -2, -3, -4
 BSR_ERR_WORKSPACE, BSR_ERR_ALIGN, BSR_ERR_HIP, BSR_ERR_LIMIT = -5, -6, -7, -8
+BSR_ERR_VALUE = -9
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libbsr_actprune.so"
@@ -38,6 +39,14 @@ EXPORTS = (
     "bsr_compress_batched", "bsr_compress_batched_workspace_bytes", "bsr_decompress_batched",
     "bsr_score_select_static", "bsr_score_select_static_max_blocks", "bsr_static_scratch_init",
     "bsr_score_select_grouped_batched",
+)
+
+# what include/bsr_token_step.h declares
+TOKEN_EXPORTS = (
+    "bsr_embedding_lookup", "bsr_embedding_grad", "bsr_embedding_grad_workspace_bytes", "bsr_expert_capacity",
+    "bsr_expert_sort", "bsr_expert_sort_workspace_bytes", "bsr_expert_gather", "bsr_expert_combine",
+    "bsr_expert_combine_grad", "bsr_distill_loss", "bsr_distill_grad", "bsr_distill_loss_grad",
+    "bsr_distill_workspace_bytes",
 )
 
 
@@ -109,6 +118,33 @@ def lib() -> C.CDLL:
     l.bsr_score_select_static.argtypes = [vp, i32, i64, i64, i64, i32, i32, dbl, vp, vp, vp]
     l.bsr_score_select_static_max_blocks.restype = i64
     l.bsr_score_select_static_max_blocks.argtypes = []
+    flt = C.c_float
+    l.bsr_embedding_lookup.restype = i32
+    l.bsr_embedding_lookup.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, flt, vp, i64, vp]
+    l.bsr_embedding_grad_workspace_bytes.restype = sz
+    l.bsr_embedding_grad_workspace_bytes.argtypes = [i64, i64, i64]
+    l.bsr_embedding_grad.restype = i32
+    l.bsr_embedding_grad.argtypes = [vp, i32, i64, vp, i32, i64, i64, flt, i64, vp, i64, i32, vp, sz, vp]
+    l.bsr_expert_capacity.restype = i64
+    l.bsr_expert_capacity.argtypes = [i64, i64, i64]
+    l.bsr_expert_sort_workspace_bytes.restype = sz
+    l.bsr_expert_sort_workspace_bytes.argtypes = [i64, i64]
+    l.bsr_expert_sort.restype = i32
+    l.bsr_expert_sort.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, sz, vp]
+    l.bsr_expert_gather.restype = i32
+    l.bsr_expert_gather.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+    l.bsr_expert_combine.restype = i32
+    l.bsr_expert_combine.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i64, vp]
+    l.bsr_expert_combine_grad.restype = i32
+    l.bsr_expert_combine_grad.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, i64, vp, vp, i64, vp, i64, vp, vp]
+    l.bsr_distill_workspace_bytes.restype = sz
+    l.bsr_distill_workspace_bytes.argtypes = [i64, i64, i64]
+    l.bsr_distill_loss.restype = i32
+    l.bsr_distill_loss.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, flt, vp, vp, vp, sz, vp]
+    l.bsr_distill_grad.restype = i32
+    l.bsr_distill_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, flt, vp, vp, vp, i64, vp]
+    l.bsr_distill_loss_grad.restype = i32
+    l.bsr_distill_loss_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, flt, vp, vp, vp, i64, vp, sz, vp]
     l.bsr_static_scratch_init.restype = i32
     l.bsr_static_scratch_init.argtypes = []
     _lib = l
@@ -495,3 +531,98 @@ def bsr_decompress_batched(batch: DecompressBatch, *, stream=None):
     rc = lib().bsr_decompress_batched(batch.items, batch.n, batch.dtype, _stream(stream))
     _check(rc, "bsr_decompress_batched")
     return batch.outputs
+
+
+# ---------------------------------------------------------------------------
+# token operators
+# ---------------------------------------------------------------------------
+
+def bsr_embedding_lookup(table: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0,
+                         out: Optional[torch.Tensor] = None, stream=None):
+    """-> out [T x D]: scale * table[tokens], +0.0 for tokens (int32 or int64, 1-D) outside the table."""
+    r = (_native or _load_native()).embedding_lookup(table, tokens, scale, out, stream)
+    return r if type(r) is not int else _failed(r, table, "bsr_embedding_lookup")
+
+
+def bsr_embedding_grad(tokens: torch.Tensor, dY: torch.Tensor, vocab: int, *, scale: float = 1.0,
+                       dE: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None,
+                       stream=None):
+    """-> dE [vocab x D] float32: scale * the sum of the rows of dY with that token (added to dE when accumulate)."""
+    r = (_native or _load_native()).embedding_grad(tokens, dY, vocab, scale, dE, accumulate, ws, stream)
+    return r if type(r) is not int else _failed(r, dY, "bsr_embedding_grad")
+
+
+def bsr_embedding_grad_workspace_bytes(T: int, vocab: int, D: int) -> int:
+    return int(lib().bsr_embedding_grad_workspace_bytes(T, vocab, D))
+
+
+def bsr_expert_capacity(entries: int, experts: int, align: int = 1) -> int:
+    """Rows of the sorted matrix for so many entries, however they fall on the experts."""
+    n = int(lib().bsr_expert_capacity(entries, experts, align))
+    if n < 0:
+        raise BsrError(BSR_ERR_SHAPE, "bsr_expert_capacity")
+    return n
+
+
+def bsr_expert_sort(expert_ids: torch.Tensor, experts: int, *, align: int = 1, offsets: Optional[torch.Tensor] = None,
+                    counts: Optional[torch.Tensor] = None, order: Optional[torch.Tensor] = None,
+                    slots: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """-> (offsets int32 [experts+1], counts int32 [experts], order int32 [rows], slots int32, as expert_ids): entries
+    sorted by expert, every expert's rows from a multiple of align on."""
+    r = (_native or _load_native()).expert_sort(expert_ids, experts, align, offsets, counts, order, slots, ws, stream)
+    return r if type(r) is not int else _check(r, "bsr_expert_sort")
+
+
+def bsr_expert_sort_workspace_bytes(entries: int, experts: int) -> int:
+    return int(lib().bsr_expert_sort_workspace_bytes(entries, experts))
+
+
+def bsr_expert_gather(X: torch.Tensor, slots: torch.Tensor, order: torch.Tensor, *, out: Optional[torch.Tensor] = None,
+                      stream=None):
+    """-> Xs [rows x D]: every token's row at its slots, +0.0 in rows of padding."""
+    r = (_native or _load_native()).expert_gather(X, slots, order, out, stream)
+    return r if type(r) is not int else _failed(r, X, "bsr_expert_gather")
+
+
+def bsr_expert_combine(Ys: torch.Tensor, slots: torch.Tensor, weights: Optional[torch.Tensor] = None, *,
+                       out: Optional[torch.Tensor] = None, stream=None):
+    """-> out [T x D]: the sum of a token's rows of Ys, each times its weight (float32 [T x k]; None: plain sum, the
+    gradient of bsr_expert_gather)."""
+    r = (_native or _load_native()).expert_combine(Ys, slots, weights, out, stream)
+    return r if type(r) is not int else _failed(r, Ys, "bsr_expert_combine")
+
+
+def bsr_expert_combine_grad(Ys: torch.Tensor, slots: torch.Tensor, order: torch.Tensor, weights: torch.Tensor,
+                            dOut: torch.Tensor, *, dYs: Optional[torch.Tensor] = None,
+                            dweights: Optional[torch.Tensor] = None, stream=None):
+    """-> (dYs [rows x D], dweights float32 [T x k]): gradients of bsr_expert_combine with weights."""
+    r = (_native or _load_native()).expert_combine_grad(Ys, slots, order, weights, dOut, dYs, dweights, stream)
+    return r if type(r) is not int else _failed(r, Ys, "bsr_expert_combine_grad")
+
+
+def bsr_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0, *,
+                     loss: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                     ws: Optional[torch.Tensor] = None, stream=None):
+    """-> (loss float32 [N], stats float32 [N x 2]): divergence of the student's softmax from the teacher's over its
+    entries (columns ids, logits teacher, both [N x K]), and what bsr_distill_grad needs of the logits."""
+    r = (_native or _load_native()).distill_loss(logits, ids, teacher, temperature, loss, stats, ws, stream)
+    return r if type(r) is not int else _failed(r, logits, "bsr_distill_loss")
+
+
+def bsr_distill_grad(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, stats: torch.Tensor,
+                     dloss: torch.Tensor, temperature: float = 1.0, *, dlogits: Optional[torch.Tensor] = None, stream=None):
+    """-> dlogits [N x V] (which may be logits itself): gradient of sum(dloss * loss)."""
+    r = (_native or _load_native()).distill_grad(logits, ids, teacher, temperature, stats, dloss, dlogits, stream)
+    return r if type(r) is not int else _failed(r, logits, "bsr_distill_grad")
+
+
+def bsr_distill_loss_grad(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, dloss: torch.Tensor,
+                          temperature: float = 1.0, *, loss: Optional[torch.Tensor] = None,
+                          dlogits: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """-> (loss, dlogits): bsr_distill_loss and bsr_distill_grad in one call, for a dloss that is known beforehand."""
+    r = (_native or _load_native()).distill_loss_grad(logits, ids, teacher, temperature, dloss, loss, dlogits, ws, stream)
+    return r if type(r) is not int else _failed(r, logits, "bsr_distill_loss_grad")
+
+
+def bsr_distill_workspace_bytes(N: int, V: int, K: int) -> int:
+    return int(lib().bsr_distill_workspace_bytes(N, V, K))

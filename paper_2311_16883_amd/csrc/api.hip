@@ -5,6 +5,7 @@
 #include <vector>
 
 #include "common.h"
+#include "bsr_token_step.h"
 
 namespace bsr {
 
@@ -331,6 +332,7 @@ const char *bsr_error_string(int code) {
     case BSR_ERR_ALIGN: return "BSR_ERR_ALIGN";
     case BSR_ERR_HIP: return "BSR_ERR_HIP";
     case BSR_ERR_LIMIT: return "BSR_ERR_LIMIT";
+    case BSR_ERR_VALUE: return "BSR_ERR_VALUE";
     default: return "BSR_ERR_UNKNOWN";
   }
 }

@@ -1,0 +1,172 @@
+// Gradient of the token table: dE[v] (+)= scale * sum of the rows of dY whose token is v, positions ascending.
+//
+// The positions are sorted by token first (token_sort.hip; its launches also clear dE).  The sorted order is cut into windows of
+// kWindow positions, whatever tokens they hold: a wave takes 64 vectors of columns of one window, walks its positions with
+// kAhead rows on their way, and keeps the sum of the current token's rows in registers.  A token whose positions all lie in one
+// window is written to dE straight away; of one that reaches into others every window leaves a partial sum, and a
+// second kernel adds these up window by window.  So the work per wave is the same however often a token occurs, and the order of
+// every sum follows from the tokens alone.  Bound by memory: dY once, dE once.
+#include "token_step.h"
+
+namespace bsr {
+
+namespace {
+
+constexpr int kWindow = 32;
+constexpr int kAhead = 8;
+constexpr int kThreads = 256;
+
+// The sum of a run of equal tokens, positions [first, last) of the sorted order (inside one window, [lo, hi)): to its row of dE,
+// or to partial[2 * window] where the run goes on from the window before, to partial[2 * window + 1] where it only goes on
+// into the next.
+template <int VE>
+__device__ __forceinline__ void put_sum(const float *sum, bool goes_on_before, bool goes_on_behind, float scale, float *row,
+                                        float *partial, int64_t at, int skip, bool accumulate) {
+  const bool whole = !goes_on_before && !goes_on_behind;
+  float *dst = (whole ? row : partial) + at;
+  const float by = whole ? scale : 1.0f;
+  const bool add = whole && accumulate;
+  if constexpr (VE % 4 == 0) {
+    if (skip == 0) {
+#pragma unroll
+      for (int q = 0; q < VE; q += 4) {
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = sum[q + i] * by;
+        if (add) {
+          const Words4 old = RowVec<float, 4>::load(dst + q);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] += __uint_as_float(old[i]);
+        }
+        RowVec<float, 4>::store(dst + q, pack_row<float, 4>(f));
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < VE; ++q) {
+    if (q < skip) continue;
+    const float v = sum[q] * by;
+    dst[q] = add ? dst[q] + v : v;
+  }
+}
+
+template <typename T, int VE>
+__global__ __launch_bounds__(kThreads) void window_sum_kernel(const uint2 *__restrict__ sorted, int64_t n, uint32_t V,
+                                                              const T *__restrict__ dY, int64_t D, int64_t lddy, float scale,
+                                                              float *__restrict__ dE, int64_t ldde, int accumulate,
+                                                              float *__restrict__ partial, int64_t slices) {
+  typedef RowVec<T, VE> R;
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t window = unit / slices, slice = unit - window * slices;
+  const int64_t lo = window * kWindow;
+  if (lo >= n) return;
+  const int count = (int)(n - lo < kWindow ? n - lo : kWindow);
+  // lane l holds position lo - 1 + l of the sorted order: its neighbours tell where runs go on
+  uint2 e = uint2{0xFFFFFFFFu, 0};
+  if (lane <= count + 1 && lo - 1 + lane >= 0 && lo - 1 + lane < n) e = sorted[lo - 1 + lane];
+  const uint32_t before = __builtin_amdgcn_readlane(e.x, 0), behind = __builtin_amdgcn_readlane(e.x, count + 1);
+  const int64_t v = slice * 64 + lane, vecs = ceil_div(D, (int64_t)VE);
+  const bool in = v < vecs;
+  const int64_t at = vector_start(in ? v : 0, VE, D);
+  const int skip = in ? (int)(v * VE - at) : VE;       // elements that belong to the vector before; all for a lane without columns
+  float sum[VE];
+#pragma unroll
+  for (int q = 0; q < VE; ++q) sum[q] = 0.0f;
+  float *head = partial + (2 * window) * D, *tail = head + D;
+  uint32_t token = __builtin_amdgcn_readlane(e.x, 1);
+  int first = 0;
+  for (int i0 = 0; i0 < count && token < V; i0 += kAhead) {
+    typename R::Raw x[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u < count ? i0 + u : count - 1;
+      const uint32_t pos = __builtin_amdgcn_readlane(e.y, 1 + i);
+      x[u] = R::load(dY + (int64_t)pos * lddy + at);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u;
+      if (i >= count || token >= V) continue;
+      const uint32_t next = __builtin_amdgcn_readlane(e.x, 2 + i);
+#pragma unroll
+      for (int q = 0; q < VE; ++q) sum[q] += R::elem(x[u], q);
+      if (next != token || i == count - 1) {
+        const bool b = first == 0 && before == token, f = i == count - 1 && behind == token;
+        put_sum<VE>(sum, b, f, scale, dE + (int64_t)token * ldde, b ? head : tail, at, skip, accumulate != 0);
+#pragma unroll
+        for (int q = 0; q < VE; ++q) sum[q] = 0.0f;
+        first = i + 1;
+        token = next;
+      }
+    }
+  }
+}
+
+// dE[token] for the tokens that reach over several windows: one wave per 64 columns of the window where such a token's run
+// starts; it adds that window's sum and those of the windows that the run goes on into.
+__global__ __launch_bounds__(kThreads) void join_kernel(const uint2 *__restrict__ sorted, int64_t n, uint32_t V, int64_t D,
+                                                        float scale, float *__restrict__ dE, int64_t ldde, int accumulate,
+                                                        const float *__restrict__ partial, int64_t windows, int64_t slices) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t window = unit / slices, slice = unit - window * slices;
+  const int64_t lo = window * kWindow, behind = lo + kWindow;
+  if (behind >= n) return;                                       // no window behind
+  const uint32_t token = sorted[behind - 1].x;
+  if (token >= V || sorted[behind].x != token) return;           // no run goes on
+  if (lo > 0 && sorted[lo].x == token && sorted[lo - 1].x == token) return;   // it started before
+  const int64_t c = slice * 64 + lane;
+  float sum = c < D ? partial[(2 * window + 1) * D + c] : 0.0f;
+  for (int64_t w0 = window + 1; w0 < windows; w0 += 64) {
+    // windows that the run reaches into: those whose first position holds its token
+    const int64_t w = w0 + lane;
+    const uint64_t more = __ballot(w < windows && sorted[w < windows ? w * kWindow : 0].x == token);
+    const int reach = more == ~uint64_t(0) ? 64 : __builtin_ctzll(~more);
+    if (c < D) {
+#pragma unroll 8
+      for (int i = 0; i < reach; ++i) sum += partial[2 * (w0 + i) * D + c];
+    }
+    if (reach < 64) break;
+  }
+  if (c < D) {
+    float *dst = dE + (int64_t)token * ldde + c;
+    *dst = accumulate ? *dst + sum * scale : sum * scale;
+  }
+}
+
+size_t partial_bytes(int64_t T, int64_t D) { return T > kWindow ? align_up((size_t)ceil_div(T, (int64_t)kWindow) * 2 * D * sizeof(float), 256) : 0; }
+
+}  // namespace
+
+size_t embedding_grad_ws_bytes(int64_t T, int64_t V, int64_t D) { return token_sort_ws_bytes(T, V) + partial_bytes(T, D); }
+
+int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const void *dY, int dtype, int64_t D, int64_t lddy,
+                          float scale, int64_t V, float *dE, int64_t ldde, int accumulate, void *ws, hipStream_t s) {
+  const ClearJob clear = {accumulate ? nullptr : dE, V, D, ldde};
+  float *partial = static_cast<float *>(ws);
+  const uint2 *sorted = nullptr;
+  int rc = launch_token_sort(tokens, index_type, T, V, clear, static_cast<char *>(ws) + partial_bytes(T, D), &sorted, s);
+  if (rc != BSR_OK || T == 0) return rc;
+  const int64_t windows = ceil_div(T, (int64_t)kWindow);
+#define BSR_CALL(TY, VE)                                                                                                       \
+  const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
+  hipLaunchKernelGGL((window_sum_kernel<TY, VE>), dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))),         \
+                     dim3(kThreads), 0, s, sorted, T, (uint32_t)V, static_cast<const TY *>(dY), D, lddy, scale, dE, ldde,      \
+                     accumulate, partial, slices)
+  if (dtype == BSR_F32) {
+    if (D >= 4) { BSR_CALL(float, 4); } else { BSR_CALL(float, 1); }
+  } else {
+    if (D >= 8) { BSR_CALL(uint16_t, 8); } else { BSR_CALL(uint16_t, 1); }
+  }
+#undef BSR_CALL
+  rc = check_launch();
+  if (rc != BSR_OK || windows == 1) return rc;
+  const int64_t slices = ceil_div(D, (int64_t)64);
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))), dim3(kThreads), 0, s,
+                     sorted, T, (uint32_t)V, D, scale, dE, ldde, accumulate, partial, windows, slices);
+  return check_launch();
+}
+
+}  // namespace bsr

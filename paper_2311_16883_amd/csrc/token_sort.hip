@@ -1,0 +1,289 @@
+// Stable sorts by key: entries by expert, positions by token.
+//
+// A counting sort of up to kMaxBins values, in two launches: every workgroup counts the values of its stretch of entries
+// (count_kernel); then every workgroup adds up the counts of all, which says where the entries of a value start in the whole
+// and where its own among them, and moves its entries there in order (place_kernel).  Tokens, which have too many values for one such
+// pass, take one per digit, lowest first.  Up to one stretch of entries needs no counts of others and one launch per pass.
+//
+// Latency bound: a few bytes per entry.  Order within a workgroup: its waves own consecutive parts of the stretch, a wave takes 64
+// entries at a time and finds, for every lane, the lanes before it with the same value from one ballot per bit of the value.
+// No atomic decides an order (they only count), so the result is the stable one whatever the timing.
+#include "token_step.h"
+
+namespace bsr {
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / 64;
+constexpr int kMaxBins = 1025;                 // kMaxExperts and the dropped entries; digits of up to 10 bits
+constexpr int kDigitBits = 10;
+constexpr int kMinSteps = 4;                   // times 64 entries that a wave takes, at least
+constexpr int kMaxBlocks = 256;                // workgroups (stretches), at most: each reads the counts of all
+constexpr int64_t kClearPerBlock = 32768;      // elements that a workgroup clears
+
+enum Source { kFromI32, kFromI64, kFromPairs };
+
+// What a pass sorts: entry i has a key, of which the pass goes by (key >> shift) & mask.
+struct Keys {
+  const void *p;
+  int64_t n;
+  uint32_t limit;            // the key of indices outside [0, limit)
+  int shift;
+  uint32_t mask;
+  int bins, bits;            // values that (key >> shift) & mask can have, and their bits
+  int steps;                 // times 64 entries per wave
+};
+
+template <Source S>
+__device__ __forceinline__ uint2 load_entry(const Keys &k, int64_t i) {
+  if constexpr (S == kFromPairs) return static_cast<const uint2 *>(k.p)[i];
+  const int64_t v = S == kFromI64 ? load_index<int64_t>(k.p, i) : load_index<int32_t>(k.p, i);
+  return uint2{v >= 0 && v < (int64_t)k.limit ? (uint32_t)v : k.limit, (uint32_t)i};
+}
+__device__ __forceinline__ uint32_t digit_of(const Keys &k, uint32_t key) { return (key >> k.shift) & k.mask; }
+
+// +0.0 over one workgroup's part of a matrix.
+__device__ __forceinline__ void clear_part(const ClearJob &c, int64_t part) {
+  if (c.ld == c.cols || c.rows == 1) {
+    const int64_t total = c.rows * c.cols, lo = part * kClearPerBlock;
+    const int64_t hi = lo + kClearPerBlock < total ? lo + kClearPerBlock : total;
+    for (int64_t i = lo + 4 * threadIdx.x; i < hi; i += 4 * kThreads) {
+      if (i + 4 <= hi) {
+        reinterpret_cast<Any16 *>(c.p + i)->w = Words4{0, 0, 0, 0};
+      } else {
+        for (int64_t j = i; j < hi; ++j) c.p[j] = 0.0f;
+      }
+    }
+    return;
+  }
+  const int64_t per = kClearPerBlock / c.cols > 0 ? kClearPerBlock / c.cols : 1;
+  for (int64_t r = part * per; r < (part + 1) * per && r < c.rows; ++r)
+    for (int64_t j = threadIdx.x; j < c.cols; j += kThreads) c.p[r * c.ld + j] = 0.0f;
+}
+
+// counts[block][bin]
+template <Source S>
+__global__ __launch_bounds__(kThreads) void count_kernel(Keys k, uint32_t *__restrict__ counts, int blocks, ClearJob clear) {
+  __shared__ uint32_t bin[kMaxBins];
+  const int t = threadIdx.x;
+  if ((int)blockIdx.x >= blocks) {
+    clear_part(clear, (int64_t)blockIdx.x - blocks);
+    return;
+  }
+  for (int b = t; b < k.bins; b += kThreads) bin[b] = 0;
+  __syncthreads();
+  const int64_t per = (int64_t)k.steps * kThreads, lo = blockIdx.x * per;
+  const int64_t hi = lo + per < k.n ? lo + per : k.n;
+  for (int64_t i = lo + t; i < hi; i += kThreads) atomicAdd(&bin[digit_of(k, load_entry<S>(k, i).x)], 1u);
+  __syncthreads();
+  for (int b = t; b < k.bins; b += kThreads) counts[(int64_t)blockIdx.x * k.bins + b] = bin[b];
+}
+
+// Where a pass puts its entries.
+struct Places {
+  uint2 *pairs;                                // (key, position) in order; or, for experts:
+  int32_t *offsets, *counts, *order, *slots;
+  int64_t rows, align, experts;
+};
+
+// a[i] -> sum of a[0 .. i) by the first wave; returns the sum of all to its lanes
+__device__ __forceinline__ uint32_t scan_bins(uint32_t *a, int n, int lane) {
+  const int per = (n + 63) / 64, lo = lane * per, hi = lo + per < n ? lo + per : n;
+  uint32_t sum = 0;
+  for (int i = lo; i < hi; ++i) sum += a[i];
+  uint32_t before = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(before, d, 64);
+    if (lane >= d) before += o;
+  }
+  const uint32_t all = __shfl(before, 63, 64);
+  before -= sum;
+  for (int i = lo; i < hi; ++i) {
+    const uint32_t v = a[i];
+    a[i] = before;
+    before += v;
+  }
+  return all;
+}
+
+template <Source S, bool EXPERTS>
+__global__ __launch_bounds__(kThreads) void place_kernel(Keys k, const uint32_t *__restrict__ counts, int blocks, Places out,
+                                                         ClearJob clear) {
+  __shared__ uint32_t next[kWaves][kMaxBins];  // place of a wave's next entry of a value
+  __shared__ uint32_t start[kMaxBins];         // of a value's entries in the whole
+  __shared__ uint32_t total[EXPERTS ? kMaxBins : 1];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  if ((int)blockIdx.x >= blocks) {
+    clear_part(clear, (int64_t)blockIdx.x - blocks);
+    return;
+  }
+  for (int b = t; b < kWaves * kMaxBins; b += kThreads) (&next[0][0])[b] = 0;
+  __syncthreads();
+  const int64_t lo = ((int64_t)blockIdx.x * kWaves + w) * k.steps * 64;
+  for (int q = 0; q < k.steps; ++q) {
+    const int64_t i = lo + q * 64 + lane;
+    if (i < k.n) atomicAdd(&next[w][digit_of(k, load_entry<S>(k, i).x)], 1u);
+  }
+  __syncthreads();
+  // a value's entries in all workgroups, and in those before this one
+  for (int b = t; b < k.bins; b += kThreads) {
+    uint32_t all = 0, before = 0;
+    if (blocks == 1) {
+      for (int v = 0; v < kWaves; ++v) all += next[v][b];
+    } else {
+#pragma unroll 8
+      for (int c = 0; c < blocks; ++c) {
+        const uint32_t n = counts[(int64_t)c * k.bins + b];
+        before += c < (int)blockIdx.x ? n : 0;
+        all += n;
+      }
+    }
+    if constexpr (EXPERTS) {
+      total[b] = all;
+      all = (uint32_t)((all + out.align - 1) / out.align * out.align);
+    }
+    start[b] = all;
+    for (int v = 0; v < kWaves; ++v) {
+      const uint32_t n = next[v][b];
+      next[v][b] = before;
+      before += n;
+    }
+  }
+  __syncthreads();
+  if (w == 0) scan_bins(start, k.bins, lane);
+  __syncthreads();
+  if constexpr (EXPERTS) {
+    // the last value stands for dropped entries: its start is the end of the last segment
+    if (blockIdx.x == 0) {
+      for (int e = t; e <= out.experts; e += kThreads) {
+        out.offsets[e] = (int32_t)start[e];
+        if (e < out.experts) out.counts[e] = (int32_t)total[e];
+      }
+    }
+    for (int64_t e = blockIdx.x * kWaves + w; e < out.experts; e += (int64_t)blocks * kWaves)
+      for (int64_t s = (int64_t)start[e] + total[e] + lane; s < start[e + 1]; s += 64) out.order[s] = -1;
+    for (int64_t s = (int64_t)start[out.experts] + blockIdx.x * kThreads + t; s < out.rows; s += (int64_t)blocks * kThreads)
+      out.order[s] = -1;
+  }
+  // 64 entries at a time, each behind those of its value that stand before it
+  for (int q = 0; q < k.steps; ++q) {
+    const int64_t i = lo + q * 64 + lane;
+    const bool in = i < k.n;
+    uint2 e = uint2{0, 0};
+    if (in) e = load_entry<S>(k, i);
+    const uint32_t d = digit_of(k, e.x);
+    uint64_t same = __ballot(in);
+    for (int b = 0; b < k.bits; ++b) {
+      const bool one = (d >> b) & 1u;
+      const uint64_t ones = __ballot(one);
+      same &= one ? ones : ~ones;
+    }
+    if (in) {
+      const uint32_t before = (uint32_t)__builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+      const uint32_t place = start[d] + next[w][d] + before;
+      if constexpr (EXPERTS) {
+        const bool kept = (int64_t)d < out.experts;
+        out.slots[i] = kept ? (int32_t)place : -1;
+        if (kept && (int64_t)place < out.rows) out.order[place] = (int32_t)i;
+      } else {
+        out.pairs[place] = e;
+      }
+    }
+    // (the wave's reads above come before the write, and the write before the next round's reads: one wave's LDS accesses
+    // are executed in order; the fences keep the compiler to that)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (in && (same >> lane) >> 1 == 0) next[w][d] += (uint32_t)__builtin_popcountll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+int bit_length(uint32_t v) { return v == 0 ? 0 : 32 - __builtin_clz(v); }
+
+// Stretches of n entries.
+void stretches(int64_t n, int *steps, int *blocks) {
+  const int64_t least = ceil_div(n, (int64_t)kMaxBlocks * kThreads);
+  *steps = (int)(least > kMinSteps ? least : kMinSteps);
+  *blocks = (int)ceil_div(n, (int64_t)*steps * kThreads);
+  if (*blocks < 1) *blocks = 1;
+}
+
+size_t counts_bytes(int64_t n, int bins) {
+  int steps, blocks;
+  stretches(n, &steps, &blocks);
+  return blocks > 1 ? align_up((size_t)blocks * bins * sizeof(uint32_t), 256) : 0;
+}
+
+unsigned clear_blocks(const ClearJob &c) {
+  if (c.p == nullptr) return 0;
+  if (c.ld == c.cols || c.rows == 1) return (unsigned)ceil_div(c.rows * c.cols, kClearPerBlock);
+  const int64_t per = kClearPerBlock / c.cols > 0 ? kClearPerBlock / c.cols : 1;
+  return (unsigned)ceil_div(c.rows, per);
+}
+
+// One pass; `clear` rides in its first launch.
+template <Source S, bool EXPERTS>
+int launch_pass(const Keys &k, int blocks, uint32_t *counts, const Places &out, const ClearJob &clear, hipStream_t s) {
+  const unsigned extra = clear_blocks(clear);
+  const ClearJob none = {nullptr, 0, 0, 0};
+  if (blocks > 1) {
+    hipLaunchKernelGGL((count_kernel<S>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, clear);
+    const int rc = check_launch();
+    if (rc != BSR_OK) return rc;
+  }
+  hipLaunchKernelGGL((place_kernel<S, EXPERTS>), dim3(blocks > 1 ? blocks : 1 + extra), dim3(kThreads), 0, s, k, counts, blocks,
+                     out, blocks > 1 ? none : clear);
+  return check_launch();
+}
+
+int digit_passes(int64_t V) { return V < 1 ? 1 : (bit_length((uint32_t)V) + kDigitBits - 1) / kDigitBits; }
+int digit_bits(int64_t V) { return V < 1 ? 1 : (bit_length((uint32_t)V) + digit_passes(V) - 1) / digit_passes(V); }
+
+}  // namespace
+
+size_t expert_sort_ws_bytes(int64_t n, int64_t E) { return counts_bytes(n, (int)E + 1); }
+
+int launch_expert_sort(const void *ids, int index_type, int64_t n, int64_t E, int64_t align, int32_t *offsets, int32_t *counts,
+                       int32_t *order, int64_t rows, int32_t *slots, void *ws, hipStream_t s) {
+  Keys k = {ids, n, (uint32_t)E, 0, 0xFFFFFFFFu, (int)E + 1, bit_length((uint32_t)E), 0};
+  int blocks;
+  stretches(n, &k.steps, &blocks);
+  const Places out = {nullptr, offsets, counts, order, slots, rows, align, E};
+  const ClearJob none = {nullptr, 0, 0, 0};
+  return index_type == BSR_I64 ? launch_pass<kFromI64, true>(k, blocks, static_cast<uint32_t *>(ws), out, none, s)
+                               : launch_pass<kFromI32, true>(k, blocks, static_cast<uint32_t *>(ws), out, none, s);
+}
+
+size_t token_sort_ws_bytes(int64_t T, int64_t V) {
+  const int buffers = digit_passes(V) > 1 ? 2 : 1;
+  return buffers * align_up((size_t)T * sizeof(uint2), 256) + counts_bytes(T, 1 << digit_bits(V));
+}
+
+int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, const ClearJob &clear, void *ws,
+                      const uint2 **sorted, hipStream_t s) {
+  const int passes = digit_passes(V), bits = digit_bits(V);
+  const size_t pairs_bytes = align_up((size_t)T * sizeof(uint2), 256);
+  char *base = static_cast<char *>(ws);
+  uint2 *buffer[2] = {reinterpret_cast<uint2 *>(base), reinterpret_cast<uint2 *>(base + (passes > 1 ? pairs_bytes : 0))};
+  uint32_t *counts = reinterpret_cast<uint32_t *>(base + (passes > 1 ? 2 : 1) * pairs_bytes);
+  const ClearJob none = {nullptr, 0, 0, 0};
+  for (int p = 0; p < passes; ++p) {
+    Keys k = {p == 0 ? tokens : buffer[(p - 1) & 1], T, (uint32_t)V, p * bits, (1u << bits) - 1u, 1 << bits, bits, 0};
+    int blocks;
+    stretches(T, &k.steps, &blocks);
+    Places out = {};
+    out.pairs = buffer[p & 1];
+    const ClearJob &c = p == 0 ? clear : none;
+    const int rc = p > 0 ? launch_pass<kFromPairs, false>(k, blocks, counts, out, c, s)
+                   : index_type == BSR_I64 ? launch_pass<kFromI64, false>(k, blocks, counts, out, c, s)
+                                           : launch_pass<kFromI32, false>(k, blocks, counts, out, c, s);
+    if (rc != BSR_OK) return rc;
+  }
+  *sorted = buffer[(passes - 1) & 1];
+  return BSR_OK;
+}
+
+}  // namespace bsr

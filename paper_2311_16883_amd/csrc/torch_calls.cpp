@@ -1,4 +1,4 @@
-// The single-tensor calls of libbsr_actprune with torch tensors as arguments: what binding.py's
+// The single-tensor calls of libbsr_actprune, the token operators among them, with torch tensors as arguments: what binding.py's
 // functions do between Python and the C ABI, in native code.  Argument checks, output and workspace
 // tensors (torch's caching allocator), device pointers, the current stream, then one C call with the GIL
 // released.  No step of the pruning path is computed here.
@@ -12,13 +12,17 @@
 #include <Python.h>
 
 #include <climits>
+#include <optional>
+#include <string>
 
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "bsr_actprune.h"
+#include "bsr_token_step.h"
 
 namespace {
 
@@ -332,6 +336,330 @@ PyObject *affine_scale_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- token operators ----
+// Their index arrays, weights and statistics are packed arrays, which are checked for type, place and extent here.
+
+// The stream of a call on tensors of like's device: `o` as for stream_handle.  While it lives that stream is the current one, so
+// that outputs and workspaces made here belong to it, and its device is the current device.
+class CallStream {
+ public:
+  CallStream(PyObject *o, const at::Tensor &like) : device_(like.device().index()), before_(c10::hip::current_device()) {
+    if (device_ != before_) c10::hip::set_device(device_);
+    current_ = c10::hip::getCurrentHIPStream(device_);
+    handle_ = current_->stream();
+    if (o == Py_None) return;
+    void *h = nullptr;
+    try {
+      h = stream_handle(o);
+    } catch (...) {
+      restore();
+      throw;
+    }
+    if (h == handle_) return;
+    handle_ = h;
+    changed_ = true;
+    c10::hip::setCurrentHIPStream(h == nullptr ? c10::hip::getDefaultHIPStream(device_)
+                                               : c10::hip::getStreamFromExternal(static_cast<hipStream_t>(h), device_));
+  }
+  ~CallStream() { restore(); }
+  CallStream(const CallStream &) = delete;
+  CallStream &operator=(const CallStream &) = delete;
+  void *handle() const { return handle_; }
+
+ private:
+  void restore() {
+    if (changed_) c10::hip::setCurrentHIPStream(*current_);
+    if (device_ != before_) c10::hip::set_device(before_);
+  }
+  c10::DeviceIndex device_, before_;
+  std::optional<c10::hip::HIPStream> current_;
+  void *handle_ = nullptr;
+  bool changed_ = false;
+};
+
+// A packed array on the device of `like`.
+const at::Tensor &packed(PyObject *o, const char *what, const at::Tensor &like) {
+  const at::Tensor &t = tensor(o, what);
+  if (!t.is_cuda() || t.device() != like.device()) value_error(std::string(what) + " must be on the device of the other tensors");
+  if (!t.is_contiguous()) value_error(std::string(what) + " must be contiguous");
+  return t;
+}
+const at::Tensor &packed(PyObject *o, const char *what, const at::Tensor &like, at::ScalarType type, at::IntArrayRef size) {
+  const at::Tensor &t = packed(o, what, like);
+  if (t.scalar_type() != type) value_error(std::string(what) + " must be " + c10::toString(type));
+  if (t.sizes() != size) value_error(std::string(what) + " has the wrong shape");
+  return t;
+}
+// ... that is an output: the caller's or a new one.
+Output packed_output(PyObject *given, const char *what, at::IntArrayRef size, at::ScalarType type, const at::Tensor &like) {
+  if (given != Py_None) (void)packed(given, what, like, type, size);
+  return output(given, what, size, type, like);
+}
+// A matrix that is an output: the caller's, of this extent and type, or a new one.
+Output matrix_output(PyObject *given, const char *what, int64_t rows, int64_t cols, at::ScalarType type, const at::Tensor &like,
+                     int64_t *ld) {
+  Output o = output(given, what, {rows, cols}, type, like);
+  const Dense d = dense2d(o.get(), what);
+  if (d.rows != rows || d.cols != cols) value_error(std::string(what) + " has the wrong shape");
+  if (o.get().scalar_type() != type) value_error(std::string(what) + " must be " + c10::toString(type));
+  if (o.get().device() != like.device()) value_error(std::string(what) + " must be on the device of the other tensors");
+  *ld = d.ld;
+  return o;
+}
+// A matrix of the type and on the device of `like`.
+Dense matrix_like(const at::Tensor &x, const char *what, const at::Tensor &like) {
+  const Dense d = dense2d(x, what);
+  if (x.scalar_type() != like.scalar_type()) value_error(std::string(what) + " has another dtype");
+  if (x.device() != like.device()) value_error(std::string(what) + " must be on the device of the other tensors");
+  return d;
+}
+
+// BSR_I32 / BSR_I64, or BSR_ERR_DTYPE.
+int index_code(const at::Tensor &t) {
+  const auto s = t.scalar_type();
+  return s == at::kInt ? BSR_I32 : s == at::kLong ? BSR_I64 : BSR_ERR_DTYPE;
+}
+
+template <typename P>
+P *typed(const at::Tensor &t) { return static_cast<P *>(pointer(t)); }
+
+// (table, tokens, scale, out, stream) -> out
+PyObject *embedding_lookup(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 5)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &table = tensor(a[0], "table");
+    const Dense e = dense2d(table, "table");
+    const at::Tensor &tokens = packed(a[1], "tokens", table);
+    if (tokens.dim() != 1) value_error("tokens must be 1-D");
+    const double scale = real(a[2]);
+    const int code = dtype_code(table), index = index_code(tokens);
+    if (code < 0 || index < 0) return code_result(BSR_ERR_DTYPE);
+    const CallStream stream(a[4], table);
+    int64_t ldo;
+    const Output out = matrix_output(a[3], "out", tokens.size(0), e.cols, table.scalar_type(), table, &ldo);
+    const int rc = released([&] {
+      return bsr_embedding_lookup(pointer(table), code, e.rows, e.cols, e.ld, pointer(tokens), index, tokens.size(0), (float)scale,
+                                  pointer(out.get()), ldo, stream.handle());
+    });
+    return rc != BSR_OK ? code_result(rc) : out.result();
+  });
+}
+
+// (tokens, dY, vocab, scale, dE, accumulate, ws, stream) -> dE
+PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &dY = tensor(a[1], "dY");
+    const Dense y = dense2d(dY, "dY");
+    const at::Tensor &tokens = packed(a[0], "tokens", dY);
+    if (tokens.dim() != 1 || tokens.size(0) != y.rows) value_error("tokens must be 1-D, one for each row of dY");
+    const int64_t V = integer(a[2]);
+    if (V < 0) value_error("vocab must not be negative");
+    const double scale = real(a[3]);
+    const bool accumulate = truth(a[5]);
+    if (a[4] == Py_None && accumulate) value_error("accumulate needs an existing dE");
+    const int code = dtype_code(dY), index = index_code(tokens);
+    if (code < 0 || index < 0) return code_result(BSR_ERR_DTYPE);
+    const CallStream stream(a[7], dY);
+    int64_t ldde;
+    const Output dE = matrix_output(a[4], "dE", V, y.cols, at::kFloat, dY, &ldde);
+    const Workspace ws(a[6], a[6] == Py_None ? bsr_embedding_grad_workspace_bytes(y.rows, V, y.cols) : 0, dY);
+    const int rc = released([&] {
+      return bsr_embedding_grad(pointer(tokens), index, y.rows, pointer(dY), code, y.cols, y.ld, (float)scale, V,
+                                typed<float>(dE.get()), ldde, accumulate ? 1 : 0, ws.p, ws.bytes, stream.handle());
+    });
+    return rc != BSR_OK ? code_result(rc) : dE.result();
+  });
+}
+
+// (expert_ids, experts, align, offsets, counts, order, slots, ws, stream) -> (offsets, counts, order, slots)
+PyObject *expert_sort(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 9)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &ids = tensor(a[0], "expert_ids");
+    (void)packed(a[0], "expert_ids", ids);
+    const int64_t E = integer(a[1]), align = integer(a[2]), entries = ids.numel();
+    const int index = index_code(ids);
+    if (index < 0) return code_result(BSR_ERR_DTYPE);
+    const int64_t rows = bsr_expert_capacity(entries, E, align);
+    if (rows < 0) return code_result(BSR_ERR_SHAPE);
+    const CallStream stream(a[8], ids);
+    const Output offsets = packed_output(a[3], "offsets", {E + 1}, at::kInt, ids);
+    const Output counts = packed_output(a[4], "counts", {E}, at::kInt, ids);
+    const Output order = packed_output(a[5], "order", {rows}, at::kInt, ids);
+    const Output slots = packed_output(a[6], "slots", ids.sizes(), at::kInt, ids);
+    const Workspace ws(a[7], a[7] == Py_None ? bsr_expert_sort_workspace_bytes(entries, E) : 0, ids);
+    const int rc = released([&] {
+      return bsr_expert_sort(pointer(ids), index, entries, E, align, typed<int32_t>(offsets.get()), typed<int32_t>(counts.get()),
+                             typed<int32_t>(order.get()), typed<int32_t>(slots.get()), ws.p, ws.bytes, stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return Py_BuildValue("(NNNN)", offsets.result(), counts.result(), order.result(), slots.result());
+  });
+}
+
+// The [T x k] slots of a call.
+const at::Tensor &routing(PyObject *o, const at::Tensor &like) {
+  const at::Tensor &slots = packed(o, "slots", like);
+  if (slots.dim() != 2 || slots.scalar_type() != at::kInt) value_error("slots must be a 2-D int32 tensor [tokens, choices]");
+  return slots;
+}
+
+// (X, slots, order, out, stream) -> Xs
+PyObject *expert_gather(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 5)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &X = tensor(a[0], "X");
+    const Dense x = dense2d(X, "X");
+    const at::Tensor &slots = routing(a[1], X);
+    if (slots.size(0) != x.rows) value_error("slots must have a row for each row of X");
+    const int64_t rows = tensor(a[2], "order").numel();
+    const at::Tensor &order = packed(a[2], "order", X, at::kInt, {rows});
+    const int code = dtype_code(X);
+    if (code < 0) return code_result(code);
+    const CallStream stream(a[4], X);
+    int64_t ldo;
+    const Output out = matrix_output(a[3], "out", rows, x.cols, X.scalar_type(), X, &ldo);
+    const int rc = released([&] {
+      return bsr_expert_gather(pointer(X), code, x.rows, x.cols, x.ld, typed<int32_t>(slots), slots.size(1), typed<int32_t>(order),
+                               rows, pointer(out.get()), ldo, stream.handle());
+    });
+    return rc != BSR_OK ? code_result(rc) : out.result();
+  });
+}
+
+// (Ys, slots, weights or None, out, stream) -> out
+PyObject *expert_combine(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 5)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &Ys = tensor(a[0], "Ys");
+    const Dense y = dense2d(Ys, "Ys");
+    const at::Tensor &slots = routing(a[1], Ys);
+    const float *weights = a[2] == Py_None ? nullptr : typed<float>(packed(a[2], "weights", Ys, at::kFloat, slots.sizes()));
+    const int code = dtype_code(Ys);
+    if (code < 0) return code_result(code);
+    const CallStream stream(a[4], Ys);
+    int64_t ldo;
+    const Output out = matrix_output(a[3], "out", slots.size(0), y.cols, Ys.scalar_type(), Ys, &ldo);
+    const int rc = released([&] {
+      return bsr_expert_combine(pointer(Ys), code, y.rows, y.cols, y.ld, typed<int32_t>(slots), slots.size(0), slots.size(1),
+                                weights, pointer(out.get()), ldo, stream.handle());
+    });
+    return rc != BSR_OK ? code_result(rc) : out.result();
+  });
+}
+
+// (Ys, slots, order, weights, dOut, dYs, dweights, stream) -> (dYs, dweights)
+PyObject *expert_combine_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &Ys = tensor(a[0], "Ys"), &dOut = tensor(a[4], "dOut");
+    const Dense y = dense2d(Ys, "Ys"), g = matrix_like(dOut, "dOut", Ys);
+    const at::Tensor &slots = routing(a[1], Ys);
+    if (g.rows != slots.size(0) || g.cols != y.cols) value_error("dOut must have a row for each row of slots, as wide as Ys");
+    const at::Tensor &order = packed(a[2], "order", Ys, at::kInt, {y.rows});
+    const at::Tensor &weights = packed(a[3], "weights", Ys, at::kFloat, slots.sizes());
+    const int code = dtype_code(Ys);
+    if (code < 0) return code_result(code);
+    const CallStream stream(a[7], Ys);
+    int64_t ldd;
+    const Output dYs = matrix_output(a[5], "dYs", y.rows, y.cols, Ys.scalar_type(), Ys, &ldd);
+    const Output dweights = packed_output(a[6], "dweights", slots.sizes(), at::kFloat, Ys);
+    const int rc = released([&] {
+      return bsr_expert_combine_grad(pointer(Ys), code, y.rows, y.cols, y.ld, typed<int32_t>(slots), typed<int32_t>(order),
+                                     slots.size(0), slots.size(1), typed<float>(weights), pointer(dOut), g.ld, pointer(dYs.get()),
+                                     ldd, typed<float>(dweights.get()), stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return Py_BuildValue("(NN)", dYs.result(), dweights.result());
+  });
+}
+
+// The tensors that every distillation call starts with: (logits, ids, teacher, temperature).
+struct DistillCall {
+  const at::Tensor &logits, &ids, &teacher;
+  Dense z;
+  int64_t K = 0;
+  int code, index, teacher_code;
+  float temperature;
+  DistillCall(PyObject *const *a)
+      : logits(tensor(a[0], "logits")), ids(tensor(a[1], "ids")), teacher(tensor(a[2], "teacher")), z(dense2d(logits, "logits")) {
+    (void)packed(a[1], "ids", logits);
+    (void)packed(a[2], "teacher", logits);
+    if (ids.dim() != 2 || ids.size(0) != z.rows || teacher.sizes() != ids.sizes())
+      value_error("ids and teacher must be [rows of logits, entries]");
+    K = ids.size(1);
+    code = dtype_code(logits);
+    index = index_code(ids);
+    teacher_code = dtype_code(teacher);
+    temperature = (float)real(a[3]);
+  }
+  bool types() const { return code >= 0 && index >= 0 && teacher_code >= 0; }
+  size_t workspace() const { return bsr_distill_workspace_bytes(z.rows, z.cols, K); }
+};
+
+// (logits, ids, teacher, temperature, loss, stats, ws, stream) -> (loss, stats)
+PyObject *distill_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const DistillCall c(a);
+    if (!c.types()) return code_result(BSR_ERR_DTYPE);
+    const CallStream stream(a[7], c.logits);
+    const Output loss = packed_output(a[4], "loss", {c.z.rows}, at::kFloat, c.logits);
+    const Output stats = packed_output(a[5], "stats", {c.z.rows, 2}, at::kFloat, c.logits);
+    const Workspace ws(a[6], a[6] == Py_None ? c.workspace() : 0, c.logits);
+    const int rc = released([&] {
+      return bsr_distill_loss(pointer(c.logits), c.code, c.z.rows, c.z.cols, c.z.ld, pointer(c.ids), c.index, pointer(c.teacher),
+                              c.teacher_code, c.K, c.temperature, typed<float>(loss.get()), typed<float>(stats.get()), ws.p,
+                              ws.bytes, stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return Py_BuildValue("(NN)", loss.result(), stats.result());
+  });
+}
+
+// (logits, ids, teacher, temperature, stats, dloss, dlogits, stream) -> dlogits
+PyObject *distill_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const DistillCall c(a);
+    if (!c.types()) return code_result(BSR_ERR_DTYPE);
+    const at::Tensor &stats = packed(a[4], "stats", c.logits, at::kFloat, {c.z.rows, 2});
+    const at::Tensor &dloss = packed(a[5], "dloss", c.logits, at::kFloat, {c.z.rows});
+    const CallStream stream(a[7], c.logits);
+    int64_t ldd;
+    const Output dlogits = matrix_output(a[6], "dlogits", c.z.rows, c.z.cols, c.logits.scalar_type(), c.logits, &ldd);
+    const int rc = released([&] {
+      return bsr_distill_grad(pointer(c.logits), c.code, c.z.rows, c.z.cols, c.z.ld, pointer(c.ids), c.index, pointer(c.teacher),
+                              c.teacher_code, c.K, c.temperature, typed<float>(stats), typed<float>(dloss), pointer(dlogits.get()),
+                              ldd, stream.handle());
+    });
+    return rc != BSR_OK ? code_result(rc) : dlogits.result();
+  });
+}
+
+// (logits, ids, teacher, temperature, dloss, loss, dlogits, ws, stream) -> (loss, dlogits)
+PyObject *distill_loss_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 9)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const DistillCall c(a);
+    if (!c.types()) return code_result(BSR_ERR_DTYPE);
+    const at::Tensor &dloss = packed(a[4], "dloss", c.logits, at::kFloat, {c.z.rows});
+    const CallStream stream(a[8], c.logits);
+    const Output loss = packed_output(a[5], "loss", {c.z.rows}, at::kFloat, c.logits);
+    int64_t ldd;
+    const Output dlogits = matrix_output(a[6], "dlogits", c.z.rows, c.z.cols, c.logits.scalar_type(), c.logits, &ldd);
+    const Workspace ws(a[7], a[7] == Py_None ? c.workspace() : 0, c.logits);
+    const int rc = released([&] {
+      return bsr_distill_loss_grad(pointer(c.logits), c.code, c.z.rows, c.z.cols, c.z.ld, pointer(c.ids), c.index,
+                                   pointer(c.teacher), c.teacher_code, c.K, c.temperature, typed<float>(dloss),
+                                   typed<float>(loss.get()), pointer(dlogits.get()), ldd, ws.p, ws.bytes, stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return Py_BuildValue("(NN)", loss.result(), dlogits.result());
+  });
+}
+
 // () -> handle of the current stream of the current device
 PyObject *current_stream(PyObject *, PyObject *) {
   return guarded([&]() -> PyObject * { return PyLong_FromVoidPtr(c10::hip::getCurrentHIPStream().stream()); });
@@ -343,6 +671,15 @@ PyMethodDef methods[] = {
     {"decompress", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(decompress)), METH_FASTCALL, nullptr},
     {"t_dense_matmul", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(t_dense_matmul)), METH_FASTCALL, nullptr},
     {"affine_scale_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(affine_scale_grad)), METH_FASTCALL, nullptr},
+    {"embedding_lookup", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(embedding_lookup)), METH_FASTCALL, nullptr},
+    {"embedding_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(embedding_grad)), METH_FASTCALL, nullptr},
+    {"expert_sort", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(expert_sort)), METH_FASTCALL, nullptr},
+    {"expert_gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(expert_gather)), METH_FASTCALL, nullptr},
+    {"expert_combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(expert_combine)), METH_FASTCALL, nullptr},
+    {"expert_combine_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(expert_combine_grad)), METH_FASTCALL, nullptr},
+    {"distill_loss", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(distill_loss)), METH_FASTCALL, nullptr},
+    {"distill_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(distill_grad)), METH_FASTCALL, nullptr},
+    {"distill_loss_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(distill_loss_grad)), METH_FASTCALL, nullptr},
     {"current_stream", current_stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
