@@ -10,6 +10,7 @@
 // Bound by memory: N * V logits in, as many gradients out.  A row is cut into chunks where there are few rows, so that every
 // compute unit has some (row_chunks): the first kernel leaves every chunk's (maximum, sum), the second joins those of its row and
 // writes its chunk of the gradient.
+#include "buffer_access.h"
 #include "token_step.h"
 
 namespace bsr {
@@ -19,7 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kAhead = 4;                      // vectors of a lane on their way
-constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float minus_inf() { return -__builtin_inff(); }
@@ -43,7 +44,7 @@ __device__ __forceinline__ int64_t entry_column(const Distill &a, int64_t i) {
   return v >= 0 && v < a.V ? v : -1;
 }
 
-// maximum and sum over the workgroup; `red` is shared, one float per wave, and free again after the next barrier
+// Maximum and sum over a workgroup of WAVES waves; `red` is shared, one float per wave, and free again after the next barrier.
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
@@ -54,27 +55,230 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
   return v;
 }
+// (The waves' values are read one per lane and combined by lane exchanges: all of them in every lane would be as many registers.)
+template <int WAVES>
 __device__ __forceinline__ float group_max(float v, float *red) {
   v = wave_max(v);
+  if (WAVES == 1) return v;
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = red[0];
+  v = red[threadIdx.x & (WAVES - 1)];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) v = fmaxf(v, red[w]);
+  for (int d = WAVES / 2; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
   return v;
 }
+template <int WAVES>
 __device__ __forceinline__ float group_sum(float v, float *red) {
   v = wave_sum(v);
+  if (WAVES == 1) return v;
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = red[0];
+  v = red[threadIdx.x & (WAVES - 1)];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) v += red[w];
+  for (int d = WAVES / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
   return v;
 }
 
-// (z - m) with the maximum of a part without any finite or +inf value taken as 0
+// Maximum as the base of differences: 0 for a part without any finite or +inf value.
 __device__ __forceinline__ float base_of(float m) { return m == minus_inf() ? 0.0f : m; }
+
+// The exponents of a row's logits, (z - m) * c, in one multiply-add each: fma(z, c, -mc).  What m * c loses by its rounding is
+// the same for every logit: the true exponent is smaller by `lost`.  Where m * c might overflow (|m| above 1e30 / c: a row of nothing
+// but the type's lowest value, say) logits that differ from m differ by so much that their exponential is 0 with any c that is not
+// tiny, and 2^-30 takes its place: m * 2^-30 is exact.
+struct Exponent {
+  float c, mc, lost;
+  __device__ __forceinline__ Exponent(float m, float c_) {
+    c = fabsf(m * c_) <= 1e30f || m != m ? c_ : 0x1p-30f;
+    mc = m * c;
+    lost = fabsf(m) < __builtin_inff() ? fmaf(m, c, -mc) : 0.0f;
+  }
+  __device__ __forceinline__ float at(float z) const { return fmaf(z, c, -mc); }
+};
+
+// g * exp((z - m) / tau) / S in one multiply-add, exponential and product: the logarithm of S goes into the constant of the exponent,
+// and what that sum's rounding loses into the factor.
+struct Share {
+  float c, k, g;
+  // log2_s: of the sum of 2^at(z)
+  __device__ __forceinline__ Share(const Exponent &ex, float log2_s, float g_) : c(ex.c) {
+    k = ex.mc + log2_s;
+    const float hi = k - ex.mc, lo = (ex.mc - (k - hi)) + (log2_s - hi);
+    g = g_ * exp2_of(fabsf(k) < __builtin_inff() ? -lo : 0.0f);
+  }
+  __device__ __forceinline__ float at(float z) const { return g * exp2_of(fmaf(z, c, -k)); }
+};
+
+// Columns [lo, hi) of a row as `head` single ones up to the next 16-byte boundary, whole vectors, and single ones again.
+struct Cut {
+  int64_t head, vecs, singles;
+  template <typename T>
+  __device__ __forceinline__ Cut(const T *row, int64_t lo, int64_t hi) {
+    constexpr int VE = 16 / (int)sizeof(T);
+    const int64_t off = (int64_t)((16 - ((uintptr_t)(row + lo) & 15)) & 15) / (int)sizeof(T);
+    head = off < hi - lo ? off : hi - lo;
+    vecs = (hi - lo - head) / VE;
+    singles = hi - lo - vecs * VE;
+  }
+  // column of single i < singles
+  template <int VE>
+  __device__ __forceinline__ int64_t single(int64_t lo, int64_t i) const { return lo + (i < head ? i : i + vecs * VE); }
+};
+
+// A row's entries in shared memory.
+struct Entries {
+  int32_t *at;                                 // columns, -1: no entry
+  float *share;                                // teacher's logits, then e_j
+  float *z;                                    // student's logits there
+  __device__ __forceinline__ Entries(void *lds, int K)
+      : at(static_cast<int32_t *>(lds)), share(static_cast<float *>(lds) + K), z(static_cast<float *>(lds) + 2 * K) {}
+};
+size_t entries_bytes(int64_t K) { return (size_t)K * 3 * sizeof(float); }
+
+// The row's entries to shared memory; returns the lane's largest teacher logit.  z_of(j, column): the logit at entry j.
+template <int THREADS, typename F>
+__device__ __forceinline__ float load_entries(const Distill &a, int64_t n, const Entries &en, F z_of) {
+  float top = minus_inf();
+  for (int j = threadIdx.x; j < a.K; j += THREADS) {
+    const int64_t v = entry_column(a, n * a.K + j);
+    const float x = v >= 0 ? teacher_logit(a, n * a.K + j) : minus_inf();
+    en.at[j] = (int32_t)v;
+    en.share[j] = x;
+    en.z[j] = z_of(j, v);
+    top = fmaxf(top, x);
+  }
+  return top;
+}
+
+// e_j in place of the teacher's logits, and the lane's sums of e_j and of e_j * ((t_j - max t) - (z_j - m)).
+template <int THREADS>
+__device__ __forceinline__ void weigh_entries(const Distill &a, const Entries &en, float top, float m, float *e_sum, float *cross) {
+  const bool none = top == minus_inf();
+  *e_sum = 0.0f;
+  *cross = 0.0f;
+  for (int j = threadIdx.x; j < a.K; j += THREADS) {
+    const float x = en.share[j] - top, e = none || en.at[j] < 0 ? 0.0f : exp2_of(x * a.c);
+    en.share[j] = e;
+    *e_sum += e;
+    if (e != 0.0f) *cross = fmaf(e, x - (en.z[j] - m), *cross);
+  }
+}
+
+// Teacher's shares subtracted from the gradient at the entries' columns in [lo, hi), once those columns are written and the
+// workgroup has met at a barrier.  A column that several entries share gets all of them, from every one of its entries alike.
+template <int THREADS, typename T>
+__device__ __forceinline__ void subtract_entries(const Distill &a, const Entries &en, float total, float g, int64_t lo, int64_t hi,
+                                                 T *out, const Share &share) {
+  const float by = 1.0f / total;
+  for (int j = threadIdx.x; j < a.K; j += THREADS) {
+    const int32_t v = en.at[j];
+    if (v < lo || v >= hi) continue;
+    float q = 0.0f;
+    for (int i = 0; i < a.K; ++i) q += en.at[i] == v ? en.share[i] : 0.0f;
+    out[v] = from_float<T>(share.at(en.z[j]) - g * (q * by));
+  }
+}
+
+__device__ __forceinline__ float loss_of(const Distill &a, float cross, float total, float log_s) {
+  return a.tau * a.tau * (cross / (a.tau * total) - logf(total) + log_s);
+}
+
+// ---- a row in registers: loss and gradient in one pass ----
+
+// One workgroup per row, whose lanes keep R vectors each: the logits are read once.  alike: the rows of dlogits start as far from a
+// 16-byte boundary as those of the logits.  The row has a whole vector at least.
+template <typename T, int THREADS, int R_>
+__global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(Distill a, const float *__restrict__ dloss, float *__restrict__ loss,
+                                                              T *dlogits, int64_t ldd, bool alike) {
+  constexpr int VE = 16 / (int)sizeof(T), WAVES = THREADS / 64;
+  constexpr uint32_t kNothing = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;       // -inf, for vectors behind the row
+  typedef RowVec<T, VE> R;
+  extern __shared__ uint32_t lds[];
+  __shared__ float red[5][WAVES];
+  const Entries en(lds, a.K);
+  const int t = threadIdx.x;
+  const int64_t n = blockIdx.x;
+  const T *row = static_cast<const T *>(a.logits) + n * a.ldz;
+  const Cut cut(row, 0, a.V);
+  // the whole vectors as a buffer: accesses behind them are neither loads nor stores
+  const int vecs = (int)cut.vecs;
+  const __amdgpu_buffer_rsrc_t body = make_rsrc(row + cut.head, (uint32_t)vecs * 16u);
+  Words4 x[R_];
+#pragma unroll
+  for (int r = 0; r < R_; ++r) x[r] = buffer_load<16>(body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u);
+  const bool one = t < cut.singles;
+  const int64_t single = cut.single<VE>(0, one ? t : 0);
+  const float zs = one ? elem_to_float<T>(row[single]) : minus_inf();
+  const float tm = load_entries<THREADS>(a, n, en, [&](int, int64_t v) { return v >= 0 ? elem_to_float<T>(row[v]) : 0.0f; });
+  float m = zs;
+#pragma unroll
+  for (int r = 0; r < R_; ++r) {
+    // (Here and below: one vector after the other, unpacked anew in each pass.  Left to itself the compiler works on all of them
+    // at a time and keeps every element as binary32 from one pass to the next, several times the registers.)
+    asm volatile("" : "+v"(x[r]));
+    if ((r + 1) * THREADS > vecs) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[r][i] = r * THREADS + t < vecs ? x[r][i] : kNothing;
+    }
+#pragma unroll
+    for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(x[r], q));
+    asm volatile("" : "+v"(m));
+  }
+  m = group_max<WAVES>(m, red[0]);
+  const float top = group_max<WAVES>(tm, red[1]);
+  const bool none = top == minus_inf();
+  T *out = dlogits + n * ldd;
+  const __amdgpu_buffer_rsrc_t out_body = make_rsrc(out + cut.head, (uint32_t)vecs * 16u);
+  const Exponent ex(m, a.c);
+  auto put = [&](auto f) {
+#pragma unroll
+    for (int r = 0; r < R_; ++r) {
+      asm volatile("" : "+v"(x[r]));
+      float v[VE];
+#pragma unroll
+      for (int q = 0; q < VE; ++q) v[q] = f(R::elem(x[r], q));
+      const Words4 w = pack_row<T, VE>(v);
+      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, 0);
+      else if (r * THREADS + t < vecs) R::store(out + cut.head + (int64_t)(r * THREADS + t) * VE, w);
+    }
+    if (one) out[single] = from_float<T>(f(zs));
+  };
+  if (none) {
+    if (t == 0) loss[n] = 0.0f;
+    put([](float) { return 0.0f; });
+    return;
+  }
+  float e_sum, cross;
+  float acc[4] = {exp2_of(ex.at(zs)), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int r = 0; r < R_; ++r) {
+    asm volatile("" : "+v"(x[r]));
+#pragma unroll
+    for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(x[r], q)));
+    asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
+  }
+  weigh_entries<THREADS>(a, en, top, m, &e_sum, &cross);
+  const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[2]);
+  const float total = group_sum<WAVES>(e_sum, red[3]), x_sum = group_sum<WAVES>(cross, red[4]);
+  const float log2_s = m == minus_inf() ? __builtin_nanf("") : log2f(s);
+  if (t == 0) loss[n] = loss_of(a, x_sum, total, (log2_s - ex.lost) * kLn2);
+  const float g = dloss[n] * a.tau;
+  const Share share(ex, log2_s, g);
+  put([&](float z) { return share.at(z); });
+  __syncthreads();
+  subtract_entries<THREADS>(a, en, total, g, 0, a.V, out, share);
+}
+
+// ---- a row in chunks: two passes over the logits ----
+
+// Columns of chunk i: boundaries are multiples of a.chunk behind the row's first 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ void chunk_of(const Distill &a, const T *row, int64_t i, int64_t *lo, int64_t *hi) {
+  const int64_t head = (int64_t)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T);
+  const int64_t l = i == 0 ? 0 : i * a.chunk + head, h = (i + 1) * a.chunk + head;
+  *hi = i == a.chunks - 1 || h > a.V ? a.V : h;
+  *lo = l < *hi ? l : *hi;
+}
 
 // parts[n][chunk] = (maximum, sum of exp((z - maximum) / tau)) of a chunk; the first chunk's workgroup also leaves the logits at
 // the row's entries in picked[n][j].
@@ -92,38 +296,47 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill a, floa
       picked[n * a.K + j] = v >= 0 ? elem_to_float<T>(row[v]) : 0.0f;
     }
   }
-  const int64_t lo = blockIdx.x * a.chunk, hi = lo + a.chunk < a.V ? lo + a.chunk : a.V;
-  const int64_t vecs = (hi - lo) / VE;
+  int64_t lo, hi;
+  chunk_of(a, row, blockIdx.x, &lo, &hi);
+  const Cut cut(row, lo, hi);
+  const Words4 *body = reinterpret_cast<const Words4 *>(row + lo + cut.head);
   float m = minus_inf(), s = 0.0f;
-  for (int64_t v0 = t; v0 < vecs; v0 += kAhead * kThreads) {
-    typename R::Raw x[kAhead];
+  if (t < cut.singles) {
+    m = elem_to_float<T>(row[cut.single<VE>(lo, t)]);
+    s = exp2_of((m - base_of(m)) * a.c);
+  }
+  auto take = [&](auto load) {
+    Words4 x[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (v0 + u * kThreads < vecs) x[u] = R::load(row + lo + (v0 + u * kThreads) * VE);
+    for (int u = 0; u < kAhead; ++u) x[u] = load(u);
     float top = m;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (v0 + u * kThreads < vecs) {
+    for (int u = 0; u < kAhead; ++u) {
 #pragma unroll
-        for (int q = 0; q < VE; ++q) top = fmaxf(top, R::elem(x[u], q));
-      }
+      for (int q = 0; q < VE; ++q) top = fmaxf(top, R::elem(x[u], q));
+    }
     const float base = base_of(top);
-    s *= exp2_of((m - base) * a.c);
+    float acc[4] = {s * exp2_of((m - base) * a.c), 0.0f, 0.0f, 0.0f};
     m = top;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (v0 + u * kThreads < vecs) {
+    for (int u = 0; u < kAhead; ++u) {
 #pragma unroll
-        for (int q = 0; q < VE; ++q) s += exp2_of((R::elem(x[u], q) - base) * a.c);
-      }
+      for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of((R::elem(x[u], q) - base) * a.c);
+    }
+    s = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+  };
+  int64_t v = t;
+  for (; v + (kAhead - 1) * kThreads < cut.vecs; v += kAhead * kThreads) take([&](int u) { return body[v + u * kThreads]; });
+  if (v < cut.vecs) {
+    constexpr uint32_t kNothing = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;     // -inf
+    take([&](int u) {
+      Words4 w = {kNothing, kNothing, kNothing, kNothing};
+      if (v + u * kThreads < cut.vecs) w = body[v + u * kThreads];
+      return w;
+    });
   }
-  for (int64_t v = lo + vecs * VE + t; v < hi; v += kThreads) {
-    const float z = elem_to_float<T>(row[v]), top = fmaxf(m, z), base = base_of(top);
-    s = s * exp2_of((m - base) * a.c) + exp2_of((z - base) * a.c);
-    m = top;
-  }
-  const float top = group_max(m, red[0]), base = base_of(top);
-  const float sum = group_sum(s * exp2_of((m - base) * a.c), red[1]);
+  const float top = group_max<kWaves>(m, red[0]), base = base_of(top);
+  const float sum = group_sum<kWaves>(s * exp2_of((m - base) * a.c), red[1]);
   if (t == 0) parts[n * a.chunks + blockIdx.x] = float2{top, sum};
 }
 
@@ -136,58 +349,46 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
                                                                   const float *__restrict__ dloss, T *dlogits, int64_t ldd) {
   constexpr int VE = 16 / (int)sizeof(T);
   typedef RowVec<T, VE> R;
-  __shared__ int32_t at[kMaxTeacher];          // columns, -1: no entry
-  __shared__ float share[kMaxTeacher];         // e_j
-  __shared__ float zs[kMaxTeacher];            // logits there
-  __shared__ float red[6][kWaves];
+  extern __shared__ uint32_t lds[];
+  __shared__ float red[5][kWaves];
+  const Entries en(lds, a.K);
   const int t = threadIdx.x;
   const int64_t n = blockIdx.y;
   const T *row = static_cast<const T *>(a.logits) + n * a.ldz;
-  const int64_t lo = GRAD ? blockIdx.x * a.chunk : 0;
-  const int64_t hi = !GRAD || lo + a.chunk > a.V ? a.V : lo + a.chunk;
-  float tm = minus_inf();
-  for (int j = t; j < a.K; j += kThreads) {
-    const int64_t v = entry_column(a, n * a.K + j);
-    const float x = v >= 0 ? teacher_logit(a, n * a.K + j) : minus_inf();
-    at[j] = (int32_t)v;
-    share[j] = x;
-    // (only columns of this chunk are read from the row: others may be overwritten by their own chunk's workgroup by now)
-    zs[j] = FROM_PARTS ? picked[n * a.K + j] : v >= lo && v < hi ? elem_to_float<T>(row[v]) : 0.0f;
-    tm = fmaxf(tm, x);
-  }
+  int64_t lo = 0, hi = a.V;
+  if (GRAD) chunk_of(a, row, blockIdx.x, &lo, &hi);
+  // (only columns of this chunk are read from the row: others may be overwritten by their own chunk's workgroup by now)
+  const float tm = load_entries<kThreads>(a, n, en, [&](int j, int64_t v) {
+    return FROM_PARTS ? picked[n * a.K + j] : v >= lo && v < hi ? elem_to_float<T>(row[v]) : 0.0f;
+  });
   float m, log_s;
   if constexpr (FROM_PARTS) {
     float pm = minus_inf();
     for (int i = t; i < parts_per_row; i += kThreads) pm = fmaxf(pm, parts[n * parts_per_row + i].x);
-    m = group_max(pm, red[0]);
+    m = group_max<kWaves>(pm, red[0]);
     const float base = base_of(m);
     float ps = 0.0f;
     for (int i = t; i < parts_per_row; i += kThreads) {
       const float2 p = parts[n * parts_per_row + i];
       ps += p.y * exp2_of((p.x - base) * a.c);
     }
-    const float s = group_sum(ps, red[1]);
+    const float s = group_sum<kWaves>(ps, red[1]);
     log_s = m == minus_inf() ? __builtin_nanf("") : logf(s);
   } else {
     const float2 st = stats[n];
     m = st.x;
     log_s = st.y;
   }
-  const float top = group_max(tm, red[2]);
+  const float top = group_max<kWaves>(tm, red[2]);
   const bool none = top == minus_inf();
-  float e_sum = 0.0f, cross = 0.0f;
-  for (int j = t; j < a.K; j += kThreads) {
-    const float x = share[j] - top, e = none || at[j] < 0 ? 0.0f : exp2_of(x * a.c);
-    share[j] = e;
-    e_sum += e;
-    if (e != 0.0f) cross = fmaf(e, x - (zs[j] - m), cross);
-  }
-  const float total = group_sum(e_sum, red[3]);
+  float e_sum, cross;
+  weigh_entries<kThreads>(a, en, top, m, &e_sum, &cross);
+  const float total = group_sum<kWaves>(e_sum, red[3]);
   if constexpr (FROM_PARTS) {
     if (blockIdx.x == 0) {
-      const float x = group_sum(cross, red[4]);
+      const float x = group_sum<kWaves>(cross, red[4]);
       if (t == 0) {
-        loss[n] = none ? 0.0f : a.tau * a.tau * (x / (a.tau * total) - logf(total) + log_s);
+        loss[n] = none ? 0.0f : loss_of(a, x, total, log_s);
         if (stats != nullptr) stats[n] = float2{m, log_s};
       }
     }
@@ -195,34 +396,41 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
   if constexpr (GRAD) {
     T *out = dlogits + n * ldd;
     const float g = none ? 0.0f : dloss[n] * a.tau;
-    const float log2_s = log_s * kLog2E;
-    auto grad = [&](float z) { return none ? 0.0f : g * exp2_of(fmaf(z - m, a.c, -log2_s)); };
-    const int64_t vecs = (hi - lo) / VE;
-    for (int64_t v0 = t; v0 < vecs; v0 += kAhead * kThreads) {
-      typename R::Raw x[kAhead];
+    const Exponent ex(m, a.c);
+    const Share share(ex, log_s * kLog2E + ex.lost, g);
+    const Cut cut(row, lo, hi);
+    const Words4 *body = reinterpret_cast<const Words4 *>(row + lo + cut.head);
+    T *out_body = out + lo + cut.head;
+    auto run = [&](auto f) {
+      auto take = [&](int64_t v, auto in) {
+        Words4 x[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (v0 + u * kThreads < vecs) x[u] = R::load(row + lo + (v0 + u * kThreads) * VE);
+        for (int u = 0; u < kAhead; ++u)
+          if (in(u)) x[u] = body[v + u * kThreads];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (v0 + u * kThreads < vecs) {
-          float f[VE];
+        for (int u = 0; u < kAhead; ++u)
+          if (in(u)) {
+            float w[VE];
 #pragma unroll
-          for (int q = 0; q < VE; ++q) f[q] = grad(R::elem(x[u], q));
-          R::store(out + lo + (v0 + u * kThreads) * VE, pack_row<T, VE>(f));
-        }
+            for (int q = 0; q < VE; ++q) w[q] = f(R::elem(x[u], q));
+            R::store(out_body + (v + u * kThreads) * VE, pack_row<T, VE>(w));
+          }
+      };
+      int64_t v = t;
+      for (; v + (kAhead - 1) * kThreads < cut.vecs; v += kAhead * kThreads) take(v, [](int) { return true; });
+      if (v < cut.vecs) take(v, [&](int u) { return v + u * kThreads < cut.vecs; });
+      if (t < cut.singles) {
+        const int64_t c = cut.single<VE>(lo, t);
+        out[c] = from_float<T>(f(elem_to_float<T>(row[c])));
+      }
+    };
+    if (none) {
+      run([](float) { return 0.0f; });
+      return;
     }
-    for (int64_t v = lo + vecs * VE + t; v < hi; v += kThreads) out[v] = from_float<T>(grad(elem_to_float<T>(row[v])));
-    if (none) return;
+    run([&](float z) { return share.at(z); });
     __syncthreads();                           // the chunk is written; now the entries' columns again, with the teacher's shares
-    const float by = 1.0f / total;
-    for (int j = t; j < a.K; j += kThreads) {
-      const int32_t v = at[j];
-      if (v < lo || v >= hi) continue;
-      float q = 0.0f;
-      for (int i = 0; i < a.K; ++i) q += at[i] == v ? share[i] : 0.0f;
-      out[v] = from_float<T>(g * (exp2_of(fmaf(zs[j] - m, a.c, -log2_s)) - q * by));
-    }
+    subtract_entries<kThreads>(a, en, total, g, lo, hi, out, share);
   }
 }
 
@@ -252,6 +460,8 @@ size_t parts_bytes(int64_t N, int64_t V) {
   return align_up((size_t)N * chunks * sizeof(float2), 256);
 }
 
+constexpr int64_t kEnoughRows = 128;
+
 // Rows per launch: the grid's second dimension ends at 65535.
 constexpr int64_t kRowsPerLaunch = 65535;
 
@@ -264,10 +474,30 @@ Distill rows_from(const Distill &a, int64_t n, int dtype) {
   return b;
 }
 
+// One workgroup per row, at most.
+template <typename T, int THREADS, int R>
+int run_rows(const Distill &a, const float *dloss, float *loss, void *dlogits, int64_t ldd, hipStream_t s) {
+  const bool alike = ((uintptr_t)dlogits - (uintptr_t)a.logits) % 16 == 0 && (ldd - a.ldz) * (int64_t)sizeof(T) % 16 == 0;
+  hipLaunchKernelGGL((distill_row_kernel<T, THREADS, R>), dim3((unsigned)a.N), dim3(THREADS), entries_bytes(a.K), s, a, dloss, loss,
+                     static_cast<T *>(dlogits), ldd, alike);
+  return check_launch();
+}
+
 template <typename T, bool GRAD>
 int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats, void *dlogits, int64_t ldd, void *ws,
              hipStream_t s) {
   const Distill a = describe(d);
+  if constexpr (GRAD) {
+    const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
+    if (vecs >= 2 && (a.chunks == 1 || a.N >= kEnoughRows)) {
+      if (vecs <= 256) return run_rows<T, 64, 4>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 1024) return run_rows<T, 256, 4>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 2048) return run_rows<T, 256, 8>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 4096) return run_rows<T, 512, 8>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 8192) return run_rows<T, 1024, 8>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 16384) return run_rows<T, 1024, 16>(a, dloss, loss, dlogits, ldd, s);
+    }
+  }
   float2 *parts = static_cast<float2 *>(ws);
   float *picked = reinterpret_cast<float *>(static_cast<char *>(ws) + parts_bytes(d.N, d.V));
   for (int64_t n = 0; n < d.N; n += kRowsPerLaunch) {
@@ -276,7 +506,8 @@ int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats
                        picked + n * a.K);
     int rc = check_launch();
     if (rc != BSR_OK) return rc;
-    hipLaunchKernelGGL((distill_finish_kernel<T, true, GRAD>), dim3(GRAD ? a.chunks : 1, (unsigned)b.N), dim3(kThreads), 0, s, b,
+    hipLaunchKernelGGL((distill_finish_kernel<T, true, GRAD>), dim3(GRAD ? a.chunks : 1, (unsigned)b.N), dim3(kThreads),
+                       entries_bytes(a.K), s, b,
                        parts + n * a.chunks, a.chunks, picked + n * a.K, loss + n,
                        stats != nullptr ? reinterpret_cast<float2 *>(stats) + n : nullptr, dloss + (dloss != nullptr ? n : 0),
                        dlogits != nullptr ? static_cast<T *>(dlogits) + n * ldd : nullptr, ldd);
@@ -291,8 +522,8 @@ int run_grad(const DistillArgs &d, const float *stats, const float *dloss, void 
   const Distill a = describe(d);
   for (int64_t n = 0; n < d.N; n += kRowsPerLaunch) {
     const Distill b = rows_from(a, n, d.dtype);
-    hipLaunchKernelGGL((distill_finish_kernel<T, false, true>), dim3(a.chunks, (unsigned)b.N), dim3(kThreads), 0, s, b,
-                       nullptr, 0, nullptr, nullptr, reinterpret_cast<float2 *>(const_cast<float *>(stats)) + n, dloss + n,
+    hipLaunchKernelGGL((distill_finish_kernel<T, false, true>), dim3(a.chunks, (unsigned)b.N), dim3(kThreads),
+                       entries_bytes(a.K), s, b, nullptr, 0, nullptr, nullptr, reinterpret_cast<float2 *>(const_cast<float *>(stats)) + n, dloss + n,
                        static_cast<T *>(dlogits) + n * ldd, ldd);
     const int rc = check_launch();
     if (rc != BSR_OK) return rc;
