@@ -59,7 +59,11 @@ __device__ __forceinline__ float wave_sum(float v) {
 template <int WAVES>
 __device__ __forceinline__ float group_max(float v, float *red) {
   v = wave_max(v);
-  if (WAVES == 1) return v;
+  if (WAVES == 1) {                            // (what the lanes wrote to LDS before is there for the others, as behind a barrier)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    return v;
+  }
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   v = red[threadIdx.x & (WAVES - 1)];
@@ -70,7 +74,11 @@ __device__ __forceinline__ float group_max(float v, float *red) {
 template <int WAVES>
 __device__ __forceinline__ float group_sum(float v, float *red) {
   v = wave_sum(v);
-  if (WAVES == 1) return v;
+  if (WAVES == 1) {                            // (what the lanes wrote to LDS before is there for the others, as behind a barrier)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    return v;
+  }
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   v = red[threadIdx.x & (WAVES - 1)];
@@ -130,58 +138,81 @@ struct Entries {
   int32_t *at;                                 // columns, -1: no entry
   float *share;                                // teacher's logits, then e_j
   float *z;                                    // student's logits there
+  float *q;                                    // e_j of all entries of the same column
   __device__ __forceinline__ Entries(void *lds, int K)
-      : at(static_cast<int32_t *>(lds)), share(static_cast<float *>(lds) + K), z(static_cast<float *>(lds) + 2 * K) {}
+      : at(static_cast<int32_t *>(lds)), share(static_cast<float *>(lds) + K), z(static_cast<float *>(lds) + 2 * K),
+        q(static_cast<float *>(lds) + 3 * K) {}
 };
-size_t entries_bytes(int64_t K) { return (size_t)K * 3 * sizeof(float); }
+size_t entries_bytes(int64_t K) { return (size_t)K * 4 * sizeof(float); }
 
-// The row's entries to shared memory; returns the lane's largest teacher logit.  z_of(j, column): the logit at entry j.
-template <int THREADS, typename F>
-__device__ __forceinline__ float load_entries(const Distill &a, int64_t n, const Entries &en, F z_of) {
-  float top = minus_inf();
-  for (int j = threadIdx.x; j < a.K; j += THREADS) {
-    const int64_t v = entry_column(a, n * a.K + j);
-    const float x = v >= 0 ? teacher_logit(a, n * a.K + j) : minus_inf();
-    en.at[j] = (int32_t)v;
-    en.share[j] = x;
-    en.z[j] = z_of(j, v);
-    top = fmaxf(top, x);
-  }
-  return top;
+// Entry j of row n: its column (-1: none) and the teacher's logit (-inf: none).
+__device__ __forceinline__ void load_entry(const Distill &a, int64_t n, int j, int64_t *v, float *x) {
+  *v = entry_column(a, n * a.K + j);
+  *x = *v >= 0 ? teacher_logit(a, n * a.K + j) : minus_inf();
 }
 
-// e_j in place of the teacher's logits, and the lane's sums of e_j and of e_j * ((t_j - max t) - (z_j - m)).
+// e_j in place of the teacher's logits; returns the lane's sum.  top: their maximum.
 template <int THREADS>
-__device__ __forceinline__ void weigh_entries(const Distill &a, const Entries &en, float top, float m, float *e_sum, float *cross) {
-  const bool none = top == minus_inf();
-  *e_sum = 0.0f;
-  *cross = 0.0f;
+__device__ __forceinline__ float weigh_entries(const Distill &a, const Entries &en, float top) {
+  float sum = 0.0f;
   for (int j = threadIdx.x; j < a.K; j += THREADS) {
-    const float x = en.share[j] - top, e = none || en.at[j] < 0 ? 0.0f : exp2_of(x * a.c);
+    const float e = top == minus_inf() || en.at[j] < 0 ? 0.0f : exp2_of((en.share[j] - top) * a.c);
     en.share[j] = e;
-    *e_sum += e;
-    if (e != 0.0f) *cross = fmaf(e, x - (en.z[j] - m), *cross);
+    sum += e;
   }
+  return sum;
 }
 
-// Teacher's shares subtracted from the gradient at the entries' columns in [lo, hi), once those columns are written and the
-// workgroup has met at a barrier.  A column that several entries share gets all of them, from every one of its entries alike.
-template <int THREADS, typename T>
-__device__ __forceinline__ void subtract_entries(const Distill &a, const Entries &en, float total, float g, int64_t lo, int64_t hi,
-                                                 T *out, const Share &share) {
-  const float by = 1.0f / total;
+// The lane's sum of e_j * log(e_j / exp((z_j - m) / tau)), in which the teacher's part is the sum of e_j * (t_j - top) = e_j * tau * log(e_j).
+template <int THREADS>
+__device__ __forceinline__ float cross_entries(const Distill &a, const Entries &en, float m) {
+  float sum = 0.0f;
+  for (int j = threadIdx.x; j < a.K; j += THREADS) {
+    const float e = en.share[j];
+    if (e != 0.0f) sum = fmaf(e, a.tau * kLn2 * log2f(e) - (en.z[j] - m), sum);
+  }
+  return sum;
+}
+
+// e_j of all entries of a column together, for every one of them; once all e_j are there.
+template <int THREADS>
+__device__ __forceinline__ void merge_entries(const Distill &a, const Entries &en) {
   for (int j = threadIdx.x; j < a.K; j += THREADS) {
     const int32_t v = en.at[j];
-    if (v < lo || v >= hi) continue;
     float q = 0.0f;
-    for (int i = 0; i < a.K; ++i) q += en.at[i] == v ? en.share[i] : 0.0f;
-    out[v] = from_float<T>(share.at(en.z[j]) - g * (q * by));
+#pragma unroll 8
+    for (int k = 0; k < a.K; ++k) q += en.at[k] == v ? en.share[k] : 0.0f;
+    en.q[j] = q;
+  }
+}
+
+// Teacher's shares subtracted from the gradient at the entries' columns in [lo, hi): every wave writes those columns once more
+// whose vectors it has written itself (vector i of the cut by wave i / 64 mod WAVES, single columns by the first), so that no wave
+// waits for another.  (A column that several entries share gets all of them, from every one of its entries alike.)
+template <int WAVES, typename T>
+__device__ __forceinline__ void subtract_entries(const Distill &a, const Entries &en, const Cut &cut, float total, float g, int64_t lo,
+                                                 int64_t hi, T *out, const Share &share) {
+  constexpr int VE = 16 / (int)sizeof(T);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float by = 1.0f / total;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // (the wave's stores before come first)
+  __builtin_amdgcn_wave_barrier();
+  for (int j = lane; j < a.K; j += 64) {
+    const int32_t v = en.at[j];
+    if (v < lo || v >= hi) continue;
+    const uint32_t i = (uint32_t)(v - lo - cut.head);
+    const bool single = v - lo < cut.head || i >= (uint32_t)(cut.vecs * VE);
+    if ((single ? 0u : i / (VE * 64u) % WAVES) != (uint32_t)wave) continue;
+    out[v] = from_float<T>(share.at(en.z[j]) - g * (en.q[j] * by));
   }
 }
 
 __device__ __forceinline__ float loss_of(const Distill &a, float cross, float total, float log_s) {
   return a.tau * a.tau * (cross / (a.tau * total) - logf(total) + log_s);
 }
+
+// Cache policy of buffer accesses: non-temporal, for what is not read again soon.
+constexpr int kStream = 2;
 
 // ---- a row in registers: loss and gradient in one pass ----
 
@@ -200,16 +231,31 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   const int64_t n = blockIdx.x;
   const T *row = static_cast<const T *>(a.logits) + n * a.ldz;
   const Cut cut(row, 0, a.V);
+  // The entries are on their way before the row, and what they need of each other is computed while the row is still coming.
   // the whole vectors as a buffer: accesses behind them are neither loads nor stores
   const int vecs = (int)cut.vecs;
   const __amdgpu_buffer_rsrc_t body = make_rsrc(row + cut.head, (uint32_t)vecs * 16u);
+  int64_t v0 = -1;
+  float x0 = minus_inf();
+  if (t < a.K) load_entry(a, n, t, &v0, &x0);
   Words4 x[R_];
 #pragma unroll
   for (int r = 0; r < R_; ++r) x[r] = buffer_load<16>(body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u);
   const bool one = t < cut.singles;
   const int64_t single = cut.single<VE>(0, one ? t : 0);
   const float zs = one ? elem_to_float<T>(row[single]) : minus_inf();
-  const float tm = load_entries<THREADS>(a, n, en, [&](int, int64_t v) { return v >= 0 ? elem_to_float<T>(row[v]) : 0.0f; });
+  float tm = x0;
+  for (int j = t; j < a.K; j += THREADS) {
+    if (j >= THREADS) load_entry(a, n, j, &v0, &x0);
+    en.at[j] = (int32_t)v0;
+    en.share[j] = x0;
+    en.z[j] = v0 >= 0 ? elem_to_float<T>(row[v0]) : 0.0f;
+    tm = fmaxf(tm, x0);
+  }
+  const float top = group_max<WAVES>(tm, red[0]);
+  const bool none = top == minus_inf();
+  const float total = group_sum<WAVES>(weigh_entries<THREADS>(a, en, top), red[1]);
+  merge_entries<THREADS>(a, en);
   float m = zs;
 #pragma unroll
   for (int r = 0; r < R_; ++r) {
@@ -224,9 +270,7 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(x[r], q));
     asm volatile("" : "+v"(m));
   }
-  m = group_max<WAVES>(m, red[0]);
-  const float top = group_max<WAVES>(tm, red[1]);
-  const bool none = top == minus_inf();
+  m = group_max<WAVES>(m, red[2]);
   T *out = dlogits + n * ldd;
   const __amdgpu_buffer_rsrc_t out_body = make_rsrc(out + cut.head, (uint32_t)vecs * 16u);
   const Exponent ex(m, a.c);
@@ -238,7 +282,7 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
 #pragma unroll
       for (int q = 0; q < VE; ++q) v[q] = f(R::elem(x[r], q));
       const Words4 w = pack_row<T, VE>(v);
-      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, 0);
+      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, kStream);
       else if (r * THREADS + t < vecs) R::store(out + cut.head + (int64_t)(r * THREADS + t) * VE, w);
     }
     if (one) out[single] = from_float<T>(f(zs));
@@ -248,7 +292,6 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     put([](float) { return 0.0f; });
     return;
   }
-  float e_sum, cross;
   float acc[4] = {exp2_of(ex.at(zs)), 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int r = 0; r < R_; ++r) {
@@ -257,16 +300,14 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(x[r], q)));
     asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
   }
-  weigh_entries<THREADS>(a, en, top, m, &e_sum, &cross);
-  const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[2]);
-  const float total = group_sum<WAVES>(e_sum, red[3]), x_sum = group_sum<WAVES>(cross, red[4]);
+  const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m), red[3]);
+  const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[4]);
   const float log2_s = m == minus_inf() ? __builtin_nanf("") : log2f(s);
-  if (t == 0) loss[n] = loss_of(a, x_sum, total, (log2_s - ex.lost) * kLn2);
+  if (t == 0) loss[n] = loss_of(a, cross, total, (log2_s - ex.lost) * kLn2);
   const float g = dloss[n] * a.tau;
   const Share share(ex, log2_s, g);
   put([&](float z) { return share.at(z); });
-  __syncthreads();
-  subtract_entries<THREADS>(a, en, total, g, 0, a.V, out, share);
+  subtract_entries<WAVES>(a, en, cut, total, g, 0, a.V, out, share);
 }
 
 // ---- a row in chunks: two passes over the logits ----
@@ -358,9 +399,16 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
   int64_t lo = 0, hi = a.V;
   if (GRAD) chunk_of(a, row, blockIdx.x, &lo, &hi);
   // (only columns of this chunk are read from the row: others may be overwritten by their own chunk's workgroup by now)
-  const float tm = load_entries<kThreads>(a, n, en, [&](int j, int64_t v) {
-    return FROM_PARTS ? picked[n * a.K + j] : v >= lo && v < hi ? elem_to_float<T>(row[v]) : 0.0f;
-  });
+  float tm = minus_inf();
+  for (int j = t; j < a.K; j += kThreads) {
+    int64_t v;
+    float x;
+    load_entry(a, n, j, &v, &x);
+    en.at[j] = (int32_t)v;
+    en.share[j] = x;
+    en.z[j] = FROM_PARTS ? picked[n * a.K + j] : v >= lo && v < hi ? elem_to_float<T>(row[v]) : 0.0f;
+    tm = fmaxf(tm, x);
+  }
   float m, log_s;
   if constexpr (FROM_PARTS) {
     float pm = minus_inf();
@@ -381,12 +429,10 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
   }
   const float top = group_max<kWaves>(tm, red[2]);
   const bool none = top == minus_inf();
-  float e_sum, cross;
-  weigh_entries<kThreads>(a, en, top, m, &e_sum, &cross);
-  const float total = group_sum<kWaves>(e_sum, red[3]);
+  const float total = group_sum<kWaves>(weigh_entries<kThreads>(a, en, top), red[3]);
   if constexpr (FROM_PARTS) {
     if (blockIdx.x == 0) {
-      const float x = group_sum<kWaves>(cross, red[4]);
+      const float x = group_sum<kWaves>(cross_entries<kThreads>(a, en, m), red[4]);
       if (t == 0) {
         loss[n] = none ? 0.0f : loss_of(a, x, total, log_s);
         if (stats != nullptr) stats[n] = float2{m, log_s};
@@ -428,9 +474,10 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
       run([](float) { return 0.0f; });
       return;
     }
+    merge_entries<kThreads>(a, en);
     run([&](float z) { return share.at(z); });
-    __syncthreads();                           // the chunk is written; now the entries' columns again, with the teacher's shares
-    subtract_entries<kThreads>(a, en, total, g, lo, hi, out, share);
+    __syncthreads();
+    subtract_entries<kWaves>(a, en, cut, total, g, lo, hi, out, share);
   }
 }
 
