@@ -10,6 +10,8 @@
 // Bound by memory: N * V logits in, as many gradients out.  A row is cut into chunks where there are few rows, so that every
 // compute unit has some (row_chunks): the first kernel leaves every chunk's (maximum, sum), the second joins those of its row and
 // writes its chunk of the gradient.
+#include <type_traits>
+
 #include "buffer_access.h"
 #include "token_step.h"
 
@@ -211,7 +213,7 @@ __device__ __forceinline__ float loss_of(const Distill &a, float cross, float to
   return a.tau * a.tau * (cross / (a.tau * total) - logf(total) + log_s);
 }
 
-// Cache policy of buffer accesses: non-temporal, for what is not read again soon.
+// Cache policy of buffer accesses: non-temporal.
 constexpr int kStream = 2;
 
 // ---- a row in registers: loss and gradient in one pass ----
@@ -238,6 +240,7 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   int64_t v0 = -1;
   float x0 = minus_inf();
   if (t < a.K) load_entry(a, n, t, &v0, &x0);
+  const int first = __builtin_amdgcn_readfirstlane(t & ~63);          // vectors from here on belong to this wave
   Words4 x[R_];
 #pragma unroll
   for (int r = 0; r < R_; ++r) x[r] = buffer_load<16>(body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u);
@@ -261,6 +264,7 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   for (int r = 0; r < R_; ++r) {
     // (Here and below: one vector after the other, unpacked anew in each pass.  Left to itself the compiler works on all of them
     // at a time and keeps every element as binary32 from one pass to the next, several times the registers.)
+    if (first + r * THREADS >= vecs) continue;
     asm volatile("" : "+v"(x[r]));
     if ((r + 1) * THREADS > vecs) {
 #pragma unroll
@@ -274,27 +278,29 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   T *out = dlogits + n * ldd;
   const __amdgpu_buffer_rsrc_t out_body = make_rsrc(out + cut.head, (uint32_t)vecs * 16u);
   const Exponent ex(m, a.c);
-  auto put = [&](auto f) {
+  auto put = [&](auto policy, auto f) {
 #pragma unroll
     for (int r = 0; r < R_; ++r) {
+      if (first + r * THREADS >= vecs) continue;
       asm volatile("" : "+v"(x[r]));
       float v[VE];
 #pragma unroll
       for (int q = 0; q < VE; ++q) v[q] = f(R::elem(x[r], q));
       const Words4 w = pack_row<T, VE>(v);
-      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, kStream);
+      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, policy.value);
       else if (r * THREADS + t < vecs) R::store(out + cut.head + (int64_t)(r * THREADS + t) * VE, w);
     }
     if (one) out[single] = from_float<T>(f(zs));
   };
   if (none) {
     if (t == 0) loss[n] = 0.0f;
-    put([](float) { return 0.0f; });
+    put(std::integral_constant<int, kStream>(), [](float) { return 0.0f; });
     return;
   }
   float acc[4] = {exp2_of(ex.at(zs)), 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int r = 0; r < R_; ++r) {
+    if (first + r * THREADS >= vecs) continue;
     asm volatile("" : "+v"(x[r]));
 #pragma unroll
     for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(x[r], q)));
@@ -306,7 +312,12 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   if (t == 0) loss[n] = loss_of(a, cross, total, (log2_s - ex.lost) * kLn2);
   const float g = dloss[n] * a.tau;
   const Share share(ex, log2_s, g);
-  put([&](float z) { return share.at(z); });
+  // Stores leave the caches to others ([2048 x 131072] bf16 225 us, 231 with plain ones, [8192 x 16384] 106 and 112, [1000 x 90000]
+  // f32 147 and 158) unless many of their lines are written once more for an entry, one in 64 vectors ([4096 x 32768] with 200
+  // entries 140 and 131), or in the middle of the sizes, where plain ones are as fast or faster ([8192 x 50000] 323 and 311, [4096 x
+  // 32768] f32 196 and 198).
+  if (a.K * 64 <= vecs && THREADS * R_ != 8192) put(std::integral_constant<int, kStream>(), [&](float z) { return share.at(z); });
+  else put(std::integral_constant<int, 0>(), [&](float z) { return share.at(z); });
   subtract_entries<WAVES>(a, en, cut, total, g, 0, a.V, out, share);
 }
 
@@ -537,12 +548,13 @@ int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats
   if constexpr (GRAD) {
     const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
     if (vecs >= 2 && (a.chunks == 1 || a.N >= kEnoughRows)) {
-      if (vecs <= 256) return run_rows<T, 64, 4>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 1024) return run_rows<T, 256, 4>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 512) return run_rows<T, 64, 8>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 1024) return run_rows<T, 128, 8>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 2048) return run_rows<T, 256, 8>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 4096) return run_rows<T, 512, 8>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 8192) return run_rows<T, 1024, 8>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 16384) return run_rows<T, 1024, 16>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 24576) return run_rows<T, 1024, 24>(a, dloss, loss, dlogits, ldd, s);
     }
   }
   float2 *parts = static_cast<float2 *>(ws);
