@@ -220,14 +220,17 @@ constexpr int kStream = 2;
 
 // One workgroup per row, whose lanes keep R vectors each: the logits are read once.  alike: the rows of dlogits start as far from a
 // 16-byte boundary as those of the logits.  The row has a whole vector at least.
-template <typename T, int THREADS, int R_>
-__global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(Distill a, const float *__restrict__ dloss, float *__restrict__ loss,
-                                                              T *dlogits, int64_t ldd, bool alike) {
+// The longest rows keep L more vectors per lane in shared memory, which they reach without passing through registers.
+template <typename T, int THREADS, int R_, int L>
+__global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(Distill a, const float *__restrict__ dloss,
+                                                                               float *__restrict__ loss, T *dlogits, int64_t ldd,
+                                                                               bool alike) {
   constexpr int VE = 16 / (int)sizeof(T), WAVES = THREADS / 64;
   constexpr uint32_t kNothing = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;       // -inf, for vectors behind the row
   typedef RowVec<T, VE> R;
   extern __shared__ uint32_t lds[];
   __shared__ float red[5][WAVES];
+  __shared__ Words4 rest[L > 0 ? L * THREADS : 1];
   const Entries en(lds, a.K);
   const int t = threadIdx.x;
   const int64_t n = blockIdx.x;
@@ -259,6 +262,22 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   const bool none = top == minus_inf();
   const float total = group_sum<WAVES>(weigh_entries<THREADS>(a, en, top), red[1]);
   merge_entries<THREADS>(a, en);
+  // (The copies to LDS are issued after what the entries need of it: the compiler lets reads of LDS wait for them.)
+  if constexpr (L > 0) {
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      if (first + (R_ + l) * THREADS >= vecs) continue;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(body, (__attribute__((address_space(3))) void *)&rest[l * THREADS + first], 16,
+                                               (uint32_t)t * 16u, (uint32_t)((R_ + l) * THREADS) * 16u, 0, 0);
+    }
+  }
+  // vector R_ + l of the lane, -inf behind the row
+  auto from_lds = [&](int l) {
+    Words4 w = rest[l * THREADS + t];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (R_ + l) * THREADS + t < vecs ? w[i] : kNothing;
+    return w;
+  };
   float m = zs;
 #pragma unroll
   for (int r = 0; r < R_; ++r) {
@@ -274,21 +293,36 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(x[r], q));
     asm volatile("" : "+v"(m));
   }
+  if constexpr (L > 0) {
+#pragma unroll 1
+    for (int l = 0; l < L && first + (R_ + l) * THREADS < vecs; ++l) {
+      const Words4 w = from_lds(l);
+#pragma unroll
+      for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(w, q));
+    }
+  }
   m = group_max<WAVES>(m, red[2]);
   T *out = dlogits + n * ldd;
   const __amdgpu_buffer_rsrc_t out_body = make_rsrc(out + cut.head, (uint32_t)vecs * 16u);
   const Exponent ex(m, a.c);
   auto put = [&](auto policy, auto f) {
+    auto put_vector = [&](int r, const Words4 &z) {
+      float v[VE];
+#pragma unroll
+      for (int q = 0; q < VE; ++q) v[q] = f(R::elem(z, q));
+      const Words4 w = pack_row<T, VE>(v);
+      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, policy.value);
+      else if (r * THREADS + t < vecs) R::store(out + cut.head + (int64_t)(r * THREADS + t) * VE, w);
+    };
 #pragma unroll
     for (int r = 0; r < R_; ++r) {
       if (first + r * THREADS >= vecs) continue;
       asm volatile("" : "+v"(x[r]));
-      float v[VE];
-#pragma unroll
-      for (int q = 0; q < VE; ++q) v[q] = f(R::elem(x[r], q));
-      const Words4 w = pack_row<T, VE>(v);
-      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, policy.value);
-      else if (r * THREADS + t < vecs) R::store(out + cut.head + (int64_t)(r * THREADS + t) * VE, w);
+      put_vector(r, x[r]);
+    }
+    if constexpr (L > 0) {
+#pragma unroll 1
+      for (int l = 0; l < L && first + (R_ + l) * THREADS < vecs; ++l) put_vector(R_ + l, from_lds(l));
     }
     if (one) out[single] = from_float<T>(f(zs));
   };
@@ -305,6 +339,14 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
 #pragma unroll
     for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(x[r], q)));
     asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
+  }
+  if constexpr (L > 0) {
+#pragma unroll 1
+    for (int l = 0; l < L && first + (R_ + l) * THREADS < vecs; ++l) {
+      const Words4 w = from_lds(l);
+#pragma unroll
+      for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(w, q)));
+    }
   }
   const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m), red[3]);
   const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[4]);
@@ -518,7 +560,10 @@ size_t parts_bytes(int64_t N, int64_t V) {
   return align_up((size_t)N * chunks * sizeof(float2), 256);
 }
 
-constexpr int64_t kEnoughRows = 128;
+// Rows from which long ones (more than 8192 vectors) have a workgroup each although they may be fewer than the compute units, against
+// two passes over chunks ([100 x 262144] bf16 36.9 and 37.4 us, [64 x 262144] 34.6 and 23.0, [100 x 131072] 22.5 and 21.6, [32 x
+// 131072] 19.7 and 14.4).  Up to 8192 vectors a single row is as fast so ([1 x 50000] 12.0 and 12.6, [8 x 20000] 9.8 and 12.5).
+constexpr int64_t kEnoughRows = 96;
 
 // Rows per launch: the grid's second dimension ends at 65535.
 constexpr int64_t kRowsPerLaunch = 65535;
@@ -533,10 +578,10 @@ Distill rows_from(const Distill &a, int64_t n, int dtype) {
 }
 
 // One workgroup per row, at most.
-template <typename T, int THREADS, int R>
+template <typename T, int THREADS, int R, int L = 0>
 int run_rows(const Distill &a, const float *dloss, float *loss, void *dlogits, int64_t ldd, hipStream_t s) {
   const bool alike = ((uintptr_t)dlogits - (uintptr_t)a.logits) % 16 == 0 && (ldd - a.ldz) * (int64_t)sizeof(T) % 16 == 0;
-  hipLaunchKernelGGL((distill_row_kernel<T, THREADS, R>), dim3((unsigned)a.N), dim3(THREADS), entries_bytes(a.K), s, a, dloss, loss,
+  hipLaunchKernelGGL((distill_row_kernel<T, THREADS, R, L>), dim3((unsigned)a.N), dim3(THREADS), entries_bytes(a.K), s, a, dloss, loss,
                      static_cast<T *>(dlogits), ldd, alike);
   return check_launch();
 }
@@ -547,7 +592,7 @@ int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats
   const Distill a = describe(d);
   if constexpr (GRAD) {
     const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
-    if (vecs >= 2 && (a.chunks == 1 || a.N >= kEnoughRows)) {
+    if (vecs >= 2 && (vecs <= 8192 || a.N >= kEnoughRows)) {
       if (vecs <= 512) return run_rows<T, 64, 8>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 1024) return run_rows<T, 128, 8>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 2048) return run_rows<T, 256, 8>(a, dloss, loss, dlogits, ldd, s);
@@ -555,6 +600,7 @@ int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats
       if (vecs <= 8192) return run_rows<T, 1024, 8>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 16384) return run_rows<T, 1024, 16>(a, dloss, loss, dlogits, ldd, s);
       if (vecs <= 24576) return run_rows<T, 1024, 24>(a, dloss, loss, dlogits, ldd, s);
+      if (vecs <= 32768) return run_rows<T, 1024, 24, 8>(a, dloss, loss, dlogits, ldd, s);
     }
   }
   float2 *parts = static_cast<float2 *>(ws);

@@ -344,6 +344,34 @@ def test_distill(dtype, tdtype, index, N, V, K):
         assert torch.equal(got4, got2) and torch.equal(loss4, loss2) and around_is_untouched(fresh, pad, offset, 7.0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vecs", [1, 2, 511, 512, 513, 1024, 1025, 2048, 2049, 4096, 4097, 8192, 8193, 16384, 16385, 24576, 24577, 32767,
+                                  32768, 32769])
+def test_distill_at_the_edges_of_row_lengths(dtype, vecs):
+    """Rows of so many 16-byte vectors and a few columns more or less, enough rows for a workgroup each, at any alignment."""
+    per = 128 // torch.finfo(DT[dtype]).bits
+    N, K = 130, 7
+    for V, pad, offset in ((vecs * per, 0, 0), (vecs * per + per - 1, 1, 3)):
+        z, ids, t, dloss = student(N, V, K, V, dtype, "f32")
+        ids[7] = V - 1                                                          # the last column, by every entry
+        part = torch.tensor([0, 1, 2, 3, 4, 7, 64, N - 1])
+        zd = strided(z, pad, offset)
+        loss, grad = B.bsr_distill_loss_grad(zd, ids.cuda(), t.cuda(), dloss.cuda(), 0.9)
+        want, _, g, el, eg = P.distill(f64(z[part]), ids[part].numpy(), f64(t[part]), float(np.float32(0.9)), f64(dloss[part]))
+        check(loss[part], want, el)
+        check(grad[part], g, eg, dtype)
+        one, stats = B.bsr_distill_loss(zd, ids.cuda(), t.cuda(), 0.9)
+        other = B.bsr_distill_grad(zd, ids.cuda(), t.cuda(), stats, dloss.cuda(), 0.9)
+        check(one[part], want, el)
+        check(other[part], g, eg, dtype)
+        # every row, against the other way round (two roundings of either)
+        close = (grad.float() - other.float()).abs() <= 2.0 ** -7 * other.float().abs() + 1e-6
+        assert bool(close.all())
+        fresh = strided(z, pad, offset, fill=7.0)
+        loss2, grad2 = B.bsr_distill_loss_grad(fresh, ids.cuda(), t.cuda(), dloss.cuda(), 0.9, dlogits=fresh)
+        assert torch.equal(loss2, loss) and torch.equal(grad2, grad) and around_is_untouched(fresh, pad, offset, 7.0)
+
+
 def test_distill_of_more_rows_than_a_grid_dimension():
     N, V, K = 70001, 40, 3
     z, ids, t, dloss = student(N, V, K, 1)
