@@ -10,8 +10,6 @@
 // Bound by memory: N * V logits in, as many gradients out.  A row is cut into chunks where there are few rows, so that every
 // compute unit has some (row_chunks): the first kernel leaves every chunk's (maximum, sum), the second joins those of its row and
 // writes its chunk of the gradient.
-#include <type_traits>
-
 #include "buffer_access.h"
 #include "token_step.h"
 
@@ -37,9 +35,6 @@ struct Distill {
   int chunks;
 };
 
-__device__ __forceinline__ float teacher_logit(const Distill &a, int64_t i) {
-  return a.teacher_bf16 ? bf16_bits_to_float(static_cast<const uint16_t *>(a.teacher)[i]) : static_cast<const float *>(a.teacher)[i];
-}
 // column of an entry, or -1
 __device__ __forceinline__ int64_t entry_column(const Distill &a, int64_t i) {
   const int64_t v = a.ids64 ? load_index<int64_t>(a.ids, i) : load_index<int32_t>(a.ids, i);
@@ -135,6 +130,15 @@ struct Cut {
   __device__ __forceinline__ int64_t single(int64_t lo, int64_t i) const { return lo + (i < head ? i : i + vecs * VE); }
 };
 
+// Columns of chunk i: boundaries are multiples of a.chunk behind the row's first 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ void chunk_of(const Distill &a, const T *row, int64_t i, int64_t *lo, int64_t *hi) {
+  const int64_t head = (int64_t)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T);
+  const int64_t l = i == 0 ? 0 : i * a.chunk + head, h = (i + 1) * a.chunk + head;
+  *hi = i == a.chunks - 1 || h > a.V ? a.V : h;
+  *lo = l < *hi ? l : *hi;
+}
+
 // A row's entries in shared memory.
 struct Entries {
   int32_t *at;                                 // columns, -1: no entry
@@ -147,11 +151,32 @@ struct Entries {
 };
 size_t entries_bytes(int64_t K) { return (size_t)K * 4 * sizeof(float); }
 
-// Entry j of row n: its column (-1: none) and the teacher's logit (-inf: none).
-__device__ __forceinline__ void load_entry(const Distill &a, int64_t n, int j, int64_t *v, float *x) {
-  *v = entry_column(a, n * a.K + j);
-  *x = *v >= 0 ? teacher_logit(a, n * a.K + j) : minus_inf();
-}
+// The first use of a loaded value: keeps the compiler from moving that, and the wait for the load, up to the load.
+template <typename V>
+__device__ __forceinline__ void used_here(V &v) { asm volatile("" : "+v"(v)); }
+
+// Entry j of row n as it comes from memory (nothing waits for it here), and its column (-1: none) and the teacher's logit (-inf: none).
+struct RawEntry {
+  uint32_t id[2];                              // low and high word (of an int32: the same)
+  uint16_t logit[2];                           // ... half
+  __device__ __forceinline__ void load(const Distill &a, int64_t n, int j) {
+    const int64_t i = n * a.K + j;
+    const char *p = static_cast<const char *>(a.ids) + i * (a.ids64 ? 8 : 4), *x = static_cast<const char *>(a.teacher) + i * (a.teacher_bf16 ? 2 : 4);
+    id[0] = *reinterpret_cast<const uint32_t *>(p);
+    id[1] = *reinterpret_cast<const uint32_t *>(p + (a.ids64 ? 4 : 0));
+    logit[0] = *reinterpret_cast<const uint16_t *>(x);
+    logit[1] = *reinterpret_cast<const uint16_t *>(x + (a.teacher_bf16 ? 0 : 2));
+  }
+  __device__ __forceinline__ void take(const Distill &a, int64_t *v, float *x) {
+    used_here(id[0]);
+    used_here(id[1]);
+    used_here(logit[0]);
+    used_here(logit[1]);
+    const int64_t c = a.ids64 ? (int64_t)((uint64_t)id[1] << 32 | id[0]) : (int64_t)(int32_t)id[0];
+    *v = c >= 0 && c < a.V ? c : -1;
+    *x = *v < 0 ? minus_inf() : __uint_as_float((uint32_t)logit[1] << 16 | (a.teacher_bf16 ? 0u : (uint32_t)logit[0]));
+  }
+};
 
 // e_j in place of the teacher's logits; returns the lane's sum.  top: their maximum.
 template <int THREADS>
@@ -176,24 +201,25 @@ __device__ __forceinline__ float cross_entries(const Distill &a, const Entries &
   return sum;
 }
 
-// e_j of all entries of a column together, for every one of them; once all e_j are there.
+// e_j of all entries of a column in [lo, hi) together, for every one of them; once all e_j are there.
 template <int THREADS>
-__device__ __forceinline__ void merge_entries(const Distill &a, const Entries &en) {
+__device__ __forceinline__ void merge_entries(const Distill &a, const Entries &en, int64_t lo, int64_t hi) {
   for (int j = threadIdx.x; j < a.K; j += THREADS) {
     const int32_t v = en.at[j];
+    if (v < lo || v >= hi) continue;
     float q = 0.0f;
-#pragma unroll 8
+#pragma unroll 4
     for (int k = 0; k < a.K; ++k) q += en.at[k] == v ? en.share[k] : 0.0f;
     en.q[j] = q;
   }
 }
 
 // Teacher's shares subtracted from the gradient at the entries' columns in [lo, hi): every wave writes those columns once more
-// whose vectors it has written itself (vector i of the cut by wave i / 64 mod WAVES, single columns by the first), so that no wave
-// waits for another.  (A column that several entries share gets all of them, from every one of its entries alike.)
+// whose vectors it has written itself (vector i of the cut by wave i / (64 * each) mod WAVES, single columns by the first), so that no
+// wave waits for another.  (A column that several entries share gets all of them, from every one of its entries alike.)
 template <int WAVES, typename T>
-__device__ __forceinline__ void subtract_entries(const Distill &a, const Entries &en, const Cut &cut, float total, float g, int64_t lo,
-                                                 int64_t hi, T *out, const Share &share) {
+__device__ __forceinline__ void subtract_entries(const Distill &a, const Entries &en, const Cut &cut, int each, float total, float g,
+                                                 int64_t lo, int64_t hi, T *out, const Share &share) {
   constexpr int VE = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float by = 1.0f / total;
@@ -204,7 +230,7 @@ __device__ __forceinline__ void subtract_entries(const Distill &a, const Entries
     if (v < lo || v >= hi) continue;
     const uint32_t i = (uint32_t)(v - lo - cut.head);
     const bool single = v - lo < cut.head || i >= (uint32_t)(cut.vecs * VE);
-    if ((single ? 0u : i / (VE * 64u) % WAVES) != (uint32_t)wave) continue;
+    if ((single ? 0u : i / (VE * 64u * (uint32_t)each) % WAVES) != (uint32_t)wave) continue;
     out[v] = from_float<T>(share.at(en.z[j]) - g * (en.q[j] * by));
   }
 }
@@ -216,163 +242,203 @@ __device__ __forceinline__ float loss_of(const Distill &a, float cross, float to
 // Cache policy of buffer accesses: non-temporal.
 constexpr int kStream = 2;
 
-// ---- a row in registers: loss and gradient in one pass ----
+// ---- a row in registers: one pass over the logits ----
 
-// One workgroup per row, whose lanes keep R vectors each: the logits are read once.  alike: the rows of dlogits start as far from a
-// 16-byte boundary as those of the logits.  The row has a whole vector at least.
+// 16 bytes per lane from a buffer to LDS, to `to` + 16 bytes times the lane's number.  Whoever reads them has to wait for vmcnt first.
+__device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, Words4 *to, uint32_t offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, offset, 0, 0, 0);
+}
+
+// What a call computes.
+constexpr int kLoss = 1, kGrad = 2;
+
+// One workgroup per row, whose lanes keep R vectors each: the logits are read once, all of them on their way at the same time.
+// MODE: kLoss (loss and statistics), kGrad (the gradient from given statistics; a workgroup per chunk of a row), or both.
 // The longest rows keep L more vectors per lane in shared memory, which they reach without passing through registers.
-template <typename T, int THREADS, int R_, int L>
+template <typename T, int THREADS, int R_, int L, int MODE>
 __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(Distill a, const float *__restrict__ dloss,
-                                                                               float *__restrict__ loss, T *dlogits, int64_t ldd,
-                                                                               bool alike) {
+                                                                               float *__restrict__ loss, float2 *stats, T *dlogits,
+                                                                               int64_t ldd) {
+  static_assert(L == 0 || MODE == (kLoss | kGrad), "the copies to LDS are waited for where the maximum is taken");
   constexpr int VE = 16 / (int)sizeof(T), WAVES = THREADS / 64;
   constexpr uint32_t kNothing = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;       // -inf, for vectors behind the row
+  // Stores of the longest rows, which have a compute unit to themselves, leave the caches to others ([2048 x 131072] bf16 227 us,
+  // 238 with plain ones, [1000 x 180000] 171 and 180; but [8192 x 50000] 329 and 312, [16384 x 4096] 64 and 51).
+  constexpr int kPolicy = R_ >= 16 ? kStream : 0;
   typedef RowVec<T, VE> R;
   extern __shared__ uint32_t lds[];
   __shared__ float red[5][WAVES];
   __shared__ Words4 rest[L > 0 ? L * THREADS : 1];
   const Entries en(lds, a.K);
   const int t = threadIdx.x;
-  const int64_t n = blockIdx.x;
+  const int64_t n = MODE == kGrad ? blockIdx.x / a.chunks : blockIdx.x;
   const T *row = static_cast<const T *>(a.logits) + n * a.ldz;
-  const Cut cut(row, 0, a.V);
-  // The entries are on their way before the row, and what they need of each other is computed while the row is still coming.
-  // the whole vectors as a buffer: accesses behind them are neither loads nor stores
+  int64_t lo = 0, hi = a.V;
+  if constexpr (MODE == kGrad) chunk_of(a, row, blockIdx.x - n * a.chunks, &lo, &hi);
+  const Cut cut(row, lo, hi);
   const int vecs = (int)cut.vecs;
-  const __amdgpu_buffer_rsrc_t body = make_rsrc(row + cut.head, (uint32_t)vecs * 16u);
-  int64_t v0 = -1;
-  float x0 = minus_inf();
-  if (t < a.K) load_entry(a, n, t, &v0, &x0);
-  const int first = __builtin_amdgcn_readfirstlane(t & ~63);          // vectors from here on belong to this wave
+  // The entries are on their way before the row, and what they need of each other is computed while the row is still coming.
+  // (No load here is under a lane's condition, and no value has a default: the compiler would wait for the load at once.)
+  RawEntry entry;
+  if (a.K > 0) entry.load(a, n, t < a.K ? t : 0);
+  const bool one = t < cut.singles;
+  const int64_t single = one ? cut.single<VE>(lo, t) : lo;
+  T raw_single, raw_z;
+  if (hi > lo) raw_single = row[single];
+  // Every wave has `each` times 64 consecutive vectors, four of these a buffer of their own: accesses beyond are neither loads nor
+  // stores.  (What the range check goes by is the offset in the lane's register and that in the 12 bits of the instruction; vectors
+  // THREADS apart in one buffer would take a register each.)
+  const int lane = t & 63, each = (vecs + THREADS - 1) / THREADS, first = __builtin_amdgcn_readfirstlane(t >> 6) * each * 64;
+  const int left = vecs - first < 0 ? 0 : vecs - first < each * 64 ? vecs - first : each * 64;
+  auto buffer = [&](const T *p, int r) {
+    const int skip = r / 4 * 256, rest = left - skip;
+    return make_rsrc(p + lo + cut.head + (int64_t)(first + skip) * VE, rest > 0 ? (uint32_t)rest * 16u : 0u);
+  };
+  auto offset = [&](int r) { return (uint32_t)lane * 16u + r % 4 * 1024u; };
   Words4 x[R_];
 #pragma unroll
-  for (int r = 0; r < R_; ++r) x[r] = buffer_load<16>(body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u);
-  const bool one = t < cut.singles;
-  const int64_t single = cut.single<VE>(0, one ? t : 0);
-  const float zs = one ? elem_to_float<T>(row[single]) : minus_inf();
-  float tm = x0;
-  for (int j = t; j < a.K; j += THREADS) {
-    if (j >= THREADS) load_entry(a, n, j, &v0, &x0);
-    en.at[j] = (int32_t)v0;
-    en.share[j] = x0;
-    en.z[j] = v0 >= 0 ? elem_to_float<T>(row[v0]) : 0.0f;
-    tm = fmaxf(tm, x0);
+  for (int r = 0; r < R_; ++r) x[r] = buffer_load<16>(buffer(row, r), offset(r));
+  // (Loads return in order: what is used before the row is here has to be issued before it, and the logits at the entries, which are
+  // not, are put away with the row's.  Only columns of this workgroup are read from the row: others may be overwritten by now.)
+  float tm = minus_inf();
+  auto put_entry = [&](int j) {                // returns where the entry's logit is read, at the first column where it is not needed
+    int64_t v;
+    float x;
+    entry.take(a, &v, &x);
+    en.at[j] = (int32_t)v;
+    en.share[j] = x;
+    tm = fmaxf(tm, x);
+    return v >= lo && v < hi ? v : lo;
+  };
+  int64_t z_at = lo;
+  if (t < a.K) z_at = put_entry(t);
+  if (hi > lo) raw_z = row[z_at];
+  for (int j = t + THREADS; j < a.K; j += THREADS) {
+    entry.load(a, n, j);
+    const int64_t v = put_entry(j);
+    if (hi > lo) en.z[j] = elem_to_float<T>(row[v]);
   }
   const float top = group_max<WAVES>(tm, red[0]);
   const bool none = top == minus_inf();
   const float total = group_sum<WAVES>(weigh_entries<THREADS>(a, en, top), red[1]);
-  merge_entries<THREADS>(a, en);
-  // (The copies to LDS are issued after what the entries need of it: the compiler lets reads of LDS wait for them.)
+  if constexpr (MODE & kGrad) merge_entries<THREADS>(a, en, lo, hi);
   if constexpr (L > 0) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
-      if (first + (R_ + l) * THREADS >= vecs) continue;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(body, (__attribute__((address_space(3))) void *)&rest[l * THREADS + first], 16,
-                                               (uint32_t)t * 16u, (uint32_t)((R_ + l) * THREADS) * 16u, 0, 0);
+      if ((R_ + l) * 64 >= left) continue;
+      copy_to_lds(buffer(row, R_ + l), &rest[l * THREADS + (t - lane)], offset(R_ + l));
     }
   }
   // vector R_ + l of the lane, -inf behind the row
   auto from_lds = [&](int l) {
     Words4 w = rest[l * THREADS + t];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (R_ + l) * THREADS + t < vecs ? w[i] : kNothing;
+    for (int i = 0; i < 4; ++i) w[i] = (R_ + l) * 64 + lane < left ? w[i] : kNothing;
     return w;
   };
+  used_here(raw_single);
+  const float zs = one ? elem_to_float<T>(raw_single) : minus_inf();
   float m = zs;
+  if constexpr (MODE == kGrad) {
+    m = stats[n].x;
+    used_here(raw_z);
+    if (t < a.K) en.z[t] = elem_to_float<T>(raw_z);
+    __syncthreads();
+  } else {
 #pragma unroll
-  for (int r = 0; r < R_; ++r) {
-    // (Here and below: one vector after the other, unpacked anew in each pass.  Left to itself the compiler works on all of them
-    // at a time and keeps every element as binary32 from one pass to the next, several times the registers.)
-    if (first + r * THREADS >= vecs) continue;
-    asm volatile("" : "+v"(x[r]));
-    if ((r + 1) * THREADS > vecs) {
+    for (int r = 0; r < R_; ++r) {
+      // (Here and below: one vector after the other, unpacked anew in each pass.  Left to itself the compiler works on all of them
+      // at a time and keeps every element as binary32 from one pass to the next, several times the registers.)
+      if (r * 64 >= left) continue;
+      asm volatile("" : "+v"(x[r]));
+      if (r * 64 + 64 > left) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[r][i] = r * THREADS + t < vecs ? x[r][i] : kNothing;
+        for (int i = 0; i < 4; ++i) x[r][i] = r * 64 + lane < left ? x[r][i] : kNothing;
+      }
+#pragma unroll
+      for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(x[r], q));
+      asm volatile("" : "+v"(m));
     }
-#pragma unroll
-    for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(x[r], q));
-    asm volatile("" : "+v"(m));
-  }
-  if constexpr (L > 0) {
+    if constexpr (L > 0) {
+      // the copies have to be there: the compiler does not know that what is read here is what they write
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll 1
-    for (int l = 0; l < L && first + (R_ + l) * THREADS < vecs; ++l) {
-      const Words4 w = from_lds(l);
+      for (int l = 0; l < L && (R_ + l) * 64 < left; ++l) {
+        const Words4 w = from_lds(l);
 #pragma unroll
-      for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(w, q));
+        for (int q = 0; q < VE; ++q) m = fmaxf(m, R::elem(w, q));
+      }
     }
+    used_here(raw_z);
+    if (t < a.K) en.z[t] = elem_to_float<T>(raw_z);
+    m = group_max<WAVES>(m, red[2]);
   }
-  m = group_max<WAVES>(m, red[2]);
   T *out = dlogits + n * ldd;
-  const __amdgpu_buffer_rsrc_t out_body = make_rsrc(out + cut.head, (uint32_t)vecs * 16u);
   const Exponent ex(m, a.c);
-  auto put = [&](auto policy, auto f) {
+  auto put = [&](auto f) {
     auto put_vector = [&](int r, const Words4 &z) {
       float v[VE];
 #pragma unroll
       for (int q = 0; q < VE; ++q) v[q] = f(R::elem(z, q));
       const Words4 w = pack_row<T, VE>(v);
-      if (alike) __builtin_amdgcn_raw_buffer_store_b128(w, out_body, (uint32_t)t * 16u, (uint32_t)(r * THREADS) * 16u, policy.value);
-      else if (r * THREADS + t < vecs) R::store(out + cut.head + (int64_t)(r * THREADS + t) * VE, w);
+      __builtin_amdgcn_raw_buffer_store_b128(w, buffer(out, r), offset(r), 0, kPolicy);
     };
 #pragma unroll
     for (int r = 0; r < R_; ++r) {
-      if (first + r * THREADS >= vecs) continue;
+      if (r * 64 >= left) continue;
       asm volatile("" : "+v"(x[r]));
       put_vector(r, x[r]);
     }
     if constexpr (L > 0) {
 #pragma unroll 1
-      for (int l = 0; l < L && first + (R_ + l) * THREADS < vecs; ++l) put_vector(R_ + l, from_lds(l));
+      for (int l = 0; l < L && (R_ + l) * 64 < left; ++l) put_vector(R_ + l, from_lds(l));
     }
     if (one) out[single] = from_float<T>(f(zs));
   };
-  if (none) {
-    if (t == 0) loss[n] = 0.0f;
-    put(std::integral_constant<int, kStream>(), [](float) { return 0.0f; });
+  if (none && (MODE & kGrad)) {
+    if (t == 0 && (MODE & kLoss)) loss[n] = 0.0f;
+    put([](float) { return 0.0f; });
     return;
   }
-  float acc[4] = {exp2_of(ex.at(zs)), 0.0f, 0.0f, 0.0f};
+  float log2_s;                                // of the sum of 2^(the exponents)
+  if constexpr (MODE == kGrad) {
+    log2_s = fmaf(stats[n].y, kLog2E, ex.lost);
+  } else {
+    float acc[4] = {exp2_of(ex.at(zs)), 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int r = 0; r < R_; ++r) {
-    if (first + r * THREADS >= vecs) continue;
-    asm volatile("" : "+v"(x[r]));
+    for (int r = 0; r < R_; ++r) {
+      if (r * 64 >= left) continue;
+      asm volatile("" : "+v"(x[r]));
 #pragma unroll
-    for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(x[r], q)));
-    asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
-  }
-  if constexpr (L > 0) {
+      for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(x[r], q)));
+      asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
+    }
+    if constexpr (L > 0) {
 #pragma unroll 1
-    for (int l = 0; l < L && first + (R_ + l) * THREADS < vecs; ++l) {
-      const Words4 w = from_lds(l);
+      for (int l = 0; l < L && (R_ + l) * 64 < left; ++l) {
+        const Words4 w = from_lds(l);
 #pragma unroll
-      for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(w, q)));
+        for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(w, q)));
+      }
+    }
+    const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m), red[3]);
+    const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[4]);
+    log2_s = m == minus_inf() ? __builtin_nanf("") : log2f(s);
+    if (t == 0) {
+      const float log_s = (log2_s - ex.lost) * kLn2;
+      loss[n] = none ? 0.0f : loss_of(a, cross, total, log_s);
+      if constexpr (MODE == kLoss) stats[n] = float2{m, log_s};
     }
   }
-  const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m), red[3]);
-  const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[4]);
-  const float log2_s = m == minus_inf() ? __builtin_nanf("") : log2f(s);
-  if (t == 0) loss[n] = loss_of(a, cross, total, (log2_s - ex.lost) * kLn2);
-  const float g = dloss[n] * a.tau;
-  const Share share(ex, log2_s, g);
-  // Stores leave the caches to others ([2048 x 131072] bf16 225 us, 231 with plain ones, [8192 x 16384] 106 and 112, [1000 x 90000]
-  // f32 147 and 158) unless many of their lines are written once more for an entry, one in 64 vectors ([4096 x 32768] with 200
-  // entries 140 and 131), or in the middle of the sizes, where plain ones are as fast or faster ([8192 x 50000] 323 and 311, [4096 x
-  // 32768] f32 196 and 198).
-  if (a.K * 64 <= vecs && THREADS * R_ != 8192) put(std::integral_constant<int, kStream>(), [&](float z) { return share.at(z); });
-  else put(std::integral_constant<int, 0>(), [&](float z) { return share.at(z); });
-  subtract_entries<WAVES>(a, en, cut, total, g, 0, a.V, out, share);
+  if constexpr (MODE & kGrad) {
+    const float g = dloss[n] * a.tau;
+    const Share share(ex, log2_s, g);
+    put([&](float z) { return share.at(z); });
+    subtract_entries<WAVES>(a, en, cut, each, total, g, lo, hi, out, share);
+  }
 }
 
 // ---- a row in chunks: two passes over the logits ----
-
-// Columns of chunk i: boundaries are multiples of a.chunk behind the row's first 16-byte boundary.
-template <typename T>
-__device__ __forceinline__ void chunk_of(const Distill &a, const T *row, int64_t i, int64_t *lo, int64_t *hi) {
-  const int64_t head = (int64_t)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T);
-  const int64_t l = i == 0 ? 0 : i * a.chunk + head, h = (i + 1) * a.chunk + head;
-  *hi = i == a.chunks - 1 || h > a.V ? a.V : h;
-  *lo = l < *hi ? l : *hi;
-}
 
 // parts[n][chunk] = (maximum, sum of exp((z - maximum) / tau)) of a chunk; the first chunk's workgroup also leaves the logits at
 // the row's entries in picked[n][j].
@@ -434,9 +500,8 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill a, floa
   if (t == 0) parts[n * a.chunks + blockIdx.x] = float2{top, sum};
 }
 
-// FROM_PARTS: statistics from the chunks' parts, and the loss (by the first chunk's workgroup); else statistics as given.
-// GRAD: the chunk's gradient.
-template <typename T, bool FROM_PARTS, bool GRAD>
+// Statistics from the chunks' parts; the loss, by the first chunk's workgroup; GRAD: the chunk's gradient.
+template <typename T, bool GRAD>
 __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, const float2 *__restrict__ parts, int parts_per_row,
                                                                   const float *__restrict__ picked,
                                                                   float *__restrict__ loss, float2 *stats,
@@ -451,45 +516,36 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
   const T *row = static_cast<const T *>(a.logits) + n * a.ldz;
   int64_t lo = 0, hi = a.V;
   if (GRAD) chunk_of(a, row, blockIdx.x, &lo, &hi);
-  // (only columns of this chunk are read from the row: others may be overwritten by their own chunk's workgroup by now)
   float tm = minus_inf();
   for (int j = t; j < a.K; j += kThreads) {
     int64_t v;
     float x;
-    load_entry(a, n, j, &v, &x);
+    RawEntry entry;
+    entry.load(a, n, j);
+    entry.take(a, &v, &x);
     en.at[j] = (int32_t)v;
     en.share[j] = x;
-    en.z[j] = FROM_PARTS ? picked[n * a.K + j] : v >= lo && v < hi ? elem_to_float<T>(row[v]) : 0.0f;
+    en.z[j] = picked[n * a.K + j];             // (the row's own may be overwritten by other chunks' workgroups by now)
     tm = fmaxf(tm, x);
   }
-  float m, log_s;
-  if constexpr (FROM_PARTS) {
-    float pm = minus_inf();
-    for (int i = t; i < parts_per_row; i += kThreads) pm = fmaxf(pm, parts[n * parts_per_row + i].x);
-    m = group_max<kWaves>(pm, red[0]);
-    const float base = base_of(m);
-    float ps = 0.0f;
-    for (int i = t; i < parts_per_row; i += kThreads) {
-      const float2 p = parts[n * parts_per_row + i];
-      ps += p.y * exp2_of((p.x - base) * a.c);
-    }
-    const float s = group_sum<kWaves>(ps, red[1]);
-    log_s = m == minus_inf() ? __builtin_nanf("") : logf(s);
-  } else {
-    const float2 st = stats[n];
-    m = st.x;
-    log_s = st.y;
+  float pm = minus_inf();
+  for (int i = t; i < parts_per_row; i += kThreads) pm = fmaxf(pm, parts[n * parts_per_row + i].x);
+  const float m = group_max<kWaves>(pm, red[0]), base = base_of(m);
+  float ps = 0.0f;
+  for (int i = t; i < parts_per_row; i += kThreads) {
+    const float2 p = parts[n * parts_per_row + i];
+    ps += p.y * exp2_of((p.x - base) * a.c);
   }
+  const float s = group_sum<kWaves>(ps, red[1]);
+  const float log_s = m == minus_inf() ? __builtin_nanf("") : logf(s);
   const float top = group_max<kWaves>(tm, red[2]);
   const bool none = top == minus_inf();
   const float total = group_sum<kWaves>(weigh_entries<kThreads>(a, en, top), red[3]);
-  if constexpr (FROM_PARTS) {
-    if (blockIdx.x == 0) {
-      const float x = group_sum<kWaves>(cross_entries<kThreads>(a, en, m), red[4]);
-      if (t == 0) {
-        loss[n] = none ? 0.0f : loss_of(a, x, total, log_s);
-        if (stats != nullptr) stats[n] = float2{m, log_s};
-      }
+  if (blockIdx.x == 0) {
+    const float x = group_sum<kWaves>(cross_entries<kThreads>(a, en, m), red[4]);
+    if (t == 0) {
+      loss[n] = none ? 0.0f : loss_of(a, x, total, log_s);
+      if (stats != nullptr) stats[n] = float2{m, log_s};
     }
   }
   if constexpr (GRAD) {
@@ -527,10 +583,10 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
       run([](float) { return 0.0f; });
       return;
     }
-    merge_entries<kThreads>(a, en);
+    merge_entries<kThreads>(a, en, lo, hi);
     run([&](float z) { return share.at(z); });
     __syncthreads();
-    subtract_entries<kWaves>(a, en, cut, total, g, lo, hi, out, share);
+    subtract_entries<kWaves>(a, en, cut, 1, total, g, lo, hi, out, share);
   }
 }
 
@@ -565,56 +621,70 @@ size_t parts_bytes(int64_t N, int64_t V) {
 // 131072] 19.7 and 14.4).  Up to 8192 vectors a single row is as fast so ([1 x 50000] 12.0 and 12.6, [8 x 20000] 9.8 and 12.5).
 constexpr int64_t kEnoughRows = 96;
 
-// Rows per launch: the grid's second dimension ends at 65535.
-constexpr int64_t kRowsPerLaunch = 65535;
+// Rows per launch of a two-dimensional grid, workgroups of a one-dimensional one: the second dimension ends at 65535, the first at
+// 2^32 lanes.
+constexpr int64_t kRowsPerLaunch = 65535, kWorkgroupsPerGrid = int64_t(1) << 21;
 
-Distill rows_from(const Distill &a, int64_t n, int dtype) {
+// The call's rows from n on, `most` at most.
+Distill rows_from(const Distill &a, int64_t n, int dtype, int64_t most) {
   Distill b = a;
   b.logits = static_cast<const char *>(a.logits) + n * a.ldz * elem_bytes(dtype);
   b.ids = static_cast<const char *>(a.ids) + n * a.K * (a.ids64 ? 8 : 4);
   b.teacher = static_cast<const char *>(a.teacher) + n * a.K * (a.teacher_bf16 ? 2 : 4);
-  b.N = a.N - n < kRowsPerLaunch ? a.N - n : kRowsPerLaunch;
+  b.N = a.N - n < most ? a.N - n : most;
   return b;
 }
 
-// One workgroup per row, at most.
-template <typename T, int THREADS, int R, int L = 0>
-int run_rows(const Distill &a, const float *dloss, float *loss, void *dlogits, int64_t ldd, hipStream_t s) {
-  const bool alike = ((uintptr_t)dlogits - (uintptr_t)a.logits) % 16 == 0 && (ldd - a.ldz) * (int64_t)sizeof(T) % 16 == 0;
-  hipLaunchKernelGGL((distill_row_kernel<T, THREADS, R, L>), dim3((unsigned)a.N), dim3(THREADS), entries_bytes(a.K), s, a, dloss, loss,
-                     static_cast<T *>(dlogits), ldd, alike);
-  return check_launch();
+template <typename T, int THREADS, int R, int L, int MODE>
+int run_rows(const Distill &whole, const float *dloss, float *loss, float2 *stats, void *dlogits, int64_t ldd, hipStream_t s) {
+  const int64_t chunk = (int64_t)THREADS * (R + L) * (16 / (int64_t)sizeof(T)), chunks = MODE == kGrad ? ceil_div(whole.V, chunk) : 1;
+  const int64_t most = chunks < kWorkgroupsPerGrid ? kWorkgroupsPerGrid / chunks : 1;
+  for (int64_t n = 0; n < whole.N; n += most) {
+    Distill a = rows_from(whole, n, sizeof(T) == 4 ? BSR_F32 : BSR_BF16, most);
+    a.chunk = chunk;
+    a.chunks = (int)chunks;
+    hipLaunchKernelGGL((distill_row_kernel<T, THREADS, R, L, MODE>), dim3((unsigned)(a.N * chunks)), dim3(THREADS),
+                       entries_bytes(a.K), s, a, dloss == nullptr ? dloss : dloss + n, loss == nullptr ? loss : loss + n,
+                       stats == nullptr ? stats : stats + n, dlogits == nullptr ? nullptr : static_cast<T *>(dlogits) + n * ldd, ldd);
+    const int rc = check_launch();
+    if (rc != BSR_OK) return rc;
+  }
+  return BSR_OK;
 }
 
 template <typename T, bool GRAD>
 int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats, void *dlogits, int64_t ldd, void *ws,
              hipStream_t s) {
   const Distill a = describe(d);
+  const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
+  constexpr int MODE = GRAD ? kLoss | kGrad : kLoss;
+  float2 *st = reinterpret_cast<float2 *>(stats);
+  if (vecs <= 8192) {
+    if (vecs <= 512) return run_rows<T, 64, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+    if (vecs <= 1024) return run_rows<T, 128, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+    if (vecs <= 2048) return run_rows<T, 256, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+    if (vecs <= 4096) return run_rows<T, 512, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+    return run_rows<T, 1024, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+  }
   if constexpr (GRAD) {
-    const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
-    if (vecs >= 2 && (vecs <= 8192 || a.N >= kEnoughRows)) {
-      if (vecs <= 512) return run_rows<T, 64, 8>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 1024) return run_rows<T, 128, 8>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 2048) return run_rows<T, 256, 8>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 4096) return run_rows<T, 512, 8>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 8192) return run_rows<T, 1024, 8>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 16384) return run_rows<T, 1024, 16>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 24576) return run_rows<T, 1024, 24>(a, dloss, loss, dlogits, ldd, s);
-      if (vecs <= 32768) return run_rows<T, 1024, 24, 8>(a, dloss, loss, dlogits, ldd, s);
+    if (a.N >= kEnoughRows && vecs <= 32768) {
+      if (vecs <= 16384) return run_rows<T, 1024, 16, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+      if (vecs <= 24576) return run_rows<T, 1024, 24, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+      return run_rows<T, 1024, 24, 8, MODE>(a, dloss, loss, st, dlogits, ldd, s);
     }
   }
   float2 *parts = static_cast<float2 *>(ws);
   float *picked = reinterpret_cast<float *>(static_cast<char *>(ws) + parts_bytes(d.N, d.V));
   for (int64_t n = 0; n < d.N; n += kRowsPerLaunch) {
-    const Distill b = rows_from(a, n, d.dtype);
+    const Distill b = rows_from(a, n, d.dtype, kRowsPerLaunch);
     hipLaunchKernelGGL((distill_parts_kernel<T>), dim3(a.chunks, (unsigned)b.N), dim3(kThreads), 0, s, b, parts + n * a.chunks,
                        picked + n * a.K);
     int rc = check_launch();
     if (rc != BSR_OK) return rc;
-    hipLaunchKernelGGL((distill_finish_kernel<T, true, GRAD>), dim3(GRAD ? a.chunks : 1, (unsigned)b.N), dim3(kThreads),
+    hipLaunchKernelGGL((distill_finish_kernel<T, GRAD>), dim3(GRAD ? a.chunks : 1, (unsigned)b.N), dim3(kThreads),
                        entries_bytes(a.K), s, b,
                        parts + n * a.chunks, a.chunks, picked + n * a.K, loss + n,
-                       stats != nullptr ? reinterpret_cast<float2 *>(stats) + n : nullptr, dloss + (dloss != nullptr ? n : 0),
+                       st != nullptr ? st + n : nullptr, dloss + (dloss != nullptr ? n : 0),
                        dlogits != nullptr ? static_cast<T *>(dlogits) + n * ldd : nullptr, ldd);
     rc = check_launch();
     if (rc != BSR_OK) return rc;
@@ -625,15 +695,11 @@ int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats
 template <typename T>
 int run_grad(const DistillArgs &d, const float *stats, const float *dloss, void *dlogits, int64_t ldd, hipStream_t s) {
   const Distill a = describe(d);
-  for (int64_t n = 0; n < d.N; n += kRowsPerLaunch) {
-    const Distill b = rows_from(a, n, d.dtype);
-    hipLaunchKernelGGL((distill_finish_kernel<T, false, true>), dim3(a.chunks, (unsigned)b.N), dim3(kThreads),
-                       entries_bytes(a.K), s, b, nullptr, 0, nullptr, nullptr, reinterpret_cast<float2 *>(const_cast<float *>(stats)) + n, dloss + n,
-                       static_cast<T *>(dlogits) + n * ldd, ldd);
-    const int rc = check_launch();
-    if (rc != BSR_OK) return rc;
-  }
-  return BSR_OK;
+  const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
+  float2 *st = reinterpret_cast<float2 *>(const_cast<float *>(stats));
+  if (vecs <= 512) return run_rows<T, 64, 8, 0, kGrad>(a, dloss, nullptr, st, dlogits, ldd, s);
+  if (vecs <= 1024) return run_rows<T, 128, 8, 0, kGrad>(a, dloss, nullptr, st, dlogits, ldd, s);
+  return run_rows<T, 256, 4, 0, kGrad>(a, dloss, nullptr, st, dlogits, ldd, s);
 }
 
 }  // namespace
