@@ -1,7 +1,7 @@
 // Gradient of the token table: dE[v] (+)= scale * sum of the rows of dY whose token is v, positions ascending.
 //
 // The positions are sorted by token first (token_sort.hip; its launches also clear dE).  The sorted order is cut into windows of
-// kWindow positions, whatever tokens they hold: a wave takes 64 vectors of columns of one window, walks its positions with
+// 4 to 32 positions, whatever tokens they hold: a wave takes 64 vectors of columns of one window, walks its positions with
 // kAhead rows on their way, and keeps the sum of the current token's rows in registers.  A token whose positions all lie in one
 // window is written to dE straight away; of one that reaches into others every window leaves a partial sum, and a
 // second kernel adds these up window by window.  So the work per wave is the same however often a token occurs, and the order of
@@ -12,8 +12,11 @@ namespace bsr {
 
 namespace {
 
-constexpr int kWindow = 32;
 constexpr int kAhead = 8;
+constexpr int kGroup = 16;                     // windows whose runs a workgroup of the second kernel joins
+constexpr int kLong = 15;                      // windows of a run from which the waves share it
+constexpr int kLeastWindow = 4;
+constexpr int64_t kEnoughWaves = 2048;
 constexpr int kThreads = 256;
 
 // The sum of a run of equal tokens, positions [first, last) of the sorted order (inside one window, [lo, hi)): to its row of dE,
@@ -55,14 +58,14 @@ template <typename T, int VE>
 __global__ __launch_bounds__(kThreads) void window_sum_kernel(const uint2 *__restrict__ sorted, int64_t n, uint32_t V,
                                                               const T *__restrict__ dY, int64_t D, int64_t lddy, float scale,
                                                               float *__restrict__ dE, int64_t ldde, int accumulate,
-                                                              float *__restrict__ partial, int64_t slices) {
+                                                              float *__restrict__ partial, int64_t slices, int size) {
   typedef RowVec<T, VE> R;
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
   const int64_t window = unit / slices, slice = unit - window * slices;
-  const int64_t lo = window * kWindow;
+  const int64_t lo = window * size;
   if (lo >= n) return;
-  const int count = (int)(n - lo < kWindow ? n - lo : kWindow);
+  const int count = (int)(n - lo < size ? n - lo : size);
   // lane l holds position lo - 1 + l of the sorted order: its neighbours tell where runs go on
   uint2 e = uint2{0xFFFFFFFFu, 0};
   if (lane <= count + 1 && lo - 1 + lane >= 0 && lo - 1 + lane < n) e = sorted[lo - 1 + lane];
@@ -104,39 +107,117 @@ __global__ __launch_bounds__(kThreads) void window_sum_kernel(const uint2 *__res
   }
 }
 
-// dE[token] for the tokens that reach over several windows: one wave per 64 columns of the window where such a token's run
-// starts; it adds that window's sum and those of the windows that the run goes on into.
-__global__ __launch_bounds__(kThreads) void join_kernel(const uint2 *__restrict__ sorted, int64_t n, uint32_t V, int64_t D,
-                                                        float scale, float *__restrict__ dE, int64_t ldde, int accumulate,
-                                                        const float *__restrict__ partial, int64_t windows, int64_t slices) {
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int64_t window = unit / slices, slice = unit - window * slices;
-  const int64_t lo = window * kWindow, behind = lo + kWindow;
-  if (behind >= n) return;                                       // no window behind
-  const uint32_t token = sorted[behind - 1].x;
-  if (token >= V || sorted[behind].x != token) return;           // no run goes on
-  if (lo > 0 && sorted[lo].x == token && sorted[lo - 1].x == token) return;   // it started before
-  const int64_t c = slice * 64 + lane;
-  float sum = c < D ? partial[(2 * window + 1) * D + c] : 0.0f;
-  for (int64_t w0 = window + 1; w0 < windows; w0 += 64) {
-    // windows that the run reaches into: those whose first position holds its token
-    const int64_t w = w0 + lane;
-    const uint64_t more = __ballot(w < windows && sorted[w < windows ? w * kWindow : 0].x == token);
-    const int reach = more == ~uint64_t(0) ? 64 : __builtin_ctzll(~more);
-    if (c < D) {
-#pragma unroll 8
-      for (int i = 0; i < reach; ++i) sum += partial[2 * (w0 + i) * D + c];
-    }
-    if (reach < 64) break;
-  }
-  if (c < D) {
-    float *dst = dE + (int64_t)token * ldde + c;
-    *dst = accumulate ? *dst + sum * scale : sum * scale;
+// sum += the first sums (`partial`, 2 D apart) of `count` windows, in order.
+template <int VE>
+__device__ __forceinline__ void add_windows(const float *partial, int64_t count, int64_t D, float *sum) {
+  typedef RowVec<float, VE> R;
+  for (int64_t i0 = 0; i0 < count; i0 += kAhead) {
+    typename R::Raw x[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) x[u] = R::load(partial + 2 * (i0 + u < count ? i0 + u : count - 1) * D);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int q = 0; q < VE; ++q) sum[q] = i0 + u < count ? sum[q] + R::elem(x[u], q) : sum[q];
   }
 }
 
-size_t partial_bytes(int64_t T, int64_t D) { return T > kWindow ? align_up((size_t)ceil_div(T, (int64_t)kWindow) * 2 * D * sizeof(float), 256) : 0; }
+// dE[token] for the tokens that reach over several windows: one workgroup per kGroup windows and 64 vectors of columns takes the
+// runs that start in them.  Its waves take the short runs in turn; the windows of a long one are shared out among them in four parts,
+// whose sums are added in order.
+template <int VE>
+__global__ __launch_bounds__(kThreads) void join_kernel(const uint2 *__restrict__ sorted, int64_t n, uint32_t V, int64_t D,
+                                                        float scale, float *__restrict__ dE, int64_t ldde, int accumulate,
+                                                        const float *__restrict__ partial, int64_t windows, int64_t slices, int size) {
+  constexpr int kWaves = kThreads / 64;
+  typedef RowVec<float, VE> R;
+  __shared__ float parts[kWaves][64 * VE];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
+  // lane l: whether a run starts in window l of the group and goes on behind it, and whose it is
+  const int64_t mine = group * kGroup + lane, lo = mine * size, behind = lo + size;
+  uint32_t token = V;
+  if (lane < kGroup && behind < n) {
+    const uint32_t last = sorted[behind - 1].x, next = sorted[behind].x, start = sorted[lo].x, before = lo > 0 ? sorted[lo - 1].x : V;
+    if (last == next && !(start == last && before == last)) token = last;
+  }
+  uint64_t runs = __ballot(token < V);
+  if (runs == 0) return;
+  const int64_t v = slice * 64 + lane, vecs = ceil_div(D, (int64_t)VE);
+  const bool in = v < vecs;
+  const int64_t at = vector_start(in ? v : 0, VE, D);
+  const int skip = in ? (int)(v * VE - at) : VE;
+  // windows behind window w that a run of `tok` goes on into, up to `most` of them or a few more
+  auto reach_of = [&](int64_t w, uint32_t tok, int64_t most) {
+    int64_t reach = 0;
+    while (reach < most) {
+      const int64_t x = w + 1 + reach + lane;
+      const uint64_t more = __ballot(x < windows && sorted[x < windows ? x * size : 0].x == tok);
+      reach += more == ~uint64_t(0) ? 64 : __builtin_ctzll(~more);
+      if (more != ~uint64_t(0)) break;
+    }
+    return reach;
+  };
+  uint64_t late = 0;
+  for (int turn = 0; runs != 0; runs &= runs - 1, ++turn) {
+    const int l = __builtin_ctzll(runs);
+    const int64_t w = group * kGroup + l;
+    const uint32_t tok = __builtin_amdgcn_readlane(token, l);
+    // (a run is long for all waves or for none: whether the window kLong behind still begins with its token)
+    if (w + 1 + kLong < windows && sorted[(w + 1 + kLong) * size].x == tok) {
+      late |= uint64_t(1) << l;
+      continue;
+    }
+    if (turn % kWaves != wave) continue;
+    const int64_t reach = reach_of(w, tok, 64);
+    float sum[VE];
+    const typename R::Raw own = R::load(partial + (2 * w + 1) * D + at);
+#pragma unroll
+    for (int q = 0; q < VE; ++q) sum[q] = R::elem(own, q);
+    add_windows<VE>(partial + 2 * (w + 1) * D + at, reach, D, sum);
+    put_sum<VE>(sum, false, false, scale, dE + (int64_t)tok * ldde, nullptr, at, skip, accumulate != 0);
+  }
+  for (; late != 0; late &= late - 1) {
+    const int l = __builtin_ctzll(late);
+    const int64_t w = group * kGroup + l;
+    const uint32_t tok = __builtin_amdgcn_readlane(token, l);
+    const int64_t reach = reach_of(w, tok, windows), share = (reach + kWaves - 1) / kWaves;
+    const int64_t from = wave * share < reach ? wave * share : reach, count = reach - from < share ? reach - from : share;
+    float sum[VE];
+#pragma unroll
+    for (int q = 0; q < VE; ++q) sum[q] = 0.0f;
+    if (wave == 0) {
+      const typename R::Raw own = R::load(partial + (2 * w + 1) * D + at);
+#pragma unroll
+      for (int q = 0; q < VE; ++q) sum[q] = R::elem(own, q);
+    }
+    add_windows<VE>(partial + 2 * (w + 1 + from) * D + at, count, D, sum);
+#pragma unroll
+    for (int q = 0; q < VE; ++q) parts[wave][q * 64 + lane] = sum[q];
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int q = 0; q < VE; ++q) {
+        for (int o = 1; o < kWaves; ++o) sum[q] += parts[o][q * 64 + lane];
+      }
+      put_sum<VE>(sum, false, false, scale, dE + (int64_t)tok * ldde, nullptr, at, skip, accumulate != 0);
+    }
+    __syncthreads();
+  }
+}
+
+// Positions of a window: 32, or fewer where that leaves too few waves (64 vectors of `per` columns of a window each) to hide the
+// loads' latency.
+int window_size(int64_t T, int64_t D) {
+  int size = 32;
+  while (size > kLeastWindow && T > size / 2 && ceil_div(T, (int64_t)size) * ceil_div(D, (int64_t)512) < kEnoughWaves) size /= 2;
+  return size;
+}
+
+size_t partial_bytes(int64_t T, int64_t D) {
+  const int64_t windows = ceil_div(T, (int64_t)window_size(T, D));
+  return windows > 1 ? align_up((size_t)windows * 2 * D * sizeof(float), 256) : 0;
+}
 
 }  // namespace
 
@@ -149,12 +230,13 @@ int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const v
   const uint2 *sorted = nullptr;
   int rc = launch_token_sort(tokens, index_type, T, V, clear, static_cast<char *>(ws) + partial_bytes(T, D), &sorted, s);
   if (rc != BSR_OK || T == 0) return rc;
-  const int64_t windows = ceil_div(T, (int64_t)kWindow);
+  const int size = window_size(T, D);
+  const int64_t windows = ceil_div(T, (int64_t)size);
 #define BSR_CALL(TY, VE)                                                                                                       \
   const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
   hipLaunchKernelGGL((window_sum_kernel<TY, VE>), dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))),         \
                      dim3(kThreads), 0, s, sorted, T, (uint32_t)V, static_cast<const TY *>(dY), D, lddy, scale, dE, ldde,      \
-                     accumulate, partial, slices)
+                     accumulate, partial, slices, size)
   if (dtype == BSR_F32) {
     if (D >= 4) { BSR_CALL(float, 4); } else { BSR_CALL(float, 1); }
   } else {
@@ -163,9 +245,12 @@ int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const v
 #undef BSR_CALL
   rc = check_launch();
   if (rc != BSR_OK || windows == 1) return rc;
-  const int64_t slices = ceil_div(D, (int64_t)64);
-  hipLaunchKernelGGL(join_kernel, dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))), dim3(kThreads), 0, s,
-                     sorted, T, (uint32_t)V, D, scale, dE, ldde, accumulate, partial, windows, slices);
+#define BSR_JOIN(VE)                                                                                                           \
+  const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
+  hipLaunchKernelGGL((join_kernel<VE>), dim3((unsigned)(ceil_div(windows, (int64_t)kGroup) * slices)), dim3(kThreads),         \
+                     0, s, sorted, T, (uint32_t)V, D, scale, dE, ldde, accumulate, partial, windows, slices, size)
+  if (D >= 4) { BSR_JOIN(4); } else { BSR_JOIN(1); }
+#undef BSR_JOIN
   return check_launch();
 }
 

@@ -64,11 +64,11 @@ __device__ __forceinline__ void clear_part(const ClearJob &c, int64_t part) {
 
 // counts[block][bin]
 template <Source S>
-__global__ __launch_bounds__(kThreads) void count_kernel(Keys k, uint32_t *__restrict__ counts, int blocks, ClearJob clear) {
+__global__ __launch_bounds__(kThreads) void count_kernel(Keys k, uint32_t *__restrict__ counts, int blocks, ClearJob clear, unsigned part) {
   __shared__ uint32_t bin[kMaxBins];
   const int t = threadIdx.x;
   if ((int)blockIdx.x >= blocks) {
-    clear_part(clear, (int64_t)blockIdx.x - blocks);
+    clear_part(clear, (int64_t)part + blockIdx.x - blocks);
     return;
   }
   for (int b = t; b < k.bins; b += kThreads) bin[b] = 0;
@@ -110,13 +110,13 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t *a, int n, int lane) {
 
 template <Source S, bool EXPERTS>
 __global__ __launch_bounds__(kThreads) void place_kernel(Keys k, const uint32_t *__restrict__ counts, int blocks, Places out,
-                                                         ClearJob clear) {
+                                                         ClearJob clear, unsigned part) {
   __shared__ uint32_t next[kWaves][kMaxBins];  // place of a wave's next entry of a value
   __shared__ uint32_t start[kMaxBins];         // of a value's entries in the whole
   __shared__ uint32_t total[EXPERTS ? kMaxBins : 1];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   if ((int)blockIdx.x >= blocks) {
-    clear_part(clear, (int64_t)blockIdx.x - blocks);
+    clear_part(clear, (int64_t)part + blockIdx.x - blocks);
     return;
   }
   for (int b = t; b < kWaves * kMaxBins; b += kThreads) (&next[0][0])[b] = 0;
@@ -224,18 +224,33 @@ unsigned clear_blocks(const ClearJob &c) {
   return (unsigned)ceil_div(c.rows, per);
 }
 
-// One pass; `clear` rides in its first launch.
+// What is to be cleared, handed out to the launches of a sort: each takes its share of the parts that are left.
+struct Clearing {
+  ClearJob job;
+  unsigned parts, next = 0;
+  explicit Clearing(const ClearJob &j) : job(j), parts(clear_blocks(j)) {}
+  // the share of a launch with `launches` more to come, in workgroups; *first: its first part
+  unsigned share(int launches, unsigned *first) {
+    *first = next;
+    const unsigned n = (parts - next) / (unsigned)(launches + 1);
+    const unsigned mine = launches == 0 ? parts - next : n;
+    next += mine;
+    return mine;
+  }
+};
+
+// One pass, with `later` launches of the sort behind it.
 template <Source S, bool EXPERTS>
-int launch_pass(const Keys &k, int blocks, uint32_t *counts, const Places &out, const ClearJob &clear, hipStream_t s) {
-  const unsigned extra = clear_blocks(clear);
-  const ClearJob none = {nullptr, 0, 0, 0};
+int launch_pass(const Keys &k, int blocks, uint32_t *counts, const Places &out, Clearing *clear, int later, hipStream_t s) {
+  unsigned first, extra;
   if (blocks > 1) {
-    hipLaunchKernelGGL((count_kernel<S>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, clear);
+    extra = clear->share(later + 1, &first);
+    hipLaunchKernelGGL((count_kernel<S>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, clear->job, first);
     const int rc = check_launch();
     if (rc != BSR_OK) return rc;
   }
-  hipLaunchKernelGGL((place_kernel<S, EXPERTS>), dim3(blocks > 1 ? blocks : 1 + extra), dim3(kThreads), 0, s, k, counts, blocks,
-                     out, blocks > 1 ? none : clear);
+  extra = clear->share(later, &first);
+  hipLaunchKernelGGL((place_kernel<S, EXPERTS>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, out, clear->job, first);
   return check_launch();
 }
 
@@ -252,9 +267,9 @@ int launch_expert_sort(const void *ids, int index_type, int64_t n, int64_t E, in
   int blocks;
   stretches(n, &k.steps, &blocks);
   const Places out = {nullptr, offsets, counts, order, slots, rows, align, E};
-  const ClearJob none = {nullptr, 0, 0, 0};
-  return index_type == BSR_I64 ? launch_pass<kFromI64, true>(k, blocks, static_cast<uint32_t *>(ws), out, none, s)
-                               : launch_pass<kFromI32, true>(k, blocks, static_cast<uint32_t *>(ws), out, none, s);
+  Clearing none(ClearJob{nullptr, 0, 0, 0});
+  return index_type == BSR_I64 ? launch_pass<kFromI64, true>(k, blocks, static_cast<uint32_t *>(ws), out, &none, 0, s)
+                               : launch_pass<kFromI32, true>(k, blocks, static_cast<uint32_t *>(ws), out, &none, 0, s);
 }
 
 size_t token_sort_ws_bytes(int64_t T, int64_t V) {
@@ -269,17 +284,17 @@ int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, 
   char *base = static_cast<char *>(ws);
   uint2 *buffer[2] = {reinterpret_cast<uint2 *>(base), reinterpret_cast<uint2 *>(base + (passes > 1 ? pairs_bytes : 0))};
   uint32_t *counts = reinterpret_cast<uint32_t *>(base + (passes > 1 ? 2 : 1) * pairs_bytes);
-  const ClearJob none = {nullptr, 0, 0, 0};
+  Clearing clearing(clear);
   for (int p = 0; p < passes; ++p) {
     Keys k = {p == 0 ? tokens : buffer[(p - 1) & 1], T, (uint32_t)V, p * bits, (1u << bits) - 1u, 1 << bits, bits, 0};
     int blocks;
     stretches(T, &k.steps, &blocks);
     Places out = {};
     out.pairs = buffer[p & 1];
-    const ClearJob &c = p == 0 ? clear : none;
-    const int rc = p > 0 ? launch_pass<kFromPairs, false>(k, blocks, counts, out, c, s)
-                   : index_type == BSR_I64 ? launch_pass<kFromI64, false>(k, blocks, counts, out, c, s)
-                                           : launch_pass<kFromI32, false>(k, blocks, counts, out, c, s);
+    const int later = (passes - 1 - p) * (blocks > 1 ? 2 : 1);
+    const int rc = p > 0 ? launch_pass<kFromPairs, false>(k, blocks, counts, out, &clearing, later, s)
+                   : index_type == BSR_I64 ? launch_pass<kFromI64, false>(k, blocks, counts, out, &clearing, later, s)
+                                           : launch_pass<kFromI32, false>(k, blocks, counts, out, &clearing, later, s);
     if (rc != BSR_OK) return rc;
   }
   *sorted = buffer[(passes - 1) & 1];
