@@ -3,7 +3,8 @@
 // A counting sort of up to kMaxBins values, in two launches: every workgroup counts the values of its stretch of entries
 // (count_kernel); then every workgroup adds up the counts of all, which says where the entries of a value start in the whole
 // and where its own among them, and moves its entries there in order (place_kernel).  Tokens, which have too many values for one such
-// pass, take one per digit, lowest first.  Up to one stretch of entries needs no counts of others and one launch per pass.
+// pass, take one per digit, lowest first.  Up to one stretch of entries needs no counts of others and one launch per pass; up to
+// kOneSort positions take one launch for all digits.
 //
 // Latency bound: a few bytes per entry.  Order within a workgroup: its waves own consecutive parts of the stretch, a wave takes 64
 // entries at a time and finds, for every lane, the lanes before it with the same value from one ballot per bit of the value.
@@ -18,8 +19,8 @@ constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxBins = 1025;                 // kMaxExperts and the dropped entries; digits of up to 10 bits
 constexpr int kDigitBits = 10;
-constexpr int kMinSteps = 4;                   // times 64 entries that a wave takes, at least
-constexpr int kMaxBlocks = 256;                // workgroups (stretches), at most: each reads the counts of all
+constexpr int kFewSteps = 4, kManySteps = 16;  // times 64 entries that a wave takes
+constexpr int kManyBlocks = 256;               // workgroups from which each takes kManySteps: each reads the counts of all
 constexpr int64_t kClearPerBlock = 32768;      // elements that a workgroup clears
 
 enum Source { kFromI32, kFromI64, kFromPairs };
@@ -32,7 +33,6 @@ struct Keys {
   int shift;
   uint32_t mask;
   int bins, bits;            // values that (key >> shift) & mask can have, and their bits
-  int steps;                 // times 64 entries per wave
 };
 
 template <Source S>
@@ -48,7 +48,7 @@ __device__ __forceinline__ void clear_part(const ClearJob &c, int64_t part) {
   if (c.ld == c.cols || c.rows == 1) {
     const int64_t total = c.rows * c.cols, lo = part * kClearPerBlock;
     const int64_t hi = lo + kClearPerBlock < total ? lo + kClearPerBlock : total;
-    for (int64_t i = lo + 4 * threadIdx.x; i < hi; i += 4 * kThreads) {
+    for (int64_t i = lo + 4 * threadIdx.x; i < hi; i += 4 * (int)blockDim.x) {
       if (i + 4 <= hi) {
         reinterpret_cast<Any16 *>(c.p + i)->w = Words4{0, 0, 0, 0};
       } else {
@@ -59,12 +59,13 @@ __device__ __forceinline__ void clear_part(const ClearJob &c, int64_t part) {
   }
   const int64_t per = kClearPerBlock / c.cols > 0 ? kClearPerBlock / c.cols : 1;
   for (int64_t r = part * per; r < (part + 1) * per && r < c.rows; ++r)
-    for (int64_t j = threadIdx.x; j < c.cols; j += kThreads) c.p[r * c.ld + j] = 0.0f;
+    for (int64_t j = threadIdx.x; j < c.cols; j += blockDim.x) c.p[r * c.ld + j] = 0.0f;
 }
 
 // counts[block][bin]
-template <Source S>
-__global__ __launch_bounds__(kThreads) void count_kernel(Keys k, uint32_t *__restrict__ counts, int blocks, ClearJob clear, unsigned part) {
+template <Source S, int STEPS>
+__global__ __launch_bounds__(kThreads) void count_kernel(Keys k, uint32_t *__restrict__ counts, int blocks, ClearJob clear,
+                                                         unsigned part) {
   __shared__ uint32_t bin[kMaxBins];
   const int t = threadIdx.x;
   if ((int)blockIdx.x >= blocks) {
@@ -73,7 +74,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Keys k, uint32_t *__res
   }
   for (int b = t; b < k.bins; b += kThreads) bin[b] = 0;
   __syncthreads();
-  const int64_t per = (int64_t)k.steps * kThreads, lo = blockIdx.x * per;
+  const int64_t per = (int64_t)STEPS * kThreads, lo = blockIdx.x * per;
   const int64_t hi = lo + per < k.n ? lo + per : k.n;
   for (int64_t i = lo + t; i < hi; i += kThreads) atomicAdd(&bin[digit_of(k, load_entry<S>(k, i).x)], 1u);
   __syncthreads();
@@ -87,9 +88,11 @@ struct Places {
   int64_t rows, align, experts;
 };
 
-// a[i] -> sum of a[0 .. i) by the first wave; returns the sum of all to its lanes
-__device__ __forceinline__ uint32_t scan_bins(uint32_t *a, int n, int lane) {
-  const int per = (n + 63) / 64, lo = lane * per, hi = lo + per < n ? lo + per : n;
+// a[i] -> sum of a[0 .. i) over the whole workgroup of WAVES waves; `sums` is shared, one number per wave.
+template <int WAVES>
+__device__ __forceinline__ void scan_bins(uint32_t *a, int n, uint32_t *sums) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, threads = WAVES * 64;
+  const int per = (n + threads - 1) / threads, lo = t * per, hi = lo + per < n ? lo + per : n;
   uint32_t sum = 0;
   for (int i = lo; i < hi; ++i) sum += a[i];
   uint32_t before = sum;
@@ -98,41 +101,72 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t *a, int n, int lane) {
     const uint32_t o = __shfl_up(before, d, 64);
     if (lane >= d) before += o;
   }
-  const uint32_t all = __shfl(before, 63, 64);
+  if (lane == 63) sums[w] = before;
+  __syncthreads();
   before -= sum;
+  for (int o = 0; o < w; ++o) before += sums[o];
   for (int i = lo; i < hi; ++i) {
     const uint32_t v = a[i];
     a[i] = before;
     before += v;
   }
-  return all;
+  __syncthreads();
 }
 
-template <Source S, bool EXPERTS>
+// The entry's number among its wave's entries of the same value so far (`count`: how many there were of every value), by the wave as
+// a whole; lanes with in == false have no entry.  count goes on.
+__device__ __forceinline__ uint32_t rank_entry(uint32_t *count, uint32_t d, int bits, bool in, int lane) {
+  uint64_t same = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (d >> b) & 1u;
+    const uint64_t ones = __ballot(one);
+    same &= one ? ones : ~ones;
+  }
+  uint32_t rank = 0;
+  if (in) rank = count[d] + (uint32_t)__builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+  // (the wave's reads above come before the write, and the write before the next round's reads: one wave's LDS accesses are
+  // executed in order; the fences keep the compiler to that)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (in && (same >> lane) >> 1 == 0) count[d] += (uint32_t)__builtin_popcountll(same);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  return rank;
+}
+
+// STEPS times 64 entries per wave.
+template <Source S, bool EXPERTS, int STEPS>
 __global__ __launch_bounds__(kThreads) void place_kernel(Keys k, const uint32_t *__restrict__ counts, int blocks, Places out,
                                                          ClearJob clear, unsigned part) {
-  __shared__ uint32_t next[kWaves][kMaxBins];  // place of a wave's next entry of a value
+  __shared__ uint32_t next[kWaves][kMaxBins];  // a wave's entries of a value, then where they start among the workgroup's and all before it
   __shared__ uint32_t start[kMaxBins];         // of a value's entries in the whole
   __shared__ uint32_t total[EXPERTS ? kMaxBins : 1];
+  __shared__ uint32_t sums[kWaves];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   if ((int)blockIdx.x >= blocks) {
     clear_part(clear, (int64_t)part + blockIdx.x - blocks);
     return;
   }
-  for (int b = t; b < kWaves * kMaxBins; b += kThreads) (&next[0][0])[b] = 0;
-  __syncthreads();
-  const int64_t lo = ((int64_t)blockIdx.x * kWaves + w) * k.steps * 64;
-  for (int q = 0; q < k.steps; ++q) {
-    const int64_t i = lo + q * 64 + lane;
-    if (i < k.n) atomicAdd(&next[w][digit_of(k, load_entry<S>(k, i).x)], 1u);
+  const int64_t lo = ((int64_t)blockIdx.x * kWaves + w) * STEPS * 64;
+  uint2 e[STEPS];
+  if (k.n > 0) {
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q) e[q] = load_entry<S>(k, lo + q * 64 + lane < k.n ? lo + q * 64 + lane : 0);
+  }
+  for (int b = lane; b < k.bins; b += 64) next[w][b] = 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  uint32_t rank[STEPS];
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {
+    rank[q] = 0;
+    if (lo + q * 64 < k.n) rank[q] = rank_entry(next[w], digit_of(k, e[q].x), k.bits, lo + q * 64 + lane < k.n, lane);
   }
   __syncthreads();
   // a value's entries in all workgroups, and in those before this one
   for (int b = t; b < k.bins; b += kThreads) {
     uint32_t all = 0, before = 0;
-    if (blocks == 1) {
-      for (int v = 0; v < kWaves; ++v) all += next[v][b];
-    } else {
+    if (blocks > 1) {
 #pragma unroll 8
       for (int c = 0; c < blocks; ++c) {
         const uint32_t n = counts[(int64_t)c * k.bins + b];
@@ -140,80 +174,114 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Keys k, const uint32_t 
         all += n;
       }
     }
+    uint32_t here = before;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+      const uint32_t n = next[v][b];
+      next[v][b] = here;
+      here += n;
+    }
+    if (blocks == 1) all = here;
     if constexpr (EXPERTS) {
       total[b] = all;
       all = (uint32_t)((all + out.align - 1) / out.align * out.align);
     }
     start[b] = all;
-    for (int v = 0; v < kWaves; ++v) {
-      const uint32_t n = next[v][b];
-      next[v][b] = before;
-      before += n;
-    }
   }
   __syncthreads();
-  if (w == 0) scan_bins(start, k.bins, lane);
-  __syncthreads();
+  scan_bins<kWaves>(start, k.bins, sums);
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {
+    const int64_t i = lo + q * 64 + lane;
+    if (i >= k.n) continue;
+    const uint32_t d = digit_of(k, e[q].x), place = start[d] + next[w][d] + rank[q];
+    if constexpr (EXPERTS) {
+      const bool kept = (int64_t)d < out.experts;
+      out.slots[i] = kept ? (int32_t)place : -1;
+      if (kept && (int64_t)place < out.rows) out.order[place] = (int32_t)i;
+    } else {
+      out.pairs[place] = e[q];
+    }
+  }
   if constexpr (EXPERTS) {
     // the last value stands for dropped entries: its start is the end of the last segment
     if (blockIdx.x == 0) {
-      for (int e = t; e <= out.experts; e += kThreads) {
-        out.offsets[e] = (int32_t)start[e];
-        if (e < out.experts) out.counts[e] = (int32_t)total[e];
+      for (int x = t; x <= out.experts; x += kThreads) {
+        out.offsets[x] = (int32_t)start[x];
+        if (x < out.experts) out.counts[x] = (int32_t)total[x];
       }
     }
-    for (int64_t e = blockIdx.x * kWaves + w; e < out.experts; e += (int64_t)blocks * kWaves)
-      for (int64_t s = (int64_t)start[e] + total[e] + lane; s < start[e + 1]; s += 64) out.order[s] = -1;
+    for (int64_t x = blockIdx.x * kWaves + w; x < out.experts; x += (int64_t)blocks * kWaves)
+      for (int64_t s = (int64_t)start[x] + total[x] + lane; s < start[x + 1]; s += 64) out.order[s] = -1;
     for (int64_t s = (int64_t)start[out.experts] + blockIdx.x * kThreads + t; s < out.rows; s += (int64_t)blocks * kThreads)
       out.order[s] = -1;
   }
-  // 64 entries at a time, each behind those of its value that stand before it
-  for (int q = 0; q < k.steps; ++q) {
-    const int64_t i = lo + q * 64 + lane;
-    const bool in = i < k.n;
-    uint2 e = uint2{0, 0};
-    if (in) e = load_entry<S>(k, i);
-    const uint32_t d = digit_of(k, e.x);
-    uint64_t same = __ballot(in);
-    for (int b = 0; b < k.bits; ++b) {
-      const bool one = (d >> b) & 1u;
-      const uint64_t ones = __ballot(one);
-      same &= one ? ones : ~ones;
-    }
-    if (in) {
-      const uint32_t before = (uint32_t)__builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
-      const uint32_t place = start[d] + next[w][d] + before;
-      if constexpr (EXPERTS) {
-        const bool kept = (int64_t)d < out.experts;
-        out.slots[i] = kept ? (int32_t)place : -1;
-        if (kept && (int64_t)place < out.rows) out.order[place] = (int32_t)i;
-      } else {
-        out.pairs[place] = e;
+}
+
+// Up to kOneSort positions sorted by all digits of their token in one launch, by one workgroup; the others clear.
+constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64, kOneSteps = 8, kOneSort = kOneThreads * kOneSteps;
+template <Source S>
+__global__ __launch_bounds__(kOneThreads) void sort_one_kernel(Keys k, int passes, uint2 *__restrict__ sorted, ClearJob clear) {
+  constexpr int kBins = 1 << kDigitBits;
+  __shared__ uint32_t next[kOneWaves][kBins];
+  __shared__ uint32_t start[kBins];
+  __shared__ uint32_t sums[kOneWaves];
+  __shared__ uint2 moved[kOneSort];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, n = (int)k.n;
+  if (blockIdx.x > 0) {
+    clear_part(clear, (int64_t)blockIdx.x - 1);
+    return;
+  }
+  const int steps = (n + kOneThreads - 1) / kOneThreads, lo = w * steps * 64;
+  uint2 e[kOneSteps];
+#pragma unroll
+  for (int q = 0; q < kOneSteps; ++q)
+    if (q < steps) e[q] = load_entry<S>(k, lo + q * 64 + lane < n ? lo + q * 64 + lane : 0);
+  for (int p = 0; p < passes; ++p, k.shift += k.bits) {
+    for (int b = lane; b < k.bins; b += 64) next[w][b] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    uint32_t rank[kOneSteps];
+#pragma unroll
+    for (int q = 0; q < kOneSteps; ++q)
+      if (q < steps && lo + q * 64 < n)
+        rank[q] = rank_entry(next[w], digit_of(k, e[q].x), k.bits, lo + q * 64 + lane < n, lane);
+    __syncthreads();
+    for (int b = t; b < k.bins; b += kOneThreads) {
+      uint32_t here = 0;
+#pragma unroll
+      for (int v = 0; v < kOneWaves; ++v) {
+        const uint32_t c = next[v][b];
+        next[v][b] = here;
+        here += c;
       }
+      start[b] = here;
     }
-    // (the wave's reads above come before the write, and the write before the next round's reads: one wave's LDS accesses
-    // are executed in order; the fences keep the compiler to that)
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (in && (same >> lane) >> 1 == 0) next[w][d] += (uint32_t)__builtin_popcountll(same);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    __syncthreads();
+    scan_bins<kOneWaves>(start, k.bins, sums);
+#pragma unroll
+    for (int q = 0; q < kOneSteps; ++q) {
+      if (q >= steps || lo + q * 64 + lane >= n) continue;
+      const uint32_t d = digit_of(k, e[q].x), place = start[d] + next[w][d] + rank[q];
+      if (p == passes - 1) sorted[place] = e[q];
+      else moved[place] = e[q];
+    }
+    if (p == passes - 1) return;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kOneSteps; ++q)
+      if (q < steps && lo + q * 64 + lane < n) e[q] = moved[lo + q * 64 + lane];
   }
 }
 
 int bit_length(uint32_t v) { return v == 0 ? 0 : 32 - __builtin_clz(v); }
 
 // Stretches of n entries.
-void stretches(int64_t n, int *steps, int *blocks) {
-  const int64_t least = ceil_div(n, (int64_t)kMaxBlocks * kThreads);
-  *steps = (int)(least > kMinSteps ? least : kMinSteps);
-  *blocks = (int)ceil_div(n, (int64_t)*steps * kThreads);
-  if (*blocks < 1) *blocks = 1;
-}
+int steps_of(int64_t n) { return n > (int64_t)kManyBlocks * kFewSteps * kThreads ? kManySteps : kFewSteps; }
+int blocks_of(int64_t n) { return n > 0 ? (int)ceil_div(n, (int64_t)steps_of(n) * kThreads) : 1; }
 
 size_t counts_bytes(int64_t n, int bins) {
-  int steps, blocks;
-  stretches(n, &steps, &blocks);
+  const int blocks = blocks_of(n);
   return blocks > 1 ? align_up((size_t)blocks * bins * sizeof(uint32_t), 256) : 0;
 }
 
@@ -240,18 +308,25 @@ struct Clearing {
 };
 
 // One pass, with `later` launches of the sort behind it.
-template <Source S, bool EXPERTS>
-int launch_pass(const Keys &k, int blocks, uint32_t *counts, const Places &out, Clearing *clear, int later, hipStream_t s) {
+template <Source S, bool EXPERTS, int STEPS>
+int launch_pass_(const Keys &k, int blocks, uint32_t *counts, const Places &out, Clearing *clear, int later, hipStream_t s) {
   unsigned first, extra;
   if (blocks > 1) {
     extra = clear->share(later + 1, &first);
-    hipLaunchKernelGGL((count_kernel<S>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, clear->job, first);
+    hipLaunchKernelGGL((count_kernel<S, STEPS>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, clear->job, first);
     const int rc = check_launch();
     if (rc != BSR_OK) return rc;
   }
   extra = clear->share(later, &first);
-  hipLaunchKernelGGL((place_kernel<S, EXPERTS>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, out, clear->job, first);
+  hipLaunchKernelGGL((place_kernel<S, EXPERTS, STEPS>), dim3(blocks + extra), dim3(kThreads), 0, s, k, counts, blocks, out,
+                     clear->job, first);
   return check_launch();
+}
+
+template <Source S, bool EXPERTS>
+int launch_pass(const Keys &k, int blocks, uint32_t *counts, const Places &out, Clearing *clear, int later, hipStream_t s) {
+  return steps_of(k.n) == kFewSteps ? launch_pass_<S, EXPERTS, kFewSteps>(k, blocks, counts, out, clear, later, s)
+                                    : launch_pass_<S, EXPERTS, kManySteps>(k, blocks, counts, out, clear, later, s);
 }
 
 int digit_passes(int64_t V) { return V < 1 ? 1 : (bit_length((uint32_t)V) + kDigitBits - 1) / kDigitBits; }
@@ -263,9 +338,8 @@ size_t expert_sort_ws_bytes(int64_t n, int64_t E) { return counts_bytes(n, (int)
 
 int launch_expert_sort(const void *ids, int index_type, int64_t n, int64_t E, int64_t align, int32_t *offsets, int32_t *counts,
                        int32_t *order, int64_t rows, int32_t *slots, void *ws, hipStream_t s) {
-  Keys k = {ids, n, (uint32_t)E, 0, 0xFFFFFFFFu, (int)E + 1, bit_length((uint32_t)E), 0};
-  int blocks;
-  stretches(n, &k.steps, &blocks);
+  const Keys k = {ids, n, (uint32_t)E, 0, 0xFFFFFFFFu, (int)E + 1, bit_length((uint32_t)E)};
+  const int blocks = blocks_of(n);
   const Places out = {nullptr, offsets, counts, order, slots, rows, align, E};
   Clearing none(ClearJob{nullptr, 0, 0, 0});
   return index_type == BSR_I64 ? launch_pass<kFromI64, true>(k, blocks, static_cast<uint32_t *>(ws), out, &none, 0, s)
@@ -284,11 +358,19 @@ int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, 
   char *base = static_cast<char *>(ws);
   uint2 *buffer[2] = {reinterpret_cast<uint2 *>(base), reinterpret_cast<uint2 *>(base + (passes > 1 ? pairs_bytes : 0))};
   uint32_t *counts = reinterpret_cast<uint32_t *>(base + (passes > 1 ? 2 : 1) * pairs_bytes);
+  if (T <= kOneSort) {
+    const Keys k = {tokens, T, (uint32_t)V, 0, (1u << bits) - 1u, 1 << bits, bits};
+    const dim3 grid(1 + clear_blocks(clear));
+    if (index_type == BSR_I64)
+      hipLaunchKernelGGL((sort_one_kernel<kFromI64>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], clear);
+    else hipLaunchKernelGGL((sort_one_kernel<kFromI32>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], clear);
+    *sorted = buffer[0];
+    return check_launch();
+  }
   Clearing clearing(clear);
   for (int p = 0; p < passes; ++p) {
-    Keys k = {p == 0 ? tokens : buffer[(p - 1) & 1], T, (uint32_t)V, p * bits, (1u << bits) - 1u, 1 << bits, bits, 0};
-    int blocks;
-    stretches(T, &k.steps, &blocks);
+    const Keys k = {p == 0 ? tokens : buffer[(p - 1) & 1], T, (uint32_t)V, p * bits, (1u << bits) - 1u, 1 << bits, bits};
+    const int blocks = blocks_of(T);
     Places out = {};
     out.pairs = buffer[p & 1];
     const int later = (passes - 1 - p) * (blocks > 1 ? 2 : 1);
