@@ -13,7 +13,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;          // vectors that a lane has on their way, per row
 constexpr int kChoices = 8;        // choices of a token that are handled together
-constexpr int kPadSlots = 64;      // rows of the sorted matrix that one wave looks over for padding
 
 // out[t] = scale * table[tokens[t]]
 template <typename T, int VE, typename I>
@@ -49,14 +48,14 @@ __global__ __launch_bounds__(kThreads) void embedding_lookup_kernel(const T *__r
   }
 }
 
-// +0.0 in the rows of [s0, s0 + kPadSlots) that hold no entry, by one wave.
+// +0.0 in the rows of [s0, s0 + count) that hold no entry, by one wave; count <= 64.
 template <typename T, int VE>
-__device__ __forceinline__ void clear_padding(const int32_t *__restrict__ order, int64_t rows, int64_t s0, T *__restrict__ Xs,
-                                              int64_t ldxs, int64_t D, int lane) {
+__device__ __forceinline__ void clear_padding(const int32_t *__restrict__ order, int64_t rows, int64_t s0, int count,
+                                              T *__restrict__ Xs, int64_t ldxs, int64_t D, int lane) {
   typedef RowVec<T, VE> R;
   if (s0 >= rows) return;
   const int64_t s = s0 + lane;
-  uint64_t pad = __ballot(s < rows && order[s < rows ? s : s0] < 0);
+  uint64_t pad = __ballot(lane < count && s < rows && order[s < rows ? s : s0] < 0);
   const int64_t vecs = ceil_div(D, (int64_t)VE);
   for (; pad != 0; pad &= pad - 1) {
     T *dst = Xs + (s0 + __builtin_ctzll(pad)) * ldxs;
@@ -69,11 +68,12 @@ template <typename T, int VE>
 __global__ __launch_bounds__(kThreads) void expert_gather_kernel(const T *__restrict__ X, int64_t tokens, int64_t D, int64_t ldx,
                                                                  const int32_t *__restrict__ slots, int64_t k,
                                                                  const int32_t *__restrict__ order, int64_t rows,
-                                                                 T *__restrict__ Xs, int64_t ldxs, int sh, unsigned pad_blocks) {
+                                                                 T *__restrict__ Xs, int64_t ldxs, int sh, unsigned pad_blocks,
+    int pad_rows) {
   typedef RowVec<T, VE> R;
   const int t = threadIdx.x;
   if (blockIdx.x < pad_blocks) {
-    clear_padding<T, VE>(order, rows, ((int64_t)blockIdx.x * (kThreads / 64) + (t >> 6)) * kPadSlots, Xs, ldxs, D, t & 63);
+    clear_padding<T, VE>(order, rows, ((int64_t)blockIdx.x * (kThreads / 64) + (t >> 6)) * pad_rows, pad_rows, Xs, ldxs, D, t & 63);
     return;
   }
   const int64_t row = ((int64_t)(blockIdx.x - pad_blocks) * kThreads + t) >> sh;
@@ -164,11 +164,12 @@ template <typename T, int VE, int KC>
 __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
     const T *__restrict__ Ys, int64_t rows, int64_t D, int64_t ldys, const int32_t *__restrict__ slots,
     const int32_t *__restrict__ order, int64_t tokens, int64_t k, const float *__restrict__ weights, const T *__restrict__ dOut,
-    int64_t lddo, T *__restrict__ dYs, int64_t lddys, float *__restrict__ dweights, int sh, unsigned pad_blocks) {
+    int64_t lddo, T *__restrict__ dYs, int64_t lddys, float *__restrict__ dweights, int sh, unsigned pad_blocks,
+    int pad_rows) {
   typedef RowVec<T, VE> R;
   const int t = threadIdx.x;
   if (blockIdx.x < pad_blocks) {
-    clear_padding<T, VE>(order, rows, ((int64_t)blockIdx.x * (kThreads / 64) + (t >> 6)) * kPadSlots, dYs, lddys, D, t & 63);
+    clear_padding<T, VE>(order, rows, ((int64_t)blockIdx.x * (kThreads / 64) + (t >> 6)) * pad_rows, pad_rows, dYs, lddys, D, t & 63);
     return;
   }
   const int64_t row = ((int64_t)(blockIdx.x - pad_blocks) * kThreads + t) >> sh;
@@ -220,7 +221,9 @@ int row_lanes(int64_t vecs) { return vecs > 32 ? 6 : vecs > 16 ? 5 : 4; }
 
 unsigned row_blocks(int64_t rows, int sh) { return (unsigned)ceil_div(rows << sh, (int64_t)kThreads); }
 
-unsigned padding_blocks(int64_t rows) { return (unsigned)ceil_div(rows, (int64_t)kPadSlots * (kThreads / 64)); }
+// Rows of the sorted matrix that one wave looks over for padding, one after the other: few where there are few rows.
+int padding_rows(int64_t rows) { return rows < 4096 ? 1 : rows < 32768 ? 4 : 16; }
+unsigned padding_blocks(int64_t rows) { return (unsigned)ceil_div(rows, (int64_t)padding_rows(rows) * (kThreads / 64)); }
 
 }  // namespace
 
@@ -252,7 +255,8 @@ int launch_expert_gather(const void *X, int dtype, int64_t T, int64_t D, int64_t
 #define BSR_CALL(TY, VE)                                                                                                      \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
   hipLaunchKernelGGL((expert_gather_kernel<TY, VE>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,                      \
-                     static_cast<const TY *>(X), T, D, ldx, slots, k, order, rows, static_cast<TY *>(Xs), ldxs, sh, pad)
+                     static_cast<const TY *>(X), T, D, ldx, slots, k, order, rows, static_cast<TY *>(Xs), ldxs, sh, pad,       \
+                     padding_rows(rows))
   BSR_BY_ROW(dtype, D, BSR_CALL)
 #undef BSR_CALL
   return check_launch();
@@ -280,7 +284,7 @@ int launch_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t 
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
   hipLaunchKernelGGL((expert_combine_grad_kernel<TY, VE, KC>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,            \
                      static_cast<const TY *>(Ys), rows, D, ldys, slots, order, T, k, weights, static_cast<const TY *>(dOut),  \
-                     lddo, static_cast<TY *>(dYs), lddys, dweights, sh, pad)
+                     lddo, static_cast<TY *>(dYs), lddys, dweights, sh, pad, padding_rows(rows))
 #define BSR_CALL(TY, VE)                                                    \
   if (k <= 2) { BSR_CALL_(TY, VE, 2); } else if (k <= 4) { BSR_CALL_(TY, VE, 4); } else { BSR_CALL_(TY, VE, kChoices); }
   BSR_BY_ROW(dtype, D, BSR_CALL)
