@@ -12,6 +12,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;          // vectors that a lane has on their way, per row
+// Sorted rows that are read past the caches, in bytes of them all ([25088 x 2] choices of 1536 bf16, combine and its gradient with
+// the inputs' gradient 123 -> 110 us, [4096 x 8] of 2048 115 -> 93, [8000 x 4] of 1024 f32 37.1 -> 34.7; of rows that share lines,
+// [9947 x 3] of 805 bf16, 12.0 -> 14.5).
+constexpr int64_t kStreamBytes = int64_t(64) << 20;
 constexpr int kChoices = 8;        // choices of a token that are handled together
 
 // out[t] = scale * table[tokens[t]]
@@ -121,8 +125,15 @@ __device__ __forceinline__ void load_choices(const int32_t *__restrict__ slots, 
   }
 }
 
+// A vector of a row that only one group of lanes reads: non-temporal (STREAM) or as any other.
+template <typename T, int VE, bool STREAM>
+__device__ __forceinline__ typename RowVec<T, VE>::Raw load_once(const T *p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const typename RowVec<T, VE>::Raw *>(p));
+  else return RowVec<T, VE>::load(p);
+}
+
 // out[t] = sum_j weights[t][j] * Ys[slots[t][j]]; KC choices are read together.
-template <typename T, int VE, int KC>
+template <typename T, int VE, int KC, bool STREAM>
 __global__ __launch_bounds__(kThreads) void expert_combine_kernel(const T *__restrict__ Ys, int64_t rows, int64_t D, int64_t ldys,
                                                                   const int32_t *__restrict__ slots, int64_t tokens, int64_t k,
                                                                   const float *__restrict__ weights, T *__restrict__ out,
@@ -146,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void expert_combine_kernel(const T *__res
 #pragma unroll
       for (int j = 0; j < KC; ++j) {
         y[j] = R::zero();
-        if (c.there[j]) y[j] = R::load(Ys + (int64_t)c.slot[j] * ldys + at);
+        if (c.there[j]) y[j] = load_once<T, VE, STREAM>(Ys + (int64_t)c.slot[j] * ldys + at);
       }
 #pragma unroll
       for (int j = 0; j < KC; ++j) {
@@ -160,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void expert_combine_kernel(const T *__res
 
 // dYs[slots[t][j]] = weights[t][j] * dOut[t], dweights[t][j] = <Ys[slots[t][j]], dOut[t]>: dOut is read once per KC choices, and
 // the products of a row are added up by its lanes in a fixed order.
-template <typename T, int VE, int KC>
+template <typename T, int VE, int KC, bool STREAM>
 __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
     const T *__restrict__ Ys, int64_t rows, int64_t D, int64_t ldys, const int32_t *__restrict__ slots,
     const int32_t *__restrict__ order, int64_t tokens, int64_t k, const float *__restrict__ weights, const T *__restrict__ dOut,
@@ -192,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
 #pragma unroll
       for (int j = 0; j < KC; ++j) {
         y[j] = R::zero();
-        if (c.there[j]) y[j] = R::load(Ys + (int64_t)c.slot[j] * ldys + at);
+        if (c.there[j]) y[j] = load_once<T, VE, STREAM>(Ys + (int64_t)c.slot[j] * ldys + at);
       }
       float gf[VE];
 #pragma unroll
@@ -226,6 +237,12 @@ int padding_rows(int64_t rows) { return rows < 4096 ? 1 : rows < 32768 ? 4 : 16;
 unsigned padding_blocks(int64_t rows) { return (unsigned)ceil_div(rows, (int64_t)padding_rows(rows) * (kThreads / 64)); }
 
 }  // namespace
+
+// Whether the sorted rows are read past the caches: not where they may still be there, or share 128-byte lines.
+bool stream_rows(const void *p, int64_t rows, int64_t D, int64_t ld, int dtype) {
+  const int64_t e = elem_bytes(dtype);
+  return (uintptr_t)p % 128 == 0 && D * e % 128 == 0 && ld * e % 128 == 0 && rows * D * e >= kStreamBytes;
+}
 
 // f32 / bf16 and whole or single-element vectors
 #define BSR_BY_ROW(dtype, D, CALL)                              \
@@ -262,14 +279,21 @@ int launch_expert_gather(const void *X, int dtype, int64_t T, int64_t D, int64_t
   return check_launch();
 }
 
+// as many choices together as a token has, up to kChoices
+#define BSR_CHOICES(TY, VE, STREAM)                           \
+  if (k <= 2) { BSR_CALL_(TY, VE, 2, STREAM); }               \
+  else if (k <= 4) { BSR_CALL_(TY, VE, 4, STREAM); }          \
+  else { BSR_CALL_(TY, VE, kChoices, STREAM); }
+
 int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, int64_t ldys, const int32_t *slots, int64_t T,
                           int64_t k, const float *weights, void *out, int64_t ldo, hipStream_t s) {
-#define BSR_CALL_(TY, VE, KC)                                                                                                 \
+  const bool stream = stream_rows(Ys, rows, D, ldys, dtype);
+#define BSR_CALL_(TY, VE, KC, ST)                                                                                             \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_combine_kernel<TY, VE, KC>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,                       \
+  hipLaunchKernelGGL((expert_combine_kernel<TY, VE, KC, ST>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,                       \
                      static_cast<const TY *>(Ys), rows, D, ldys, slots, T, k, weights, static_cast<TY *>(out), ldo, sh)
 #define BSR_CALL(TY, VE)                                                    \
-  if (k <= 2) { BSR_CALL_(TY, VE, 2); } else if (k <= 4) { BSR_CALL_(TY, VE, 4); } else { BSR_CALL_(TY, VE, kChoices); }
+  if (stream) { BSR_CHOICES(TY, VE, (VE != 1)) } else { BSR_CHOICES(TY, VE, false) }
   BSR_BY_ROW(dtype, D, BSR_CALL)
 #undef BSR_CALL
 #undef BSR_CALL_
@@ -279,14 +303,15 @@ int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, in
 int launch_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t D, int64_t ldys, const int32_t *slots,
                                const int32_t *order, int64_t T, int64_t k, const float *weights, const void *dOut, int64_t lddo,
                                void *dYs, int64_t lddys, float *dweights, hipStream_t s) {
+  const bool stream = stream_rows(Ys, rows, D, ldys, dtype);
   const unsigned pad = padding_blocks(rows);
-#define BSR_CALL_(TY, VE, KC)                                                                                                 \
+#define BSR_CALL_(TY, VE, KC, ST)                                                                                             \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_combine_grad_kernel<TY, VE, KC>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,            \
+  hipLaunchKernelGGL((expert_combine_grad_kernel<TY, VE, KC, ST>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,            \
                      static_cast<const TY *>(Ys), rows, D, ldys, slots, order, T, k, weights, static_cast<const TY *>(dOut),  \
                      lddo, static_cast<TY *>(dYs), lddys, dweights, sh, pad, padding_rows(rows))
 #define BSR_CALL(TY, VE)                                                    \
-  if (k <= 2) { BSR_CALL_(TY, VE, 2); } else if (k <= 4) { BSR_CALL_(TY, VE, 4); } else { BSR_CALL_(TY, VE, kChoices); }
+  if (stream) { BSR_CHOICES(TY, VE, (VE != 1)) } else { BSR_CHOICES(TY, VE, false) }
   BSR_BY_ROW(dtype, D, BSR_CALL)
 #undef BSR_CALL
 #undef BSR_CALL_

@@ -165,6 +165,15 @@ int64_t blocks(int64_t n, int64_t b) { return b > 0 ? (n + b - 1) / b : 0; }
 
 PyObject *code_result(int rc) { return PyLong_FromLong(rc); }
 
+// Parts of one allocation: each a contiguous tensor of its own from element `offset` on.  (Several small outputs cost one allocation
+// this way, and a view made by torch's operators costs as much as an allocation.)
+at::Tensor part_of(const at::Tensor &whole, int64_t offset, at::IntArrayRef size) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+  t.unsafeGetTensorImpl()->set_storage_offset(offset);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+  return t;
+}
+
 // Runs f, which calls the C library, without the GIL; it is held again however f ends.
 struct GilReleased {
   PyThreadState *const save = PyEval_SaveThread();
@@ -484,10 +493,19 @@ PyObject *expert_sort(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int64_t rows = bsr_expert_capacity(entries, E, align);
     if (rows < 0) return code_result(BSR_ERR_SHAPE);
     const CallStream stream(a[8], ids);
-    const Output offsets = packed_output(a[3], "offsets", {E + 1}, at::kInt, ids);
-    const Output counts = packed_output(a[4], "counts", {E}, at::kInt, ids);
-    const Output order = packed_output(a[5], "order", {rows}, at::kInt, ids);
-    const Output slots = packed_output(a[6], "slots", ids.sizes(), at::kInt, ids);
+    Output offsets, counts, order, slots;
+    if (a[3] == Py_None && a[4] == Py_None && a[5] == Py_None && a[6] == Py_None) {
+      const at::Tensor all = new_tensor({2 * E + 1 + rows + entries}, at::kInt, ids);
+      offsets.own = part_of(all, rows + entries, {E + 1});
+      counts.own = part_of(all, rows + entries + E + 1, {E});
+      order.own = part_of(all, 0, {rows});
+      slots.own = part_of(all, rows, ids.sizes());
+    } else {
+      offsets = packed_output(a[3], "offsets", {E + 1}, at::kInt, ids);
+      counts = packed_output(a[4], "counts", {E}, at::kInt, ids);
+      order = packed_output(a[5], "order", {rows}, at::kInt, ids);
+      slots = packed_output(a[6], "slots", ids.sizes(), at::kInt, ids);
+    }
     const Workspace ws(a[7], a[7] == Py_None ? bsr_expert_sort_workspace_bytes(entries, E) : 0, ids);
     const int rc = released([&] {
       return bsr_expert_sort(pointer(ids), index, entries, E, align, typed<int32_t>(offsets.get()), typed<int32_t>(counts.get()),
@@ -605,8 +623,15 @@ PyObject *distill_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const DistillCall c(a);
     if (!c.types()) return code_result(BSR_ERR_DTYPE);
     const CallStream stream(a[7], c.logits);
-    const Output loss = packed_output(a[4], "loss", {c.z.rows}, at::kFloat, c.logits);
-    const Output stats = packed_output(a[5], "stats", {c.z.rows, 2}, at::kFloat, c.logits);
+    Output loss, stats;
+    if (a[4] == Py_None && a[5] == Py_None) {
+      const at::Tensor all = new_tensor({3 * c.z.rows}, at::kFloat, c.logits);
+      stats.own = part_of(all, 0, {c.z.rows, 2});
+      loss.own = part_of(all, 2 * c.z.rows, {c.z.rows});
+    } else {
+      loss = packed_output(a[4], "loss", {c.z.rows}, at::kFloat, c.logits);
+      stats = packed_output(a[5], "stats", {c.z.rows, 2}, at::kFloat, c.logits);
+    }
     const Workspace ws(a[6], a[6] == Py_None ? c.workspace() : 0, c.logits);
     const int rc = released([&] {
       return bsr_distill_loss(pointer(c.logits), c.code, c.z.rows, c.z.cols, c.z.ld, pointer(c.ids), c.index, pointer(c.teacher),
