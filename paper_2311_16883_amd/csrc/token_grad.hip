@@ -13,7 +13,10 @@ namespace bsr {
 namespace {
 
 constexpr int kAhead = 8;
-constexpr int kGroup = 16;                     // windows whose runs a workgroup of the second kernel joins
+// dY read past the caches, which then hold more of the dE that was just cleared ([65536 x 1024] bf16 into 65536 rows 121 -> 98 us,
+// [30000 x 2048] 111 -> 92; but [65536 x 512] into 1000 rows 36 -> 38).
+constexpr int64_t kStreamBytes = int64_t(96) << 20;
+constexpr int kGroup = 4;                      // windows whose runs a workgroup of the second kernel joins
 constexpr int kLong = 15;                      // windows of a run from which the waves share it
 constexpr int kLeastWindow = 4;
 constexpr int64_t kEnoughWaves = 2048;
@@ -54,7 +57,7 @@ __device__ __forceinline__ void put_sum(const float *sum, bool goes_on_before, b
   }
 }
 
-template <typename T, int VE>
+template <typename T, int VE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void window_sum_kernel(const uint2 *__restrict__ sorted, int64_t n, uint32_t V,
                                                               const T *__restrict__ dY, int64_t D, int64_t lddy, float scale,
                                                               float *__restrict__ dE, int64_t ldde, int accumulate,
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void window_sum_kernel(const uint2 *__res
     for (int u = 0; u < kAhead; ++u) {
       const int i = i0 + u < count ? i0 + u : count - 1;
       const uint32_t pos = __builtin_amdgcn_readlane(e.y, 1 + i);
-      x[u] = R::load(dY + (int64_t)pos * lddy + at);
+      x[u] = load_once<T, VE, STREAM>(dY + (int64_t)pos * lddy + at);
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
@@ -232,17 +235,21 @@ int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const v
   if (rc != BSR_OK || T == 0) return rc;
   const int size = window_size(T, D);
   const int64_t windows = ceil_div(T, (int64_t)size);
-#define BSR_CALL(TY, VE)                                                                                                       \
+  const bool stream = stream_rows(dY, T, D, lddy, dtype, kStreamBytes);
+#define BSR_CALL_(TY, VE, STREAM)                                                                                              \
   const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
-  hipLaunchKernelGGL((window_sum_kernel<TY, VE>), dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))),         \
+  hipLaunchKernelGGL((window_sum_kernel<TY, VE, STREAM>), dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))),         \
                      dim3(kThreads), 0, s, sorted, T, (uint32_t)V, static_cast<const TY *>(dY), D, lddy, scale, dE, ldde,      \
                      accumulate, partial, slices, size)
+#define BSR_CALL(TY, VE) \
+  if (stream) { BSR_CALL_(TY, VE, true); } else { BSR_CALL_(TY, VE, false); }
   if (dtype == BSR_F32) {
-    if (D >= 4) { BSR_CALL(float, 4); } else { BSR_CALL(float, 1); }
+    if (D >= 4) { BSR_CALL(float, 4) } else { BSR_CALL_(float, 1, false); }
   } else {
-    if (D >= 8) { BSR_CALL(uint16_t, 8); } else { BSR_CALL(uint16_t, 1); }
+    if (D >= 8) { BSR_CALL(uint16_t, 8) } else { BSR_CALL_(uint16_t, 1, false); }
   }
 #undef BSR_CALL
+#undef BSR_CALL_
   rc = check_launch();
   if (rc != BSR_OK || windows == 1) return rc;
 #define BSR_JOIN(VE)                                                                                                           \

@@ -125,13 +125,6 @@ __device__ __forceinline__ void load_choices(const int32_t *__restrict__ slots, 
   }
 }
 
-// A vector of a row that only one group of lanes reads: non-temporal (STREAM) or as any other.
-template <typename T, int VE, bool STREAM>
-__device__ __forceinline__ typename RowVec<T, VE>::Raw load_once(const T *p) {
-  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const typename RowVec<T, VE>::Raw *>(p));
-  else return RowVec<T, VE>::load(p);
-}
-
 // out[t] = sum_j weights[t][j] * Ys[slots[t][j]]; KC choices are read together.
 template <typename T, int VE, int KC, bool STREAM>
 __global__ __launch_bounds__(kThreads) void expert_combine_kernel(const T *__restrict__ Ys, int64_t rows, int64_t D, int64_t ldys,
@@ -238,12 +231,6 @@ unsigned padding_blocks(int64_t rows) { return (unsigned)ceil_div(rows, (int64_t
 
 }  // namespace
 
-// Whether the sorted rows are read past the caches: not where they may still be there, or share 128-byte lines.
-bool stream_rows(const void *p, int64_t rows, int64_t D, int64_t ld, int dtype) {
-  const int64_t e = elem_bytes(dtype);
-  return (uintptr_t)p % 128 == 0 && D * e % 128 == 0 && ld * e % 128 == 0 && rows * D * e >= kStreamBytes;
-}
-
 // f32 / bf16 and whole or single-element vectors
 #define BSR_BY_ROW(dtype, D, CALL)                              \
   if ((dtype) == BSR_F32) {                                     \
@@ -287,7 +274,7 @@ int launch_expert_gather(const void *X, int dtype, int64_t T, int64_t D, int64_t
 
 int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, int64_t ldys, const int32_t *slots, int64_t T,
                           int64_t k, const float *weights, void *out, int64_t ldo, hipStream_t s) {
-  const bool stream = stream_rows(Ys, rows, D, ldys, dtype);
+  const bool stream = stream_rows(Ys, rows, D, ldys, dtype, kStreamBytes);
 #define BSR_CALL_(TY, VE, KC, ST)                                                                                             \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
   hipLaunchKernelGGL((expert_combine_kernel<TY, VE, KC, ST>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,                       \
@@ -303,7 +290,7 @@ int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, in
 int launch_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t D, int64_t ldys, const int32_t *slots,
                                const int32_t *order, int64_t T, int64_t k, const float *weights, const void *dOut, int64_t lddo,
                                void *dYs, int64_t lddys, float *dweights, hipStream_t s) {
-  const bool stream = stream_rows(Ys, rows, D, ldys, dtype);
+  const bool stream = stream_rows(Ys, rows, D, ldys, dtype, kStreamBytes);
   const unsigned pad = padding_blocks(rows);
 #define BSR_CALL_(TY, VE, KC, ST)                                                                                             \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \

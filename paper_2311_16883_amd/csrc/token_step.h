@@ -59,6 +59,13 @@ int launch_distill_grad(const DistillArgs &a, const float *stats, const float *d
 int launch_distill_loss_grad(const DistillArgs &a, const float *dloss, float *loss, void *dlogits, int64_t ldd, void *ws,
                              hipStream_t s);
 
+// Whether rows that are read once are read past the caches: not where they may still be there (fewer than `least` bytes of them all),
+// and not where they share 128-byte lines.
+inline bool stream_rows(const void *p, int64_t rows, int64_t D, int64_t ld, int dtype, int64_t least) {
+  const int64_t e = elem_bytes(dtype);
+  return (uintptr_t)p % 128 == 0 && D * e % 128 == 0 && ld * e % 128 == 0 && rows * D * e >= least;
+}
+
 // ---- device helpers ----
 
 // Index i of an int32 or int64 array, as int64.
@@ -110,6 +117,13 @@ __device__ __forceinline__ typename RowVec<T, VE>::Raw pack_row(const float *v) 
   else if constexpr (sizeof(T) == 4)
     return Words4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
   else return Words4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+}
+
+// A vector of a row that is read once: non-temporal (STREAM) or as any other.
+template <typename T, int VE, bool STREAM>
+__device__ __forceinline__ typename RowVec<T, VE>::Raw load_once(const T *p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const typename RowVec<T, VE>::Raw *>(p));
+  else return RowVec<T, VE>::load(p);
 }
 
 // Rows are taken VE elements at a time by the lanes of a group.  The last vector of a row that is no whole number of vectors
