@@ -12,14 +12,15 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;          // vectors that a lane has on their way, per row
-// Sorted rows that are read past the caches, in bytes of them all ([25088 x 2] choices of 1536 bf16, combine and its gradient with
-// the inputs' gradient 123 -> 110 us, [4096 x 8] of 2048 115 -> 93, [8000 x 4] of 1024 f32 37.1 -> 34.7; of rows that share lines,
-// [9947 x 3] of 805 bf16, 12.0 -> 14.5).
-constexpr int64_t kStreamBytes = int64_t(64) << 20;
+// Bytes from which rows pass by the caches.  Read: [25088 x 2] choices of 1536 bf16, weighted return 48.9 -> 42.2 us, [4096 x 8] of 2048,
+// gradients, 116.7 -> 109.5; of rows that share lines, [9947 x 3] of 805, 12.0 -> 14.5.  Written: lookup of [32768 x 1536] bf16 28.9 -> 23.4,
+// [25088 x 4] of 1536 to their experts 87 -> 75.6, return of [30000 x 1] of 1024 23.5 -> 19.4; of rows that share lines, [8000 x 2] of
+// 1537 to their experts, 22.0 -> 23.7.
+constexpr int64_t kStreamRead = int64_t(64) << 20, kStreamWrite = int64_t(32) << 20;
 constexpr int kChoices = 8;        // choices of a token that are handled together
 
 // out[t] = scale * table[tokens[t]]
-template <typename T, int VE, typename I>
+template <typename T, int VE, typename I, bool OUT>
 __global__ __launch_bounds__(kThreads) void embedding_lookup_kernel(const T *__restrict__ table, int64_t V, int64_t D,
                                                                     int64_t ldt, const void *__restrict__ tokens, int64_t rows,
                                                                     float scale, T *__restrict__ out, int64_t ldo, int sh) {
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(kThreads) void embedding_lookup_kernel(const T *__r
       float f[VE];
 #pragma unroll
       for (int q = 0; q < VE; ++q) f[q] = there ? R::elem(x[u], q) * scale : 0.0f;
-      R::store(dst + vector_start(v, VE, D), pack_row<T, VE>(f));
+      store_once<T, VE, OUT>(dst + vector_start(v, VE, D), pack_row<T, VE>(f));
     }
   }
 }
@@ -68,7 +69,7 @@ __device__ __forceinline__ void clear_padding(const int32_t *__restrict__ order,
 }
 
 // Xs[slots[t][j]] = X[t] for all j: every row of X is read once.  The first `pad_blocks` workgroups clear the padding.
-template <typename T, int VE>
+template <typename T, int VE, bool OUT>
 __global__ __launch_bounds__(kThreads) void expert_gather_kernel(const T *__restrict__ X, int64_t tokens, int64_t D, int64_t ldx,
                                                                  const int32_t *__restrict__ slots, int64_t k,
                                                                  const int32_t *__restrict__ order, int64_t rows,
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(kThreads) void expert_gather_kernel(const T *__rest
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         const int64_t v = v0 + (int64_t)u * step;
-        if (v < vecs) R::store(dst + vector_start(v, VE, D), x[u]);
+        if (v < vecs) store_once<T, VE, OUT>(dst + vector_start(v, VE, D), x[u]);
       }
     }
   }
@@ -126,7 +127,7 @@ __device__ __forceinline__ void load_choices(const int32_t *__restrict__ slots, 
 }
 
 // out[t] = sum_j weights[t][j] * Ys[slots[t][j]]; KC choices are read together.
-template <typename T, int VE, int KC, bool STREAM>
+template <typename T, int VE, int KC, bool STREAM, bool OUT>
 __global__ __launch_bounds__(kThreads) void expert_combine_kernel(const T *__restrict__ Ys, int64_t rows, int64_t D, int64_t ldys,
                                                                   const int32_t *__restrict__ slots, int64_t tokens, int64_t k,
                                                                   const float *__restrict__ weights, T *__restrict__ out,
@@ -158,13 +159,13 @@ __global__ __launch_bounds__(kThreads) void expert_combine_kernel(const T *__res
         for (int q = 0; q < VE; ++q) sum[q] = fmaf(c.weight[j], R::elem(y[j], q), sum[q]);
       }
     }
-    R::store(dst + at, pack_row<T, VE>(sum));
+    store_once<T, VE, OUT>(dst + at, pack_row<T, VE>(sum));
   }
 }
 
 // dYs[slots[t][j]] = weights[t][j] * dOut[t], dweights[t][j] = <Ys[slots[t][j]], dOut[t]>: dOut is read once per KC choices, and
 // the products of a row are added up by its lanes in a fixed order.
-template <typename T, int VE, int KC, bool STREAM>
+template <typename T, int VE, int KC, bool STREAM, bool OUT>
 __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
     const T *__restrict__ Ys, int64_t rows, int64_t D, int64_t ldys, const int32_t *__restrict__ slots,
     const int32_t *__restrict__ order, int64_t tokens, int64_t k, const float *__restrict__ weights, const T *__restrict__ dOut,
@@ -207,7 +208,7 @@ __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
         float p[VE];
 #pragma unroll
         for (int q = 0; q < VE; ++q) p[q] = c.weight[j] * gf[q];
-        R::store(dYs + (int64_t)c.slot[j] * lddys + at, pack_row<T, VE>(p));
+        store_once<T, VE, OUT>(dYs + (int64_t)c.slot[j] * lddys + at, pack_row<T, VE>(p));
 #pragma unroll
         for (int q = 0; q < VE; ++q) dot[j] = q >= again ? fmaf(R::elem(y[j], q), gf[q], dot[j]) : dot[j];
       }
@@ -241,46 +242,57 @@ unsigned padding_blocks(int64_t rows) { return (unsigned)ceil_div(rows, (int64_t
 
 int launch_embedding_lookup(const void *table, int dtype, int64_t V, int64_t D, int64_t ldt, const void *tokens, int index_type,
                             int64_t T, float scale, void *out, int64_t ldo, hipStream_t s) {
-#define BSR_CALL_(TY, VE, I)                                                                                                  \
+  const bool write = stream_rows(out, T, D, ldo, dtype, kStreamWrite);
+#define BSR_CALL__(TY, VE, I, OUT)                                                                                            \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((embedding_lookup_kernel<TY, VE, I>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,                      \
+  hipLaunchKernelGGL((embedding_lookup_kernel<TY, VE, I, OUT>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,                 \
                      static_cast<const TY *>(table), V, D, ldt, tokens, T, scale, static_cast<TY *>(out), ldo, sh)
+#define BSR_CALL_(TY, VE, I)                                                \
+  if (write) { BSR_CALL__(TY, VE, I, (VE != 1)); } else { BSR_CALL__(TY, VE, I, false); }
 #define BSR_CALL(TY, VE)                                                    \
-  if (index_type == BSR_I64) { BSR_CALL_(TY, VE, int64_t); } else { BSR_CALL_(TY, VE, int32_t); }
+  if (index_type == BSR_I64) { BSR_CALL_(TY, VE, int64_t) } else { BSR_CALL_(TY, VE, int32_t) }
   BSR_BY_ROW(dtype, D, BSR_CALL)
 #undef BSR_CALL
 #undef BSR_CALL_
+#undef BSR_CALL__
   return check_launch();
 }
 
 int launch_expert_gather(const void *X, int dtype, int64_t T, int64_t D, int64_t ldx, const int32_t *slots, int64_t k,
                          const int32_t *order, int64_t rows, void *Xs, int64_t ldxs, hipStream_t s) {
   const unsigned pad = padding_blocks(rows);
-#define BSR_CALL(TY, VE)                                                                                                      \
+  const bool write = stream_rows(Xs, rows, D, ldxs, dtype, kStreamWrite);
+#define BSR_CALL_(TY, VE, OUT)                                                                                                \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_gather_kernel<TY, VE>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,                      \
+  hipLaunchKernelGGL((expert_gather_kernel<TY, VE, OUT>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,                 \
                      static_cast<const TY *>(X), T, D, ldx, slots, k, order, rows, static_cast<TY *>(Xs), ldxs, sh, pad,       \
                      padding_rows(rows))
+#define BSR_CALL(TY, VE)                                                    \
+  if (write) { BSR_CALL_(TY, VE, (VE != 1)); } else { BSR_CALL_(TY, VE, false); }
   BSR_BY_ROW(dtype, D, BSR_CALL)
 #undef BSR_CALL
+#undef BSR_CALL_
   return check_launch();
 }
 
 // as many choices together as a token has, up to kChoices
-#define BSR_CHOICES(TY, VE, STREAM)                           \
-  if (k <= 2) { BSR_CALL_(TY, VE, 2, STREAM); }               \
-  else if (k <= 4) { BSR_CALL_(TY, VE, 4, STREAM); }          \
-  else { BSR_CALL_(TY, VE, kChoices, STREAM); }
+#define BSR_CHOICES(TY, VE, READ, WRITE)                       \
+  if (k <= 2) { BSR_CALL_(TY, VE, 2, READ, WRITE); }           \
+  else if (k <= 4) { BSR_CALL_(TY, VE, 4, READ, WRITE); }      \
+  else { BSR_CALL_(TY, VE, kChoices, READ, WRITE); }
 
 int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, int64_t ldys, const int32_t *slots, int64_t T,
                           int64_t k, const float *weights, void *out, int64_t ldo, hipStream_t s) {
-  const bool stream = stream_rows(Ys, rows, D, ldys, dtype, kStreamBytes);
-#define BSR_CALL_(TY, VE, KC, ST)                                                                                             \
+  const bool read = stream_rows(Ys, rows, D, ldys, dtype, kStreamRead), write = stream_rows(out, T, D, ldo, dtype, kStreamWrite);
+#define BSR_CALL_(TY, VE, KC, READ, WRITE)                                                                                    \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_combine_kernel<TY, VE, KC, ST>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,                       \
+  hipLaunchKernelGGL((expert_combine_kernel<TY, VE, KC, READ, WRITE>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,          \
                      static_cast<const TY *>(Ys), rows, D, ldys, slots, T, k, weights, static_cast<TY *>(out), ldo, sh)
 #define BSR_CALL(TY, VE)                                                    \
-  if (stream) { BSR_CHOICES(TY, VE, (VE != 1)) } else { BSR_CHOICES(TY, VE, false) }
+  if (read && write) { BSR_CHOICES(TY, VE, (VE != 1), (VE != 1)) }          \
+  else if (read) { BSR_CHOICES(TY, VE, (VE != 1), false) }                  \
+  else if (write) { BSR_CHOICES(TY, VE, false, (VE != 1)) }                 \
+  else { BSR_CHOICES(TY, VE, false, false) }
   BSR_BY_ROW(dtype, D, BSR_CALL)
 #undef BSR_CALL
 #undef BSR_CALL_
@@ -290,15 +302,17 @@ int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, in
 int launch_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t D, int64_t ldys, const int32_t *slots,
                                const int32_t *order, int64_t T, int64_t k, const float *weights, const void *dOut, int64_t lddo,
                                void *dYs, int64_t lddys, float *dweights, hipStream_t s) {
-  const bool stream = stream_rows(Ys, rows, D, ldys, dtype, kStreamBytes);
   const unsigned pad = padding_blocks(rows);
-#define BSR_CALL_(TY, VE, KC, ST)                                                                                             \
+  const bool read = stream_rows(Ys, rows, D, ldys, dtype, kStreamRead), write = stream_rows(dYs, rows, D, lddys, dtype, kStreamWrite);
+#define BSR_CALL_(TY, VE, KC, READ, WRITE)                                                                                    \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_combine_grad_kernel<TY, VE, KC, ST>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,            \
-                     static_cast<const TY *>(Ys), rows, D, ldys, slots, order, T, k, weights, static_cast<const TY *>(dOut),  \
+  hipLaunchKernelGGL((expert_combine_grad_kernel<TY, VE, KC, READ, WRITE>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0,  \
+                     s, static_cast<const TY *>(Ys), rows, D, ldys, slots, order, T, k, weights, static_cast<const TY *>(dOut), \
                      lddo, static_cast<TY *>(dYs), lddys, dweights, sh, pad, padding_rows(rows))
 #define BSR_CALL(TY, VE)                                                    \
-  if (stream) { BSR_CHOICES(TY, VE, (VE != 1)) } else { BSR_CHOICES(TY, VE, false) }
+  if (read && write) { BSR_CHOICES(TY, VE, (VE != 1), (VE != 1)) }          \
+  else if (write) { BSR_CHOICES(TY, VE, false, (VE != 1)) }                 \
+  else { BSR_CHOICES(TY, VE, false, false) }
   BSR_BY_ROW(dtype, D, BSR_CALL)
 #undef BSR_CALL
 #undef BSR_CALL_

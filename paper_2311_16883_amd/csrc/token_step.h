@@ -59,8 +59,8 @@ int launch_distill_grad(const DistillArgs &a, const float *stats, const float *d
 int launch_distill_loss_grad(const DistillArgs &a, const float *dloss, float *loss, void *dlogits, int64_t ldd, void *ws,
                              hipStream_t s);
 
-// Whether rows that are read once are read past the caches: not where they may still be there (fewer than `least` bytes of them all),
-// and not where they share 128-byte lines.
+// Whether rows that are read or written once pass by the caches: not where the caches can hold them (fewer than `least` bytes of them
+// all), and not where they share 128-byte lines.
 inline bool stream_rows(const void *p, int64_t rows, int64_t D, int64_t ld, int dtype, int64_t least) {
   const int64_t e = elem_bytes(dtype);
   return (uintptr_t)p % 128 == 0 && D * e % 128 == 0 && ld * e % 128 == 0 && rows * D * e >= least;
@@ -124,6 +124,13 @@ template <typename T, int VE, bool STREAM>
 __device__ __forceinline__ typename RowVec<T, VE>::Raw load_once(const T *p) {
   if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const typename RowVec<T, VE>::Raw *>(p));
   else return RowVec<T, VE>::load(p);
+}
+
+// ... and one that is written and left.
+template <typename T, int VE, bool STREAM>
+__device__ __forceinline__ void store_once(T *p, const typename RowVec<T, VE>::Raw &v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<typename RowVec<T, VE>::Raw *>(p));
+  else RowVec<T, VE>::store(p, v);
 }
 
 // Rows are taken VE elements at a time by the lanes of a group.  The last vector of a row that is no whole number of vectors
