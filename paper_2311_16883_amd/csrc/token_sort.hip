@@ -50,7 +50,8 @@ __device__ __forceinline__ void clear_part(const ClearJob &c, int64_t part) {
     const int64_t hi = lo + kClearPerBlock < total ? lo + kClearPerBlock : total;
     for (int64_t i = lo + 4 * threadIdx.x; i < hi; i += 4 * (int)blockDim.x) {
       if (i + 4 <= hi) {
-        reinterpret_cast<Any16 *>(c.p + i)->w = Words4{0, 0, 0, 0};
+        if (c.stream) __builtin_nontemporal_store(Words4{0, 0, 0, 0}, reinterpret_cast<Words4 *>(c.p + i));
+        else reinterpret_cast<Any16 *>(c.p + i)->w = Words4{0, 0, 0, 0};
       } else {
         for (int64_t j = i; j < hi; ++j) c.p[j] = 0.0f;
       }
@@ -341,7 +342,7 @@ int launch_expert_sort(const void *ids, int index_type, int64_t n, int64_t E, in
   const Keys k = {ids, n, (uint32_t)E, 0, 0xFFFFFFFFu, (int)E + 1, bit_length((uint32_t)E)};
   const int blocks = blocks_of(n);
   const Places out = {nullptr, offsets, counts, order, slots, rows, align, E};
-  Clearing none(ClearJob{nullptr, 0, 0, 0});
+  Clearing none(ClearJob{nullptr, 0, 0, 0, false});
   return index_type == BSR_I64 ? launch_pass<kFromI64, true>(k, blocks, static_cast<uint32_t *>(ws), out, &none, 0, s)
                                : launch_pass<kFromI32, true>(k, blocks, static_cast<uint32_t *>(ws), out, &none, 0, s);
 }

@@ -31,6 +31,7 @@ size_t token_sort_ws_bytes(int64_t T, int64_t V);
 struct ClearJob {
   float *p;                // null: nothing to clear
   int64_t rows, cols, ld;
+  bool stream;             // past the caches; p is 16-byte aligned and ld == cols then
 };
 int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, const ClearJob &clear, void *ws,
                       const uint2 **sorted, hipStream_t s);
