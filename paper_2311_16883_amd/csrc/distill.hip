@@ -609,17 +609,13 @@ Distill describe(const DistillArgs &d) {
   return a;
 }
 
-size_t parts_bytes(int64_t N, int64_t V) {
-  int64_t chunk;
-  int chunks;
-  row_chunks(N, V, &chunk, &chunks);
-  return align_up((size_t)N * chunks * sizeof(float2), 256);
-}
+// Room for the parts of up to N rows: ceil(kEnoughWorkgroups / n) of each, at most.
+size_t parts_bytes(int64_t N) { return align_up((size_t)(kEnoughWorkgroups + N) * sizeof(float2), 256); }
 
 // Rows from which long ones (more than 8192 vectors) have a workgroup each although they may be fewer than the compute units, against
 // two passes over chunks ([100 x 262144] bf16 36.9 and 37.4 us, [64 x 262144] 34.6 and 23.0, [100 x 131072] 22.5 and 21.6, [32 x
 // 131072] 19.7 and 14.4).  Up to 8192 vectors a single row is as fast so ([1 x 50000] 12.0 and 12.6, [8 x 20000] 9.8 and 12.5).
-constexpr int64_t kEnoughRows = 96;
+constexpr int64_t kEnoughRows = 96, kFewRows = 48, kComputeUnits = 256;
 
 // Rows per launch of a two-dimensional grid, workgroups of a one-dimensional one: the second dimension ends at 65535, the first at
 // 2^32 lanes.
@@ -652,29 +648,13 @@ int run_rows(const Distill &whole, const float *dloss, float *loss, float2 *stat
   return BSR_OK;
 }
 
+// Two passes over chunks of rows.
 template <typename T, bool GRAD>
-int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats, void *dlogits, int64_t ldd, void *ws,
-             hipStream_t s) {
+int run_chunks(const DistillArgs &d, const float *dloss, float *loss, float2 *stats, void *dlogits, int64_t ldd, void *ws,
+               hipStream_t s) {
   const Distill a = describe(d);
-  const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
-  constexpr int MODE = GRAD ? kLoss | kGrad : kLoss;
-  float2 *st = reinterpret_cast<float2 *>(stats);
-  if (vecs <= 8192) {
-    if (vecs <= 512) return run_rows<T, 64, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-    if (vecs <= 1024) return run_rows<T, 128, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-    if (vecs <= 2048) return run_rows<T, 256, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-    if (vecs <= 4096) return run_rows<T, 512, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-    return run_rows<T, 1024, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-  }
-  if constexpr (GRAD) {
-    if (a.N >= kEnoughRows && vecs <= 32768) {
-      if (vecs <= 16384) return run_rows<T, 1024, 16, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-      if (vecs <= 24576) return run_rows<T, 1024, 24, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-      return run_rows<T, 1024, 24, 8, MODE>(a, dloss, loss, st, dlogits, ldd, s);
-    }
-  }
   float2 *parts = static_cast<float2 *>(ws);
-  float *picked = reinterpret_cast<float *>(static_cast<char *>(ws) + parts_bytes(d.N, d.V));
+  float *picked = reinterpret_cast<float *>(static_cast<char *>(ws) + parts_bytes(d.N));
   for (int64_t n = 0; n < d.N; n += kRowsPerLaunch) {
     const Distill b = rows_from(a, n, d.dtype, kRowsPerLaunch);
     hipLaunchKernelGGL((distill_parts_kernel<T>), dim3(a.chunks, (unsigned)b.N), dim3(kThreads), 0, s, b, parts + n * a.chunks,
@@ -682,14 +662,46 @@ int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats
     int rc = check_launch();
     if (rc != BSR_OK) return rc;
     hipLaunchKernelGGL((distill_finish_kernel<T, GRAD>), dim3(GRAD ? a.chunks : 1, (unsigned)b.N), dim3(kThreads),
-                       entries_bytes(a.K), s, b,
-                       parts + n * a.chunks, a.chunks, picked + n * a.K, loss + n,
-                       st != nullptr ? st + n : nullptr, dloss + (dloss != nullptr ? n : 0),
+                       entries_bytes(a.K), s, b, parts + n * a.chunks, a.chunks, picked + n * a.K, loss + n,
+                       stats != nullptr ? stats + n : nullptr, dloss + (dloss != nullptr ? n : 0),
                        dlogits != nullptr ? static_cast<T *>(dlogits) + n * ldd : nullptr, ldd);
     rc = check_launch();
     if (rc != BSR_OK) return rc;
   }
   return BSR_OK;
+}
+
+template <typename T, bool GRAD>
+int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats, void *dlogits, int64_t ldd, void *ws,
+             hipStream_t s) {
+  Distill a = describe(d);
+  const int64_t vecs = a.V / (16 / (int64_t)sizeof(T));
+  constexpr int MODE = GRAD ? kLoss | kGrad : kLoss;
+  float2 *st = reinterpret_cast<float2 *>(stats);
+  if (vecs <= 512) return run_rows<T, 64, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+  if (vecs <= 1024) return run_rows<T, 128, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+  if (vecs <= 2048) return run_rows<T, 256, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+  if (vecs <= 4096) return run_rows<T, 512, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+  if (vecs <= 8192) return run_rows<T, 1024, 8, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+  if constexpr (GRAD) {
+    // Longer rows have a compute unit to themselves: a last round of few of them goes by chunks ([270 x 262144] bf16 97 -> 78 us, [300 x
+    // 131072] 48.6 -> 46.8; but [600 x 250007], 88 in the last round, 173.6 and 173.9, [1100 x 131072], 76, 139.7 and 142.7).
+    const int64_t last = d.N % kComputeUnits, few = d.N < kComputeUnits ? kEnoughRows : kFewRows, whole = last < few ? d.N - last : d.N;
+    if (whole > 0 && vecs <= 32768) {
+      a.N = whole;
+      const int rc = vecs <= 16384   ? run_rows<T, 1024, 16, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s)
+                     : vecs <= 24576 ? run_rows<T, 1024, 24, 0, MODE>(a, dloss, loss, st, dlogits, ldd, s)
+                                     : run_rows<T, 1024, 24, 8, MODE>(a, dloss, loss, st, dlogits, ldd, s);
+      if (rc != BSR_OK || whole == d.N) return rc;
+      DistillArgs rest = d;
+      rest.N = d.N - whole;
+      rest.logits = static_cast<const T *>(d.logits) + whole * d.ldz;
+      rest.ids = static_cast<const char *>(d.ids) + whole * d.K * (d.index_type == BSR_I64 ? 8 : 4);
+      rest.teacher = static_cast<const char *>(d.teacher) + whole * d.K * elem_bytes(d.teacher_dtype);
+      return run_chunks<T, GRAD>(rest, dloss + whole, loss + whole, st, static_cast<T *>(dlogits) + whole * ldd, ldd, ws, s);
+    }
+  }
+  return run_chunks<T, GRAD>(d, dloss, loss, st, dlogits, ldd, ws, s);
 }
 
 template <typename T>
@@ -705,7 +717,8 @@ int run_grad(const DistillArgs &d, const float *stats, const float *dloss, void 
 }  // namespace
 
 size_t distill_ws_bytes(int64_t N, int64_t V, int64_t K) {
-  return parts_bytes(N, V) + align_up((size_t)N * K * sizeof(float), 256);
+  (void)V;
+  return parts_bytes(N) + align_up((size_t)N * K * sizeof(float), 256);
 }
 
 int launch_distill_loss(const DistillArgs &a, float *loss, float *stats, void *ws, hipStream_t s) {

@@ -372,6 +372,22 @@ def test_distill_at_the_edges_of_row_lengths(dtype, vecs):
         assert torch.equal(loss2, loss) and torch.equal(grad2, grad) and around_is_untouched(fresh, pad, offset, 7.0)
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 70001), ("f32", 32771)])
+def test_distill_of_long_rows_in_a_last_round_of_few(dtype, V):
+    """More long rows than compute units: whole rounds a workgroup per row, the last few rows by chunks; in place and apart."""
+    N, K = 256 + 11, 6
+    z, ids, t, dloss = student(N, V, K, 9, dtype, "f32", "i32")
+    ids[260] = -1
+    part = torch.tensor([0, 1, 2, 3, 4, 255, 256, 257, 260, N - 1])
+    loss, grad = B.bsr_distill_loss_grad(z.cuda(), ids.cuda(), t.cuda(), dloss.cuda(), 1.3)
+    want, _, g, el, eg = P.distill(f64(z[part]), ids[part].numpy(), f64(t[part]), float(np.float32(1.3)), f64(dloss[part]))
+    check(loss[part], want, el)
+    check(grad[part], g, eg, dtype)
+    fresh = z.cuda()
+    loss2, grad2 = B.bsr_distill_loss_grad(fresh, ids.cuda(), t.cuda(), dloss.cuda(), 1.3, dlogits=fresh)
+    assert torch.equal(loss2, loss) and torch.equal(grad2, grad)
+
+
 def test_distill_of_more_rows_than_a_grid_dimension():
     N, V, K = 70001, 40, 3
     z, ids, t, dloss = student(N, V, K, 1)
