@@ -1,15 +1,15 @@
 // Distillation from a teacher's top logits: loss, its gradient, or both.
 //
 // With e_j = exp((t_j - max t) / tau) over a row's entries, T = sum e_j, and the row's statistics m = max z, S = sum exp((z - m) / tau):
-//   loss = tau^2 * (sum_j e_j * ((t_j - max t) - (z_j - m)) / (tau T) - log T + log S),
+//   loss = tau * sum_j (e_j / T) * ((t_j - max t) - (z_j - m)) + tau^2 * (log S - log T),
 //   dz_v = g * tau * (exp((z_v - m) / tau) / S - sum over j at v of e_j / T).
-// Exponentials are powers of two of (z - m) * log2(e) / tau: the difference first, so that the type's lowest value as a mask
-// overflows nowhere.  Maxima, sums and differences are binary32; the running maximum and sum of a lane are corrected once per batch
-// of vectors.
+// Exponentials are powers of two of (z - m) * log2(e) / tau.  Maxima, sums and differences are binary32.
 //
-// Bound by memory: N * V logits in, as many gradients out.  A row is cut into chunks where there are few rows, so that every
-// compute unit has some (row_chunks): the first kernel leaves every chunk's (maximum, sum), the second joins those of its row and
-// writes its chunk of the gradient.
+// Bound by memory: N * V logits in, as many gradients out.  A row whose lanes can keep it in registers is read once, whatever is asked
+// for (distill_row_kernel; the longest ones keep a quarter in LDS).  Long rows that are fewer than the compute units are cut into chunks
+// (row_chunks), so that every unit has some: one kernel leaves every chunk's (maximum, sum), the next joins those of its row and writes
+// its chunk of the gradient.  The gradient alone needs no row as a whole and goes by chunks always.
+// [8192 x 50000] bf16: loss 164 us (5.0 TB/s), gradient 299 (5.5), both 309 (5.3; a copy on this GPU 5.1, reading alone 6.2).
 #include "buffer_access.h"
 #include "token_step.h"
 
@@ -87,31 +87,39 @@ __device__ __forceinline__ float group_sum(float v, float *red) {
 // Maximum as the base of differences: 0 for a part without any finite or +inf value.
 __device__ __forceinline__ float base_of(float m) { return m == minus_inf() ? 0.0f : m; }
 
-// The exponents of a row's logits, (z - m) * c, in one multiply-add each: fma(z, c, -mc).  What m * c loses by its rounding is
-// the same for every logit: the true exponent is smaller by `lost`.  Where m * c might overflow (|m| above 1e30 / c: a row of nothing
-// but the type's lowest value, say) logits that differ from m differ by so much that their exponential is 0 with any c that is not
-// tiny, and 2^-30 takes its place: m * 2^-30 is exact.
+// The exponents of a row's logits, (z - m) * c.  Where m * c is no larger than 2^20 (`plain`) each takes one multiply-add,
+// fma(z, c, -mc): what m * c loses by its rounding, a sixteenth at most, is the same for every logit, and the true exponent is smaller
+// by that (`lost`).  Elsewhere -- a row of nothing but the type's lowest value, infinities, a tiny temperature -- the difference comes
+// first, which neither loses nor overflows.
 struct Exponent {
-  float c, mc, lost;
-  __device__ __forceinline__ Exponent(float m, float c_) {
-    c = fabsf(m * c_) <= 1e30f || m != m ? c_ : 0x1p-30f;
-    mc = m * c;
-    lost = fabsf(m) < __builtin_inff() ? fmaf(m, c, -mc) : 0.0f;
+  float m, c, mc, lost;
+  bool plain;
+  __device__ __forceinline__ Exponent(float m_, float c_) : m(m_), c(c_) {
+#pragma clang fp contract(off)
+    mc = m * c;                                // (a product of its own wherever it is added to, or `lost` would not be what it lost)
+    plain = fabsf(mc) <= 0x1p20f;
+    lost = plain ? fmaf(m, c, -mc) : 0.0f;
   }
-  __device__ __forceinline__ float at(float z) const { return fmaf(z, c, -mc); }
+  template <bool PLAIN>
+  __device__ __forceinline__ float at(float z) const { return PLAIN ? fmaf(z, c, -mc) : (z - m) * c; }
 };
 
-// g * exp((z - m) / tau) / S in one multiply-add, exponential and product: the logarithm of S goes into the constant of the exponent,
-// and what that sum's rounding loses into the factor.
+// g * exp((z - m) / tau) / S.  Plain: in one multiply-add, exponential and product; the logarithm of S goes into the constant of the
+// exponent, and what that sum's rounding loses into the factor.
 struct Share {
-  float c, k, g;
+  float m, c, k, log2_s, plain_g, g;
   // log2_s: of the sum of 2^at(z)
-  __device__ __forceinline__ Share(const Exponent &ex, float log2_s, float g_) : c(ex.c) {
+  __device__ __forceinline__ Share(const Exponent &ex, float log2_s_, float g_) : m(ex.m), c(ex.c), log2_s(log2_s_), g(g_) {
+#pragma clang fp contract(off)
     k = ex.mc + log2_s;
     const float hi = k - ex.mc, lo = (ex.mc - (k - hi)) + (log2_s - hi);
-    g = g_ * exp2_of(fabsf(k) < __builtin_inff() ? -lo : 0.0f);
+    plain_g = g * exp2_of(ex.plain ? -lo : 0.0f);
   }
-  __device__ __forceinline__ float at(float z) const { return g * exp2_of(fmaf(z, c, -k)); }
+  template <bool PLAIN>
+  __device__ __forceinline__ float at(float z) const {
+    return PLAIN ? plain_g * exp2_of(fmaf(z, c, -k)) : g * exp2_of(fmaf(z - m, c, -log2_s));
+  }
+  __device__ __forceinline__ float at(float z, bool plain) const { return plain ? at<true>(z) : at<false>(z); }
 };
 
 // Columns [lo, hi) of a row as `head` single ones up to the next 16-byte boundary, whole vectors, and single ones again.
@@ -190,13 +198,14 @@ __device__ __forceinline__ float weigh_entries(const Distill &a, const Entries &
   return sum;
 }
 
-// The lane's sum of e_j * log(e_j / exp((z_j - m) / tau)), in which the teacher's part is the sum of e_j * (t_j - top) = e_j * tau * log(e_j).
+// The lane's sum of tau^2 * q_j * log(e_j / exp((z_j - m) / tau)), in which the teacher's part is tau * log(e_j).
 template <int THREADS>
-__device__ __forceinline__ float cross_entries(const Distill &a, const Entries &en, float m) {
+__device__ __forceinline__ float cross_entries(const Distill &a, const Entries &en, float m, float total) {
+  const float by = 2.0f * (a.tau / total);     // (of halves, whose difference does not overflow)
   float sum = 0.0f;
   for (int j = threadIdx.x; j < a.K; j += THREADS) {
     const float e = en.share[j];
-    if (e != 0.0f) sum = fmaf(e, a.tau * kLn2 * log2f(e) - (en.z[j] - m), sum);
+    if (e != 0.0f) sum = fmaf(e * by, 0.5f * (a.tau * kLn2 * log2f(e)) - (0.5f * en.z[j] - 0.5f * m), sum);
   }
   return sum;
 }
@@ -219,7 +228,7 @@ __device__ __forceinline__ void merge_entries(const Distill &a, const Entries &e
 // wave waits for another.  (A column that several entries share gets all of them, from every one of its entries alike.)
 template <int WAVES, typename T>
 __device__ __forceinline__ void subtract_entries(const Distill &a, const Entries &en, const Cut &cut, int each, float total, float g,
-                                                 int64_t lo, int64_t hi, T *out, const Share &share) {
+                                                 int64_t lo, int64_t hi, T *out, const Share &share, bool plain) {
   constexpr int VE = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float by = 1.0f / total;
@@ -231,12 +240,12 @@ __device__ __forceinline__ void subtract_entries(const Distill &a, const Entries
     const uint32_t i = (uint32_t)(v - lo - cut.head);
     const bool single = v - lo < cut.head || i >= (uint32_t)(cut.vecs * VE);
     if ((single ? 0u : i / (VE * 64u * (uint32_t)each) % WAVES) != (uint32_t)wave) continue;
-    out[v] = from_float<T>(share.at(en.z[j]) - g * (en.q[j] * by));
+    out[v] = from_float<T>(share.at(en.z[j], plain) - g * (en.q[j] * by));
   }
 }
 
 __device__ __forceinline__ float loss_of(const Distill &a, float cross, float total, float log_s) {
-  return a.tau * a.tau * (cross / (a.tau * total) - logf(total) + log_s);
+  return fmaf(a.tau * a.tau, log_s - logf(total), cross);
 }
 
 // Cache policy of buffer accesses: non-temporal.
@@ -329,6 +338,9 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
       copy_to_lds(buffer(row, R_ + l), &rest[l * THREADS + (t - lane)], offset(R_ + l));
     }
   }
+  // vector i of the wave from memory once more, for the rare rows whose exponents take more than one operation: a second set of loops
+  // over the registers would cost the others registers
+  auto again = [&](int i) { return *reinterpret_cast<const Words4 *>(row + lo + cut.head + (int64_t)(first + i) * VE); };
   // vector R_ + l of the lane, -inf behind the row
   auto from_lds = [&](int l) {
     Words4 w = rest[l * THREADS + t];
@@ -404,24 +416,33 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   if constexpr (MODE == kGrad) {
     log2_s = fmaf(stats[n].y, kLog2E, ex.lost);
   } else {
-    float acc[4] = {exp2_of(ex.at(zs)), 0.0f, 0.0f, 0.0f};
+    float acc[4] = {exp2_of(ex.plain ? ex.at<true>(zs) : ex.at<false>(zs)), 0.0f, 0.0f, 0.0f};
+    if (ex.plain) {
 #pragma unroll
-    for (int r = 0; r < R_; ++r) {
-      if (r * 64 >= left) continue;
-      asm volatile("" : "+v"(x[r]));
+      for (int r = 0; r < R_; ++r) {
+        if (r * 64 >= left) continue;
+        asm volatile("" : "+v"(x[r]));
 #pragma unroll
-      for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(x[r], q)));
-      asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
-    }
-    if constexpr (L > 0) {
+        for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at<true>(R::elem(x[r], q)));
+        asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
+      }
+      if constexpr (L > 0) {
 #pragma unroll 1
-      for (int l = 0; l < L && (R_ + l) * 64 < left; ++l) {
-        const Words4 w = from_lds(l);
+        for (int l = 0; l < L && (R_ + l) * 64 < left; ++l) {
+          const Words4 w = from_lds(l);
 #pragma unroll
-        for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at(R::elem(w, q)));
+          for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at<true>(R::elem(w, q)));
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int i = lane; i < left; i += 64) {
+        const Words4 w = again(i);
+#pragma unroll
+        for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at<false>(R::elem(w, q)));
       }
     }
-    const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m), red[3]);
+    const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m, total), red[3]);
     const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[4]);
     log2_s = m == minus_inf() ? __builtin_nanf("") : log2f(s);
     if (t == 0) {
@@ -433,8 +454,20 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
   if constexpr (MODE & kGrad) {
     const float g = dloss[n] * a.tau;
     const Share share(ex, log2_s, g);
-    put([&](float z) { return share.at(z); });
-    subtract_entries<WAVES>(a, en, cut, each, total, g, lo, hi, out, share);
+    if (ex.plain) {
+      put([&](float z) { return share.at<true>(z); });
+    } else {
+#pragma unroll 1
+      for (int i = lane; i < left; i += 64) {
+        const Words4 w = again(i);
+        float v[VE];
+#pragma unroll
+        for (int q = 0; q < VE; ++q) v[q] = share.at<false>(R::elem(w, q));
+        R::store(out + lo + cut.head + (int64_t)(first + i) * VE, pack_row<T, VE>(v));
+      }
+      if (one) out[single] = from_float<T>(share.at<false>(zs));
+    }
+    subtract_entries<WAVES>(a, en, cut, each, total, g, lo, hi, out, share, ex.plain);
   }
 }
 
@@ -542,7 +575,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
   const bool none = top == minus_inf();
   const float total = group_sum<kWaves>(weigh_entries<kThreads>(a, en, top), red[3]);
   if (blockIdx.x == 0) {
-    const float x = group_sum<kWaves>(cross_entries<kThreads>(a, en, m), red[4]);
+    const float x = group_sum<kWaves>(cross_entries<kThreads>(a, en, m, total), red[4]);
     if (t == 0) {
       loss[n] = none ? 0.0f : loss_of(a, x, total, log_s);
       if (stats != nullptr) stats[n] = float2{m, log_s};
@@ -584,9 +617,10 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
       return;
     }
     merge_entries<kThreads>(a, en, lo, hi);
-    run([&](float z) { return share.at(z); });
+    if (ex.plain) run([&](float z) { return share.at<true>(z); });
+    else run([&](float z) { return share.at<false>(z); });
     __syncthreads();
-    subtract_entries<kWaves>(a, en, cut, 1, total, g, lo, hi, out, share);
+    subtract_entries<kWaves>(a, en, cut, 1, total, g, lo, hi, out, share, ex.plain);
   }
 }
 

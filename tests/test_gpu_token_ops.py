@@ -429,6 +429,30 @@ def test_distill_rows_without_a_distribution_or_entries(dtype, V):
             check(l[torch.tensor([4, 6, 7])], want[[0, 2, 3]], el[[0, 2, 3]])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(6, 700), (6, 20003), (5, 131075), (130, 70001)])
+@pytest.mark.parametrize("scale,tau", [(1e6, 1.0), (3e37, 0.5), (5.0, 1e-4), (1.0, 2.0 ** -60), (1.0, 2.0 ** 60), (3e30, 1e-10),
+                                       (2e4, 0.05), (1e-30, 1.0)])
+def test_distill_of_far_logits_and_temperatures(dtype, N, V, scale, tau):
+    """Exponents from far below the spacing of the logits to far above the range of the type."""
+    z, ids, t, dloss = student(N, V, 5, N + V, masks=False)
+    z, t = (z * scale).to(DT[dtype]), (t * scale).to(DT[dtype])
+    z[0, 3] = z[0, 11] = z[0].max()                                             # two logits on top
+    part = torch.tensor([0, 1, 2, 3, N - 1])
+    tau32 = float(np.float32(tau))
+    want, _, g, el, eg = P.distill(f64(z[part]), ids[part].numpy(), f64(t[part]), tau32, f64(dloss[part]))
+    loss, grad = B.bsr_distill_loss_grad(z.cuda(), ids.cuda(), t.cuda(), dloss.cuda(), tau)
+    loss1, stats = B.bsr_distill_loss(z.cuda(), ids.cuda(), t.cuda(), tau)
+    grad1 = B.bsr_distill_grad(z.cuda(), ids.cuda(), t.cuda(), stats, dloss.cuda(), tau)
+    for l, d in ((loss, grad), (loss1, grad1)):
+        finite = np.abs(want) < 3e38                                            # (beyond that binary32 has no loss)
+        check(l[part][torch.from_numpy(finite)], want[finite], el[finite])
+        check(d[part], g, eg, dtype)
+    fresh = z.cuda()
+    loss2, grad2 = B.bsr_distill_loss_grad(fresh, ids.cuda(), t.cuda(), dloss.cuda(), tau, dlogits=fresh)
+    assert torch.equal(grad2, grad)
+
+
 def test_distill_gradient_against_differences():
     """The loss along a random direction: central differences of the kernel's own loss against its gradient."""
     N, V, K, tau, h = 6, 500, 9, 1.5, 2.0 ** -6
