@@ -10,6 +10,8 @@
 // (row_chunks), so that every unit has some: one kernel leaves every chunk's (maximum, sum), the next joins those of its row and writes
 // its chunk of the gradient.  The gradient alone needs no row as a whole and goes by chunks always.
 // [8192 x 50000] bf16: loss 164 us (5.0 TB/s), gradient 299 (5.5), both 309 (5.3; a copy on this GPU 5.1, reading alone 6.2).
+#include <type_traits>
+
 #include "buffer_access.h"
 #include "token_step.h"
 
@@ -119,7 +121,6 @@ struct Share {
   __device__ __forceinline__ float at(float z) const {
     return PLAIN ? plain_g * exp2_of(fmaf(z, c, -k)) : g * exp2_of(fmaf(z - m, c, -log2_s));
   }
-  __device__ __forceinline__ float at(float z, bool plain) const { return plain ? at<true>(z) : at<false>(z); }
 };
 
 // Columns [lo, hi) of a row as `head` single ones up to the next 16-byte boundary, whole vectors, and single ones again.
@@ -226,9 +227,9 @@ __device__ __forceinline__ void merge_entries(const Distill &a, const Entries &e
 // Teacher's shares subtracted from the gradient at the entries' columns in [lo, hi): every wave writes those columns once more
 // whose vectors it has written itself (vector i of the cut by wave i / (64 * each) mod WAVES, single columns by the first), so that no
 // wave waits for another.  (A column that several entries share gets all of them, from every one of its entries alike.)
-template <int WAVES, typename T>
+template <int WAVES, bool PLAIN, typename T>
 __device__ __forceinline__ void subtract_entries(const Distill &a, const Entries &en, const Cut &cut, int each, float total, float g,
-                                                 int64_t lo, int64_t hi, T *out, const Share &share, bool plain) {
+                                                 int64_t lo, int64_t hi, T *out, const Share &share) {
   constexpr int VE = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float by = 1.0f / total;
@@ -240,7 +241,7 @@ __device__ __forceinline__ void subtract_entries(const Distill &a, const Entries
     const uint32_t i = (uint32_t)(v - lo - cut.head);
     const bool single = v - lo < cut.head || i >= (uint32_t)(cut.vecs * VE);
     if ((single ? 0u : i / (VE * 64u * (uint32_t)each) % WAVES) != (uint32_t)wave) continue;
-    out[v] = from_float<T>(share.at(en.z[j], plain) - g * (en.q[j] * by));
+    out[v] = from_float<T>(share.template at<PLAIN>(en.z[j]) - g * (en.q[j] * by));
   }
 }
 
@@ -412,63 +413,66 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     put([](float) { return 0.0f; });
     return;
   }
-  float log2_s;                                // of the sum of 2^(the exponents)
-  if constexpr (MODE == kGrad) {
-    log2_s = fmaf(stats[n].y, kLog2E, ex.lost);
-  } else {
-    float acc[4] = {exp2_of(ex.plain ? ex.at<true>(zs) : ex.at<false>(zs)), 0.0f, 0.0f, 0.0f};
-    if (ex.plain) {
+  // The rest, for rows of either kind of exponents as a whole: a branch inside would have the compiler copy the vectors where its ways
+  // meet.
+  auto finish = [&](auto plain) {
+    constexpr bool PLAIN = decltype(plain)::value;
+    float log2_s;                              // of the sum of 2^(the exponents)
+    if constexpr (MODE == kGrad) {
+      log2_s = fmaf(stats[n].y, kLog2E, ex.lost);
+    } else {
+      float acc[4] = {exp2_of(ex.template at<PLAIN>(zs)), 0.0f, 0.0f, 0.0f};
+      auto add = [&](const Words4 &w) {
 #pragma unroll
-      for (int r = 0; r < R_; ++r) {
-        if (r * 64 >= left) continue;
-        asm volatile("" : "+v"(x[r]));
+        for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.template at<PLAIN>(R::elem(w, q)));
+      };
+      if constexpr (PLAIN) {
 #pragma unroll
-        for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at<true>(R::elem(x[r], q)));
-        asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
-      }
-      if constexpr (L > 0) {
-#pragma unroll 1
-        for (int l = 0; l < L && (R_ + l) * 64 < left; ++l) {
-          const Words4 w = from_lds(l);
-#pragma unroll
-          for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at<true>(R::elem(w, q)));
+        for (int r = 0; r < R_; ++r) {
+          if (r * 64 >= left) continue;
+          asm volatile("" : "+v"(x[r]));
+          add(x[r]);
+          asm volatile("" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
         }
-      }
-    } else {
+        if constexpr (L > 0) {
 #pragma unroll 1
-      for (int i = lane; i < left; i += 64) {
-        const Words4 w = again(i);
-#pragma unroll
-        for (int q = 0; q < VE; ++q) acc[q & 3] += exp2_of(ex.at<false>(R::elem(w, q)));
-      }
-    }
-    const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m, total), red[3]);
-    const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[4]);
-    log2_s = m == minus_inf() ? __builtin_nanf("") : log2f(s);
-    if (t == 0) {
-      const float log_s = (log2_s - ex.lost) * kLn2;
-      loss[n] = none ? 0.0f : loss_of(a, cross, total, log_s);
-      if constexpr (MODE == kLoss) stats[n] = float2{m, log_s};
-    }
-  }
-  if constexpr (MODE & kGrad) {
-    const float g = dloss[n] * a.tau;
-    const Share share(ex, log2_s, g);
-    if (ex.plain) {
-      put([&](float z) { return share.at<true>(z); });
-    } else {
+          for (int l = 0; l < L && (R_ + l) * 64 < left; ++l) add(from_lds(l));
+        }
+      } else {
 #pragma unroll 1
-      for (int i = lane; i < left; i += 64) {
-        const Words4 w = again(i);
-        float v[VE];
-#pragma unroll
-        for (int q = 0; q < VE; ++q) v[q] = share.at<false>(R::elem(w, q));
-        R::store(out + lo + cut.head + (int64_t)(first + i) * VE, pack_row<T, VE>(v));
+        for (int i = lane; i < left; i += 64) add(again(i));
       }
-      if (one) out[single] = from_float<T>(share.at<false>(zs));
+      const float cross = group_sum<WAVES>(cross_entries<THREADS>(a, en, m, total), red[3]);
+      const float s = group_sum<WAVES>((acc[0] + acc[1]) + (acc[2] + acc[3]), red[4]);
+      log2_s = m == minus_inf() ? __builtin_nanf("") : log2f(s);
+      if (t == 0) {
+        const float log_s = (log2_s - ex.lost) * kLn2;
+        loss[n] = none ? 0.0f : loss_of(a, cross, total, log_s);
+        if constexpr (MODE == kLoss) stats[n] = float2{m, log_s};
+      }
     }
-    subtract_entries<WAVES>(a, en, cut, each, total, g, lo, hi, out, share, ex.plain);
-  }
+    if constexpr (MODE & kGrad) {
+      const float g = dloss[n] * a.tau;
+      const Share share(ex, log2_s, g);
+      auto gradient = [&](float z) { return share.template at<PLAIN>(z); };
+      if constexpr (PLAIN) {
+        put(gradient);
+      } else {
+#pragma unroll 1
+        for (int i = lane; i < left; i += 64) {
+          const Words4 w = again(i);
+          float v[VE];
+#pragma unroll
+          for (int q = 0; q < VE; ++q) v[q] = gradient(R::elem(w, q));
+          R::store(out + lo + cut.head + (int64_t)(first + i) * VE, pack_row<T, VE>(v));
+        }
+        if (one) out[single] = from_float<T>(gradient(zs));
+      }
+      subtract_entries<WAVES, PLAIN>(a, en, cut, each, total, g, lo, hi, out, share);
+    }
+  };
+  if (ex.plain) finish(std::true_type());
+  else finish(std::false_type());
 }
 
 // ---- a row in chunks: two passes over the logits ----
@@ -617,10 +621,14 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
       return;
     }
     merge_entries<kThreads>(a, en, lo, hi);
-    if (ex.plain) run([&](float z) { return share.at<true>(z); });
-    else run([&](float z) { return share.at<false>(z); });
-    __syncthreads();
-    subtract_entries<kWaves>(a, en, cut, 1, total, g, lo, hi, out, share, ex.plain);
+    auto both = [&](auto plain) {
+      constexpr bool PLAIN = decltype(plain)::value;
+      run([&](float z) { return share.template at<PLAIN>(z); });
+      __syncthreads();
+      subtract_entries<kWaves, PLAIN>(a, en, cut, 1, total, g, lo, hi, out, share);
+    };
+    if (ex.plain) both(std::true_type());
+    else both(std::false_type());
   }
 }
 
