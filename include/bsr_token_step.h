@@ -137,6 +137,7 @@ int bsr_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t D,
  * (its statistics are still those of its logits).  A row with a NaN or +inf logit or with
  * nothing but -inf has no distribution: its L, loss and gradient are NaN.  Logits of -inf
  * or of the type's lowest value otherwise count as p = 0 (loss +inf where q is not 0).
+ * A teacher logit of NaN or +inf makes its row's loss and the gradient at its entries NaN.
  * K = 1 with any finite teacher logit is the cross entropy of a class.
  * K <= 1024 (BSR_ERR_LIMIT beyond).
  * bsr_distill_loss is the forward pass, bsr_distill_grad the backward pass from its stats;

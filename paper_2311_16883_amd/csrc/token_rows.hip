@@ -19,13 +19,16 @@ constexpr int kAhead = 4;          // vectors that a lane has on their way, per 
 constexpr int64_t kStreamRead = int64_t(64) << 20, kStreamWrite = int64_t(32) << 20;
 constexpr int kChoices = 8;        // choices of a token that are handled together
 
+// The workgroup's number in a grid of two dimensions (the lanes of the first are counted in 32 bits).
+__device__ __forceinline__ int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // out[t] = scale * table[tokens[t]]
 template <typename T, int VE, typename I, bool OUT>
 __global__ __launch_bounds__(kThreads) void embedding_lookup_kernel(const T *__restrict__ table, int64_t V, int64_t D,
                                                                     int64_t ldt, const void *__restrict__ tokens, int64_t rows,
                                                                     float scale, T *__restrict__ out, int64_t ldo, int sh) {
   typedef RowVec<T, VE> R;
-  const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> sh;
+  const int64_t row = (block_number() * kThreads + threadIdx.x) >> sh;
   if (row >= rows) return;
   const int li = threadIdx.x & ((1 << sh) - 1), step = 1 << sh;
   const int64_t tok = load_index<I>(tokens, row);
@@ -73,15 +76,16 @@ template <typename T, int VE, bool OUT>
 __global__ __launch_bounds__(kThreads) void expert_gather_kernel(const T *__restrict__ X, int64_t tokens, int64_t D, int64_t ldx,
                                                                  const int32_t *__restrict__ slots, int64_t k,
                                                                  const int32_t *__restrict__ order, int64_t rows,
-                                                                 T *__restrict__ Xs, int64_t ldxs, int sh, unsigned pad_blocks,
+                                                                 T *__restrict__ Xs, int64_t ldxs, int sh, int64_t pad_blocks,
     int pad_rows) {
   typedef RowVec<T, VE> R;
   const int t = threadIdx.x;
-  if (blockIdx.x < pad_blocks) {
-    clear_padding<T, VE>(order, rows, ((int64_t)blockIdx.x * (kThreads / 64) + (t >> 6)) * pad_rows, pad_rows, Xs, ldxs, D, t & 63);
+  const int64_t block = block_number();
+  if (block < pad_blocks) {
+    clear_padding<T, VE>(order, rows, (block * (kThreads / 64) + (t >> 6)) * pad_rows, pad_rows, Xs, ldxs, D, t & 63);
     return;
   }
-  const int64_t row = ((int64_t)(blockIdx.x - pad_blocks) * kThreads + t) >> sh;
+  const int64_t row = ((block - pad_blocks) * kThreads + t) >> sh;
   if (row >= tokens) return;
   const int li = t & ((1 << sh) - 1), step = 1 << sh;
   const T *src = X + row * ldx;
@@ -133,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void expert_combine_kernel(const T *__res
                                                                   const float *__restrict__ weights, T *__restrict__ out,
                                                                   int64_t ldo, int sh) {
   typedef RowVec<T, VE> R;
-  const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> sh;
+  const int64_t row = (block_number() * kThreads + threadIdx.x) >> sh;
   if (row >= tokens) return;
   const int li = threadIdx.x & ((1 << sh) - 1), step = 1 << sh;
   T *dst = out + row * ldo;
@@ -169,15 +173,16 @@ template <typename T, int VE, int KC, bool STREAM, bool OUT>
 __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
     const T *__restrict__ Ys, int64_t rows, int64_t D, int64_t ldys, const int32_t *__restrict__ slots,
     const int32_t *__restrict__ order, int64_t tokens, int64_t k, const float *__restrict__ weights, const T *__restrict__ dOut,
-    int64_t lddo, T *__restrict__ dYs, int64_t lddys, float *__restrict__ dweights, int sh, unsigned pad_blocks,
+    int64_t lddo, T *__restrict__ dYs, int64_t lddys, float *__restrict__ dweights, int sh, int64_t pad_blocks,
     int pad_rows) {
   typedef RowVec<T, VE> R;
   const int t = threadIdx.x;
-  if (blockIdx.x < pad_blocks) {
-    clear_padding<T, VE>(order, rows, ((int64_t)blockIdx.x * (kThreads / 64) + (t >> 6)) * pad_rows, pad_rows, dYs, lddys, D, t & 63);
+  const int64_t block = block_number();
+  if (block < pad_blocks) {
+    clear_padding<T, VE>(order, rows, (block * (kThreads / 64) + (t >> 6)) * pad_rows, pad_rows, dYs, lddys, D, t & 63);
     return;
   }
-  const int64_t row = ((int64_t)(blockIdx.x - pad_blocks) * kThreads + t) >> sh;
+  const int64_t row = ((block - pad_blocks) * kThreads + t) >> sh;
   if (row >= tokens) return;
   const int li = t & ((1 << sh) - 1), step = 1 << sh;
   const T *src = dOut + row * lddo;
@@ -224,11 +229,16 @@ __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
 // Lanes that share a row (as a power of two): 64 for rows of 64 vectors or more, fewer for short ones, down to 16.
 int row_lanes(int64_t vecs) { return vecs > 32 ? 6 : vecs > 16 ? 5 : 4; }
 
-unsigned row_blocks(int64_t rows, int sh) { return (unsigned)ceil_div(rows << sh, (int64_t)kThreads); }
+int64_t row_blocks(int64_t rows, int sh) { return ceil_div(rows << sh, (int64_t)kThreads); }
+
+dim3 grid_of(int64_t blocks) {
+  const int64_t x = blocks < 1 ? 1 : blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22;
+  return dim3((unsigned)x, (unsigned)ceil_div(blocks, x));
+}
 
 // Rows of the sorted matrix that one wave looks over for padding, one after the other: few where there are few rows.
 int padding_rows(int64_t rows) { return rows < 4096 ? 1 : rows < 32768 ? 4 : 16; }
-unsigned padding_blocks(int64_t rows) { return (unsigned)ceil_div(rows, (int64_t)padding_rows(rows) * (kThreads / 64)); }
+int64_t padding_blocks(int64_t rows) { return ceil_div(rows, (int64_t)padding_rows(rows) * (kThreads / 64)); }
 
 }  // namespace
 
@@ -245,7 +255,7 @@ int launch_embedding_lookup(const void *table, int dtype, int64_t V, int64_t D, 
   const bool write = stream_rows(out, T, D, ldo, dtype, kStreamWrite);
 #define BSR_CALL__(TY, VE, I, OUT)                                                                                            \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((embedding_lookup_kernel<TY, VE, I, OUT>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,                 \
+  hipLaunchKernelGGL((embedding_lookup_kernel<TY, VE, I, OUT>), grid_of(row_blocks(T, sh)), dim3(kThreads), 0, s,                 \
                      static_cast<const TY *>(table), V, D, ldt, tokens, T, scale, static_cast<TY *>(out), ldo, sh)
 #define BSR_CALL_(TY, VE, I)                                                \
   if (write) { BSR_CALL__(TY, VE, I, (VE != 1)); } else { BSR_CALL__(TY, VE, I, false); }
@@ -260,11 +270,11 @@ int launch_embedding_lookup(const void *table, int dtype, int64_t V, int64_t D, 
 
 int launch_expert_gather(const void *X, int dtype, int64_t T, int64_t D, int64_t ldx, const int32_t *slots, int64_t k,
                          const int32_t *order, int64_t rows, void *Xs, int64_t ldxs, hipStream_t s) {
-  const unsigned pad = padding_blocks(rows);
+  const int64_t pad = padding_blocks(rows);
   const bool write = stream_rows(Xs, rows, D, ldxs, dtype, kStreamWrite);
 #define BSR_CALL_(TY, VE, OUT)                                                                                                \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_gather_kernel<TY, VE, OUT>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,                 \
+  hipLaunchKernelGGL((expert_gather_kernel<TY, VE, OUT>), grid_of(pad + row_blocks(T, sh)), dim3(kThreads), 0, s,                 \
                      static_cast<const TY *>(X), T, D, ldx, slots, k, order, rows, static_cast<TY *>(Xs), ldxs, sh, pad,       \
                      padding_rows(rows))
 #define BSR_CALL(TY, VE)                                                    \
@@ -286,7 +296,7 @@ int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, in
   const bool read = stream_rows(Ys, rows, D, ldys, dtype, kStreamRead), write = stream_rows(out, T, D, ldo, dtype, kStreamWrite);
 #define BSR_CALL_(TY, VE, KC, READ, WRITE)                                                                                    \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_combine_kernel<TY, VE, KC, READ, WRITE>), dim3(row_blocks(T, sh)), dim3(kThreads), 0, s,          \
+  hipLaunchKernelGGL((expert_combine_kernel<TY, VE, KC, READ, WRITE>), grid_of(row_blocks(T, sh)), dim3(kThreads), 0, s,          \
                      static_cast<const TY *>(Ys), rows, D, ldys, slots, T, k, weights, static_cast<TY *>(out), ldo, sh)
 #define BSR_CALL(TY, VE)                                                    \
   if (read && write) { BSR_CHOICES(TY, VE, (VE != 1), (VE != 1)) }          \
@@ -302,11 +312,11 @@ int launch_expert_combine(const void *Ys, int dtype, int64_t rows, int64_t D, in
 int launch_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t D, int64_t ldys, const int32_t *slots,
                                const int32_t *order, int64_t T, int64_t k, const float *weights, const void *dOut, int64_t lddo,
                                void *dYs, int64_t lddys, float *dweights, hipStream_t s) {
-  const unsigned pad = padding_blocks(rows);
+  const int64_t pad = padding_blocks(rows);
   const bool read = stream_rows(Ys, rows, D, ldys, dtype, kStreamRead), write = stream_rows(dYs, rows, D, lddys, dtype, kStreamWrite);
 #define BSR_CALL_(TY, VE, KC, READ, WRITE)                                                                                    \
   const int sh = row_lanes(ceil_div(D, (int64_t)VE));                                                                         \
-  hipLaunchKernelGGL((expert_combine_grad_kernel<TY, VE, KC, READ, WRITE>), dim3(pad + row_blocks(T, sh)), dim3(kThreads), 0,  \
+  hipLaunchKernelGGL((expert_combine_grad_kernel<TY, VE, KC, READ, WRITE>), grid_of(pad + row_blocks(T, sh)), dim3(kThreads), 0,  \
                      s, static_cast<const TY *>(Ys), rows, D, ldys, slots, order, T, k, weights, static_cast<const TY *>(dOut), \
                      lddo, static_cast<TY *>(dYs), lddys, dweights, sh, pad, padding_rows(rows))
 #define BSR_CALL(TY, VE)                                                    \

@@ -75,6 +75,26 @@ def test_lookup(dtype, index, T, V, D, pad, offset):
     check(got, P.lookup(f64(table), tokens.numpy(), float(np.float32(scale))), P.U * np.abs(f64(want)), dtype)
 
 
+def test_more_rows_than_a_launch_has_lanes_for():
+    """2^26 tokens and more, at 16 lanes a row: more than 2^30 lanes, and 2^32 for rows of 64 lanes."""
+    T = (1 << 26) + 5
+    tokens = torch.arange(T, dtype=torch.int32, device="cuda") % 1000
+    table = torch.arange(1000, dtype=torch.float32, device="cuda")[:, None].expand(1000, 2).bfloat16().contiguous()
+    out = B.bsr_embedding_lookup(table, tokens)
+    for part in (slice(0, 3000), slice((1 << 26) - 2000, T)):
+        assert torch.equal(out[part], table[tokens[part].long()])
+    assert torch.equal(out[:, 0].float().sum(dtype=torch.float64), table[:, 0].double()[tokens.long()].sum())
+    del out, tokens
+    T = (1 << 26) + 5                                    # 33 vectors of 16 bytes a row would be 70 GB: one row, read by every token
+    slots = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    row = torch.arange(264, dtype=torch.float32, device="cuda").bfloat16()[None]
+    got = B.bsr_expert_combine(row, slots)
+    for part in (slice(0, 100), slice((1 << 26) - 50, T)):
+        assert torch.equal(got[part], row.expand(got[part].shape[0], -1))
+    del got, slots
+    torch.cuda.empty_cache()
+
+
 def test_lookup_of_special_values_and_far_tokens():
     table = torch.tensor([[float("nan"), 1.0], [float("inf"), -0.0], [3.0, 4.0]]).cuda()
     tokens = torch.tensor([2, 2 ** 40, -(2 ** 40), 1, 2 ** 32 + 1, 3]).cuda()        # low words 0 and 1 must not be taken
