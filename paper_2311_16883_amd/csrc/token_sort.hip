@@ -20,8 +20,13 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kMaxBins = 1025;                 // kMaxExperts and the dropped entries; digits of up to 10 bits
 constexpr int kDigitBits = 10;
 constexpr int kFewSteps = 4, kManySteps = 16;  // times 64 entries that a wave takes
-constexpr int kManyBlocks = 256;               // workgroups from which each takes kManySteps: each reads the counts of all
-constexpr int64_t kClearPerBlock = 32768;      // elements that a workgroup clears
+// Workgroups from which each takes kManySteps, as each reads the counts of all ([1048576 x 4] choices of 256 experts, 32 columns, 216 us,
+// 444 with kFewSteps; but [25088 x 4] of 64 17 with kFewSteps and 27.5 with kManySteps).
+constexpr int kManyBlocks = 256;
+// Elements that a workgroup clears, or more where that takes more than kClearBlocks workgroups.  Past the caches and beside a sort in
+// several launches, one store per lane: [65536 x 1024] bf16 into 65536 rows 98.8 us with kClear, 91.9 so, [30000 x 2048] into 100000
+// 198 and 180; but beside the large workgroup of one launch, [3000 x 1024] into 16384, 22.2 and 24.8.
+constexpr int64_t kClear = 32768, kClearBlocks = int64_t(1) << 21;
 
 enum Source { kFromI32, kFromI64, kFromPairs };
 
@@ -46,8 +51,8 @@ __device__ __forceinline__ uint32_t digit_of(const Keys &k, uint32_t key) { retu
 // +0.0 over one workgroup's part of a matrix.
 __device__ __forceinline__ void clear_part(const ClearJob &c, int64_t part) {
   if (c.ld == c.cols || c.rows == 1) {
-    const int64_t total = c.rows * c.cols, lo = part * kClearPerBlock;
-    const int64_t hi = lo + kClearPerBlock < total ? lo + kClearPerBlock : total;
+    const int64_t total = c.rows * c.cols, lo = part * c.per;
+    const int64_t hi = lo + c.per < total ? lo + c.per : total;
     for (int64_t i = lo + 4 * threadIdx.x; i < hi; i += 4 * (int)blockDim.x) {
       if (i + 4 <= hi) {
         if (c.stream) __builtin_nontemporal_store(Words4{0, 0, 0, 0}, reinterpret_cast<Words4 *>(c.p + i));
@@ -58,7 +63,7 @@ __device__ __forceinline__ void clear_part(const ClearJob &c, int64_t part) {
     }
     return;
   }
-  const int64_t per = kClearPerBlock / c.cols > 0 ? kClearPerBlock / c.cols : 1;
+  const int64_t per = c.per / c.cols > 0 ? c.per / c.cols : 1;
   for (int64_t r = part * per; r < (part + 1) * per && r < c.rows; ++r)
     for (int64_t j = threadIdx.x; j < c.cols; j += blockDim.x) c.p[r * c.ld + j] = 0.0f;
 }
@@ -219,7 +224,8 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Keys k, const uint32_t 
   }
 }
 
-// Up to kOneSort positions sorted by all digits of their token in one launch, by one workgroup; the others clear.
+// Up to kOneSort positions sorted by all digits of their token in one launch, by one workgroup; the others clear.  ([3000 x 512] bf16
+// into 32768 rows 22 us, 33 with two launches per digit, [8000 x 512] 34.4 and 35.7.)
 constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64, kOneSteps = 8, kOneSort = kOneThreads * kOneSteps;
 template <Source S>
 __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(Keys k, int passes, uint2 *__restrict__ sorted, ClearJob clear) {
@@ -286,18 +292,25 @@ size_t counts_bytes(int64_t n, int bins) {
   return blocks > 1 ? align_up((size_t)blocks * bins * sizeof(uint32_t), 256) : 0;
 }
 
-unsigned clear_blocks(const ClearJob &c) {
+int64_t clear_blocks(const ClearJob &c) {
   if (c.p == nullptr) return 0;
-  if (c.ld == c.cols || c.rows == 1) return (unsigned)ceil_div(c.rows * c.cols, kClearPerBlock);
-  const int64_t per = kClearPerBlock / c.cols > 0 ? kClearPerBlock / c.cols : 1;
-  return (unsigned)ceil_div(c.rows, per);
+  if (c.ld == c.cols || c.rows == 1) return ceil_div(c.rows * c.cols, c.per);
+  const int64_t per = c.per / c.cols > 0 ? c.per / c.cols : 1;
+  return ceil_div(c.rows, per);
+}
+
+// The job with its workgroups' shares: `per` elements, or more.
+ClearJob shared(ClearJob c, int64_t per) {
+  c.per = per;
+  while (clear_blocks(c) > kClearBlocks) c.per *= 2;
+  return c;
 }
 
 // What is to be cleared, handed out to the launches of a sort: each takes its share of the parts that are left.
 struct Clearing {
   ClearJob job;
   unsigned parts, next = 0;
-  explicit Clearing(const ClearJob &j) : job(j), parts(clear_blocks(j)) {}
+  explicit Clearing(const ClearJob &j) : job(shared(j, j.stream ? 4 * kThreads : kClear)), parts((unsigned)clear_blocks(job)) {}
   // the share of a launch with `launches` more to come, in workgroups; *first: its first part
   unsigned share(int launches, unsigned *first) {
     *first = next;
@@ -342,7 +355,7 @@ int launch_expert_sort(const void *ids, int index_type, int64_t n, int64_t E, in
   const Keys k = {ids, n, (uint32_t)E, 0, 0xFFFFFFFFu, (int)E + 1, bit_length((uint32_t)E)};
   const int blocks = blocks_of(n);
   const Places out = {nullptr, offsets, counts, order, slots, rows, align, E};
-  Clearing none(ClearJob{nullptr, 0, 0, 0, false});
+  Clearing none(ClearJob{nullptr, 0, 0, 0, false, 0});
   return index_type == BSR_I64 ? launch_pass<kFromI64, true>(k, blocks, static_cast<uint32_t *>(ws), out, &none, 0, s)
                                : launch_pass<kFromI32, true>(k, blocks, static_cast<uint32_t *>(ws), out, &none, 0, s);
 }
@@ -361,10 +374,11 @@ int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, 
   uint32_t *counts = reinterpret_cast<uint32_t *>(base + (passes > 1 ? 2 : 1) * pairs_bytes);
   if (T <= kOneSort) {
     const Keys k = {tokens, T, (uint32_t)V, 0, (1u << bits) - 1u, 1 << bits, bits};
-    const dim3 grid(1 + clear_blocks(clear));
+    const ClearJob job = shared(clear, kClear);
+    const dim3 grid(1 + (unsigned)clear_blocks(job));
     if (index_type == BSR_I64)
-      hipLaunchKernelGGL((sort_one_kernel<kFromI64>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], clear);
-    else hipLaunchKernelGGL((sort_one_kernel<kFromI32>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], clear);
+      hipLaunchKernelGGL((sort_one_kernel<kFromI64>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], job);
+    else hipLaunchKernelGGL((sort_one_kernel<kFromI32>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], job);
     *sorted = buffer[0];
     return check_launch();
   }

@@ -32,6 +32,7 @@ struct ClearJob {
   float *p;                // null: nothing to clear
   int64_t rows, cols, ld;
   bool stream;             // past the caches; p is 16-byte aligned and ld == cols then
+  int64_t per;             // elements that a workgroup clears, set by the sort
 };
 int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, const ClearJob &clear, void *ws,
                       const uint2 **sorted, hipStream_t s);
