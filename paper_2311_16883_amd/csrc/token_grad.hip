@@ -19,7 +19,8 @@ constexpr int64_t kStreamBytes = int64_t(96) << 20;
 constexpr int kGroup = 4;                      // windows whose runs a workgroup of the second kernel joins
 constexpr int kLong = 15;                      // windows of a run from which the waves share it
 constexpr int kLeastWindow = 4;
-constexpr int64_t kEnoughWaves = 2048;
+// (waves for each window size: window_size)
+constexpr int64_t kEnoughWaves = 2048, kEnoughLongRuns = 256, kOften = 32;
 constexpr int kThreads = 256;
 
 // The sum of a run of equal tokens, positions [first, last) of the sorted order (inside one window, [lo, hi)): to its row of dE,
@@ -209,34 +210,37 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const uint2 *__restrict_
   }
 }
 
-// Positions of a window: 32, or fewer where that leaves too few waves (64 vectors of `per` columns of a window each) to hide the
-// loads' latency.
-int window_size(int64_t T, int64_t D) {
+// Positions of a window: 32, or fewer where that leaves too few waves (512 columns of a window each) to hide the loads' latency
+// ([16384 x 768] bf16 into 32768 rows 43 us, 48 with 1024 waves; but [65536 x 512] into 1000 rows 36 and, with 8192 waves, 52).
+// Where rows occur kOften times on the average, most windows leave partial sums, and fewer waves do ([8192 x 384] into 2 rows 50 -> 24,
+// [16384 x 64] binary32 into 50 25 -> 21).
+int window_size(int64_t T, int64_t V, int64_t D) {
+  const int64_t enough = T / kOften >= V ? kEnoughLongRuns : kEnoughWaves;
   int size = 32;
-  while (size > kLeastWindow && T > size / 2 && ceil_div(T, (int64_t)size) * ceil_div(D, (int64_t)512) < kEnoughWaves) size /= 2;
+  while (size > kLeastWindow && T > size / 2 && ceil_div(T, (int64_t)size) * ceil_div(D, (int64_t)512) < enough) size /= 2;
   return size;
 }
 
-size_t partial_bytes(int64_t T, int64_t D) {
-  const int64_t windows = ceil_div(T, (int64_t)window_size(T, D));
+size_t partial_bytes(int64_t T, int64_t V, int64_t D) {
+  const int64_t windows = ceil_div(T, (int64_t)window_size(T, V, D));
   return windows > 1 ? align_up((size_t)windows * 2 * D * sizeof(float), 256) : 0;
 }
 
 }  // namespace
 
-size_t embedding_grad_ws_bytes(int64_t T, int64_t V, int64_t D) { return token_sort_ws_bytes(T, V) + partial_bytes(T, D); }
+size_t embedding_grad_ws_bytes(int64_t T, int64_t V, int64_t D) { return token_sort_ws_bytes(T, V) + partial_bytes(T, V, D); }
 
 int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const void *dY, int dtype, int64_t D, int64_t lddy,
                           float scale, int64_t V, float *dE, int64_t ldde, int accumulate, void *ws, hipStream_t s) {
   // Cleared past the caches where many of the rows will be written again, and the caches are for those ([8192 x 1024] bf16 into 32768
   // rows 48.8 -> 38.7 us, [65536 x 1024] into 65536 105 -> 98; but [2048 x 1024] into 32768 28 -> 33, which the caches absorb).
   const bool stream = 8 * T >= V && (uintptr_t)dE % 16 == 0 && ldde == D;
-  const ClearJob clear = {accumulate ? nullptr : dE, V, D, ldde, stream};
+  const ClearJob clear = {accumulate ? nullptr : dE, V, D, ldde, stream, 0};
   float *partial = static_cast<float *>(ws);
   const uint2 *sorted = nullptr;
-  int rc = launch_token_sort(tokens, index_type, T, V, clear, static_cast<char *>(ws) + partial_bytes(T, D), &sorted, s);
+  int rc = launch_token_sort(tokens, index_type, T, V, clear, static_cast<char *>(ws) + partial_bytes(T, V, D), &sorted, s);
   if (rc != BSR_OK || T == 0) return rc;
-  const int size = window_size(T, D);
+  const int size = window_size(T, V, D);
   const int64_t windows = ceil_div(T, (int64_t)size);
   const bool read = stream_rows(dY, T, D, lddy, dtype, kStreamBytes);
 #define BSR_CALL_(TY, VE, STREAM)                                                                                              \
