@@ -162,6 +162,22 @@ def test_table_grad_of_many_positions(T, V, D):
     check(got, want.numpy(), ((n[:, None] + 1) * P.U * size).numpy() + 1e-44)
 
 
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("T,V,D", [(9001, 2003, 33), (9001, 281, 600), (9001, 282, 600), (16390, 2, 520), (12000, 60000, 31)])
+def test_table_grad_clears_in_parts(T, V, D, pad):
+    """Sorts in several launches, which clear dE between them: nothing of what was there stays.  Windows of either rule."""
+    tokens = token_mix("uniform", T, V, 8)
+    dY = randn(9, T, D, dtype="bf16")
+    dE = strided(torch.full((V, D), float("nan")), pad, 0, fill=9.0)
+    got = B.bsr_embedding_grad(tokens.cuda(), dY.cuda(), V, dE=dE)
+    assert got is dE and around_is_untouched(dE, pad, 0, 9.0)
+    rows = dY.double()
+    want = torch.zeros(V, D, dtype=torch.float64).index_add_(0, tokens, rows)
+    size = torch.zeros(V, D, dtype=torch.float64).index_add_(0, tokens, rows.abs())
+    n = torch.bincount(tokens, minlength=V)
+    check(got, want.numpy(), ((n[:, None] + 1) * P.U * size).numpy() + 1e-44)
+
+
 def test_table_grad_does_not_read_rows_without_a_token():
     tokens = torch.tensor([4, -1, 4, 9, 0]).cuda()
     dY = torch.ones(5, 12, device="cuda")
