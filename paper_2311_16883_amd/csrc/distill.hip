@@ -9,7 +9,9 @@
 // for (distill_row_kernel; the longest ones keep a quarter in LDS).  Long rows that are fewer than the compute units are cut into chunks
 // (row_chunks), so that every unit has some: one kernel leaves every chunk's (maximum, sum), the next joins those of its row and writes
 // its chunk of the gradient.  The gradient alone needs no row as a whole and goes by chunks always.
-// [8192 x 50000] bf16: loss 164 us (5.0 TB/s), gradient 299 (5.5), both 309 (5.3; a copy on this GPU 5.1, reading alone 6.2).
+// [8192 x 50000] bf16: loss 164 us (5.0 TB/s), gradient 299 (5.5), both 314 (5.2; a copy on this GPU 5.1, reading alone 6.2).  Rows
+// that take a compute unit whole pass their reads, arithmetic and writes one after the other, in rounds of as many rows as there are
+// units: [600 x 250007] both 177 us (3.4 TB/s).  Two passes over chunks are slower still (205).
 #include <type_traits>
 
 #include "buffer_access.h"
@@ -632,7 +634,8 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
   }
 }
 
-// Chunks of a row: enough that the rows' chunks fill the compute units several times over, none shorter than 8192 columns.
+// Chunks of a row: enough that the rows' chunks fill the compute units several times over, none shorter than 8192 columns ([8 x 131072]
+// bf16, loss: 3.5 us and 4.5 for the two launches, 9.0 with the time between them).
 constexpr int64_t kLeastChunk = 8192, kEnoughWorkgroups = 2048;
 void row_chunks(int64_t N, int64_t V, int64_t *chunk, int *chunks) {
   int64_t c = ceil_div(kEnoughWorkgroups, N > 0 ? N : 1);

@@ -5,7 +5,10 @@
 // kAhead rows on their way, and keeps the sum of the current token's rows in registers.  A token whose positions all lie in one
 // window is written to dE straight away; of one that reaches into others every window leaves a partial sum, and a
 // second kernel adds these up window by window.  So the work per wave is the same however often a token occurs, and the order of
-// every sum follows from the tokens alone.  Bound by memory: dY once, dE once.
+// every sum follows from the tokens alone.  Bound by memory: dY once, dE once, and the rows of dE that occur a second time, as these
+// were cleared before it is known which do.
+// [65536 x 1024] bf16 into 65536 rows 92 us: the sort's four launches clear 268 MB in 46 of them (5.8 TB/s), the windows read 134 MB and write
+// the rows in 41, joining takes 7.  [2999 x 411] binary32 into 10007 20 us: three launches that wait for each other, 10 + 5 + 5.
 #include "token_step.h"
 
 namespace bsr {

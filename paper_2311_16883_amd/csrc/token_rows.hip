@@ -4,6 +4,8 @@
 // written once.  A row belongs to a group of `1 << sh` lanes of one wave (16 .. 64, by the row's length: row_lanes), which
 // walk along it 16 bytes a lane, at any alignment; nothing is shared between groups, so there is no LDS and no barrier, and
 // the loads of many rows are on their way per compute unit.
+// bf16: lookup of [32768 x 1536] 22.7 us (5.8 TB/s of the rows that are read and written; a copy on this GPU 5.1, a fill 6.8), [25088 x 4] of
+// 1536 to their experts 63 (6.0), weighted return of [25088 x 2] 43 (5.3), gradients of that 60 (6.3), of the odd [9947 x 3] of 805 12 (5.0).
 #include "token_step.h"
 
 namespace bsr {

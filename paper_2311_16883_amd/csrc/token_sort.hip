@@ -6,7 +6,8 @@
 // pass, take one per digit, lowest first.  Up to one stretch of entries needs no counts of others and one launch per pass; up to
 // kOneSort positions take one launch for all digits.
 //
-// Latency bound: a few bytes per entry.  Order within a workgroup: its waves own consecutive parts of the stretch, a wave takes 64
+// Latency bound: a few bytes per entry.  [25088 x 4] choices of 64 experts 4.8 + 7.4 us, 33 x 2 3.7 (one launch), 2999 tokens of 10007 10.4
+// (one launch, two digits).  Order within a workgroup: its waves own consecutive parts of the stretch, a wave takes 64
 // entries at a time and finds, for every lane, the lanes before it with the same value from one ballot per bit of the value.
 // No atomic decides an order (they only count), so the result is the stable one whatever the timing.
 #include "token_step.h"
