@@ -3,11 +3,11 @@
 // A counting sort of up to kMaxBins values, in two launches: every workgroup counts the values of its stretch of entries
 // (count_kernel); then every workgroup adds up the counts of all, which says where the entries of a value start in the whole
 // and where its own among them, and moves its entries there in order (place_kernel).  Tokens, which have too many values for one such
-// pass, take one per digit, lowest first.  Up to one stretch of entries needs no counts of others and one launch per pass; up to
-// kOneSort positions take one launch for all digits.
+// pass, take one per digit, lowest first.  One stretch of entries needs no counts of others, and one launch per pass.  Up to kOneSort
+// tokens take one launch in which every entry is compared with all others.
 //
-// Latency bound: a few bytes per entry.  [25088 x 4] choices of 64 experts 4.8 + 7.4 us, 33 x 2 3.7 (one launch), 2999 tokens of 10007 10.4
-// (one launch, two digits).  Order within a workgroup: its waves own consecutive parts of the stretch, a wave takes 64
+// Latency bound: a few bytes per entry.  [25088 x 4] choices of 64 experts 4.8 + 7.4 us, 33 x 2 3.7 (one launch), 2999 tokens of 10007 6.8
+// (one launch, with 16 MB of dE cleared beside it).  Order within a workgroup: its waves own consecutive parts of the stretch, a wave takes 64
 // entries at a time and finds, for every lane, the lanes before it with the same value from one ballot per bit of the value.
 // No atomic decides an order (they only count), so the result is the stable one whatever the timing.
 #include "token_step.h"
@@ -24,9 +24,9 @@ constexpr int kFewSteps = 4, kManySteps = 16;  // times 64 entries that a wave t
 // Workgroups from which each takes kManySteps, as each reads the counts of all ([1048576 x 4] choices of 256 experts, 32 columns, 216 us,
 // 444 with kFewSteps; but [25088 x 4] of 64 17 with kFewSteps and 27.5 with kManySteps).
 constexpr int kManyBlocks = 256;
-// Elements that a workgroup clears, or more where that takes more than kClearBlocks workgroups.  Past the caches and beside a sort in
-// several launches, one store per lane: [65536 x 1024] bf16 into 65536 rows 98.8 us with kClear, 91.9 so, [30000 x 2048] into 100000
-// 198 and 180; but beside the large workgroup of one launch, [3000 x 1024] into 16384, 22.2 and 24.8.
+// Elements that a workgroup clears, or more where that takes more than kClearBlocks workgroups.  Past the caches one store per lane:
+// [65536 x 1024] bf16 into 65536 rows 98.8 us with kClear, 91.9 so, [30000 x 2048] into 100000 198 and 180, [8000 x 1024] into 32768 42.8
+// and 35.7; through the caches [500 x 512] into 32768 18.4 and 19.1.
 constexpr int64_t kClear = 32768, kClearBlocks = int64_t(1) << 21;
 
 enum Source { kFromI32, kFromI64, kFromPairs };
@@ -225,60 +225,66 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Keys k, const uint32_t 
   }
 }
 
-// Up to kOneSort positions sorted by all digits of their token in one launch, by one workgroup; the others clear.  ([3000 x 512] bf16
-// into 32768 rows 22 us, 33 with two launches per digit, [8000 x 512] 34.4 and 35.7.)
-constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64, kOneSteps = 8, kOneSort = kOneThreads * kOneSteps;
+// Up to kOneSort positions sorted in one launch: the place of an entry is the number of those before it in the order, with smaller
+// keys or with its own and smaller positions, so each workgroup finds kOneEntries places by comparing with all keys, which it has in
+// LDS.  Further workgroups clear.  Bound by the comparisons, T * T of two operations: [2999 x 411] binary32 into 10007 rows 16.5 us in all, 20
+// with all digits sorted by one workgroup, [8000 x 64] bf16 into 2000 22.7 and 27.9; 12000 positions 34.5, with two launches per digit 34.4.
+// 64 entries to a workgroup 18.5 and 28.2, 16 of them 15.8 and 22.0, but these leave less room to clear ([8000 x 1024] into 32768 40
+// instead of 35.7).
+constexpr int kOneSort = 8192, kOneEntries = 32, kOneParts = kThreads / kOneEntries, kOneLoads = 4;
 template <Source S>
-__global__ __launch_bounds__(kOneThreads) void sort_one_kernel(Keys k, int passes, uint2 *__restrict__ sorted, ClearJob clear) {
-  constexpr int kBins = 1 << kDigitBits;
-  __shared__ uint32_t next[kOneWaves][kBins];
-  __shared__ uint32_t start[kBins];
-  __shared__ uint32_t sums[kOneWaves];
-  __shared__ uint2 moved[kOneSort];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, n = (int)k.n;
-  if (blockIdx.x > 0) {
-    clear_part(clear, (int64_t)blockIdx.x - 1);
+__global__ __launch_bounds__(kThreads) void sort_one_kernel(Keys k, uint2 *__restrict__ sorted, ClearJob clear, int blocks) {
+  __shared__ alignas(16) uint32_t keys[kOneSort];
+  __shared__ uint32_t before[kOneParts][kOneEntries];
+  const int t = threadIdx.x, n = (int)k.n;
+  if ((int)blockIdx.x >= blocks) {
+    clear_part(clear, (int64_t)blockIdx.x - blocks);
     return;
   }
-  const int steps = (n + kOneThreads - 1) / kOneThreads, lo = w * steps * 64;
-  uint2 e[kOneSteps];
+  // whole entries of kOneEntries, those behind the last greater than any key
+  const int all = (n + kOneEntries - 1) / kOneEntries * kOneEntries;
+  for (int i0 = t; i0 < all; i0 += kOneLoads * kThreads) {
+    uint32_t key[kOneLoads];
 #pragma unroll
-  for (int q = 0; q < kOneSteps; ++q)
-    if (q < steps) e[q] = load_entry<S>(k, lo + q * 64 + lane < n ? lo + q * 64 + lane : 0);
-  for (int p = 0; p < passes; ++p, k.shift += k.bits) {
-    for (int b = lane; b < k.bins; b += 64) next[w][b] = 0;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    uint32_t rank[kOneSteps];
-#pragma unroll
-    for (int q = 0; q < kOneSteps; ++q)
-      if (q < steps && lo + q * 64 < n)
-        rank[q] = rank_entry(next[w], digit_of(k, e[q].x), k.bits, lo + q * 64 + lane < n, lane);
-    __syncthreads();
-    for (int b = t; b < k.bins; b += kOneThreads) {
-      uint32_t here = 0;
-#pragma unroll
-      for (int v = 0; v < kOneWaves; ++v) {
-        const uint32_t c = next[v][b];
-        next[v][b] = here;
-        here += c;
-      }
-      start[b] = here;
+    for (int u = 0; u < kOneLoads; ++u) {
+      const int i = i0 + u * kThreads;
+      key[u] = i < n ? load_entry<S>(k, i).x : 0xFFFFFFFFu;
     }
-    __syncthreads();
-    scan_bins<kOneWaves>(start, k.bins, sums);
 #pragma unroll
-    for (int q = 0; q < kOneSteps; ++q) {
-      if (q >= steps || lo + q * 64 + lane >= n) continue;
-      const uint32_t d = digit_of(k, e[q].x), place = start[d] + next[w][d] + rank[q];
-      if (p == passes - 1) sorted[place] = e[q];
-      else moved[place] = e[q];
-    }
-    if (p == passes - 1) return;
-    __syncthreads();
+    for (int u = 0; u < kOneLoads; ++u)
+      if (i0 + u * kThreads < all) keys[i0 + u * kThreads] = key[u];
+  }
+  __syncthreads();
+  // Every lane compares one entry with its part of the keys, four at a time: keys before the workgroup's entries count up to equal
+  // ones, those behind only if they are smaller, its own by their positions.
+  const int first = blockIdx.x * kOneEntries, i = first + (t & (kOneEntries - 1)), part = t / kOneEntries;
+  const uint32_t mine = keys[i];
+  const Words4 *fours = reinterpret_cast<const Words4 *>(keys);
+  uint32_t count = 0;
+#pragma unroll 4
+  for (int g = part; g < first / 4; g += kOneParts) {
+    const Words4 w = fours[g];
 #pragma unroll
-    for (int q = 0; q < kOneSteps; ++q)
-      if (q < steps && lo + q * 64 + lane < n) e[q] = moved[lo + q * 64 + lane];
+    for (int q = 0; q < 4; ++q) count += w[q] < mine + 1;
+  }
+#pragma unroll 4
+  for (int g = (first + kOneEntries) / 4 + part; g < all / 4; g += kOneParts) {
+    const Words4 w = fours[g];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) count += w[q] < mine;
+  }
+  for (int g = first / 4 + part; g < (first + kOneEntries) / 4; g += kOneParts) {
+    const Words4 w = fours[g];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) count += w[q] < mine || (w[q] == mine && g * 4 + q < i);
+  }
+  before[part][t & (kOneEntries - 1)] = count;
+  __syncthreads();
+  if (t < kOneEntries && i < n) {
+    uint32_t place = 0;
+#pragma unroll
+    for (int s = 0; s < kOneParts; ++s) place += before[s][t];
+    sorted[place] = uint2{mine, (uint32_t)i};
   }
 }
 
@@ -300,9 +306,9 @@ int64_t clear_blocks(const ClearJob &c) {
   return ceil_div(c.rows, per);
 }
 
-// The job with its workgroups' shares: `per` elements, or more.
-ClearJob shared(ClearJob c, int64_t per) {
-  c.per = per;
+// The job with its workgroups' shares.
+ClearJob shared(ClearJob c) {
+  c.per = c.stream ? 4 * kThreads : kClear;
   while (clear_blocks(c) > kClearBlocks) c.per *= 2;
   return c;
 }
@@ -311,7 +317,7 @@ ClearJob shared(ClearJob c, int64_t per) {
 struct Clearing {
   ClearJob job;
   unsigned parts, next = 0;
-  explicit Clearing(const ClearJob &j) : job(shared(j, j.stream ? 4 * kThreads : kClear)), parts((unsigned)clear_blocks(job)) {}
+  explicit Clearing(const ClearJob &j) : job(shared(j)), parts((unsigned)clear_blocks(job)) {}
   // the share of a launch with `launches` more to come, in workgroups; *first: its first part
   unsigned share(int launches, unsigned *first) {
     *first = next;
@@ -374,12 +380,12 @@ int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, 
   uint2 *buffer[2] = {reinterpret_cast<uint2 *>(base), reinterpret_cast<uint2 *>(base + (passes > 1 ? pairs_bytes : 0))};
   uint32_t *counts = reinterpret_cast<uint32_t *>(base + (passes > 1 ? 2 : 1) * pairs_bytes);
   if (T <= kOneSort) {
-    const Keys k = {tokens, T, (uint32_t)V, 0, (1u << bits) - 1u, 1 << bits, bits};
-    const ClearJob job = shared(clear, kClear);
-    const dim3 grid(1 + (unsigned)clear_blocks(job));
-    if (index_type == BSR_I64)
-      hipLaunchKernelGGL((sort_one_kernel<kFromI64>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], job);
-    else hipLaunchKernelGGL((sort_one_kernel<kFromI32>), grid, dim3(kOneThreads), 0, s, k, passes, buffer[0], job);
+    const ClearJob job = shared(clear);
+    const int blocks = (int)ceil_div(T, (int64_t)kOneEntries);
+    const dim3 grid(blocks + (unsigned)clear_blocks(job));
+    const Keys k = {tokens, T, (uint32_t)V, 0, 0, 0, 0};
+    if (index_type == BSR_I64) hipLaunchKernelGGL((sort_one_kernel<kFromI64>), grid, dim3(kThreads), 0, s, k, buffer[0], job, blocks);
+    else hipLaunchKernelGGL((sort_one_kernel<kFromI32>), grid, dim3(kThreads), 0, s, k, buffer[0], job, blocks);
     *sorted = buffer[0];
     return check_launch();
   }
@@ -389,7 +395,7 @@ int launch_token_sort(const void *tokens, int index_type, int64_t T, int64_t V, 
     const int blocks = blocks_of(T);
     Places out = {};
     out.pairs = buffer[p & 1];
-    const int later = (passes - 1 - p) * (blocks > 1 ? 2 : 1);
+    const int later = (passes - 1 - p) * 2;
     const int rc = p > 0 ? launch_pass<kFromPairs, false>(k, blocks, counts, out, &clearing, later, s)
                    : index_type == BSR_I64 ? launch_pass<kFromI64, false>(k, blocks, counts, out, &clearing, later, s)
                                            : launch_pass<kFromI32, false>(k, blocks, counts, out, &clearing, later, s);

@@ -178,6 +178,24 @@ def test_table_grad_clears_in_parts(T, V, D, pad):
     check(got, want.numpy(), ((n[:, None] + 1) * P.U * size).numpy() + 1e-44)
 
 
+@pytest.mark.parametrize("index", ["i32", "i64"])
+@pytest.mark.parametrize("T", [511, 512, 513, 2047, 8160, 8161, 8191, 8192, 8193])
+def test_table_grad_at_the_sizes_of_the_sorts(index, T):
+    """Around the sizes at which the sort changes: sums of equal tokens, and a permutation, which is exact."""
+    V = 97
+    tokens = token_mix("text", T, V, T).to(IX[index])
+    dY = randn(4, T, 8)
+    got = B.bsr_embedding_grad(tokens.cuda(), dY.cuda(), V)
+    want, bound = P.table_grad(tokens.numpy(), f64(dY), V, 1.0)
+    check(got, want, bound)
+    # one position per token: a permutation, exact
+    order = torch.randperm(T, generator=torch.Generator().manual_seed(T)).to(IX[index])
+    got = B.bsr_embedding_grad(order.cuda(), dY.cuda(), T + 3)
+    exact = torch.zeros(T + 3, 8)
+    exact[order.long()] = dY
+    assert torch.equal(got.cpu(), exact)
+
+
 def test_table_grad_does_not_read_rows_without_a_token():
     tokens = torch.tensor([4, -1, 4, 9, 0]).cuda()
     dY = torch.ones(5, 12, device="cuda")
