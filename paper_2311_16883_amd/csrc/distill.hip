@@ -189,6 +189,10 @@ struct RawEntry {
   }
 };
 
+// The teacher's logit x as a row's maximum takes it, which drops NaN: NaN counts as +inf there, so that a row with such an entry is none
+// without entries and its shares become NaN.
+__device__ __forceinline__ float as_top(float x) { return x != x ? __builtin_inff() : x; }
+
 // e_j in place of the teacher's logits; returns the lane's sum.  top: their maximum.
 template <int THREADS>
 __device__ __forceinline__ float weigh_entries(const Distill &a, const Entries &en, float top) {
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     entry.take(a, &v, &x);
     en.at[j] = (int32_t)v;
     en.share[j] = x;
-    tm = fmaxf(tm, x);
+    tm = fmaxf(tm, as_top(x));
     return v >= lo && v < hi ? v : lo;
   };
   int64_t z_at = lo;
@@ -565,7 +569,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
     en.at[j] = (int32_t)v;
     en.share[j] = x;
     en.z[j] = picked[n * a.K + j];             // (the row's own may be overwritten by other chunks' workgroups by now)
-    tm = fmaxf(tm, x);
+    tm = fmaxf(tm, as_top(x));
   }
   float pm = minus_inf();
   for (int i = t; i < parts_per_row; i += kThreads) pm = fmaxf(pm, parts[n * parts_per_row + i].x);
