@@ -212,7 +212,9 @@ __device__ __forceinline__ float cross_entries(const Distill &a, const Entries &
   float sum = 0.0f;
   for (int j = threadIdx.x; j < a.K; j += THREADS) {
     const float e = en.share[j];
-    if (e != 0.0f) sum = fmaf(e * by, 0.5f * (a.tau * kLn2 * log2f(e)) - (0.5f * en.z[j] - 0.5f * m), sum);
+    if (e == 0.0f) continue;
+    const float cost = 0.5f * (a.tau * kLn2 * log2f(e)) - (0.5f * en.z[j] - 0.5f * m);
+    sum = cost == __builtin_inff() ? sum + cost : fmaf(e * by, cost, sum);       // (e * by may have no bits left, which times inf is NaN)
   }
   return sum;
 }

@@ -1,12 +1,12 @@
-"""Distillation where the teacher's logits are no numbers: NaN and +inf must reach the loss and the gradient at the entries, in every
-form of the kernels."""
+"""Distillation where the teacher's logits, or the student's at the teacher's entries, are no ordinary numbers: NaN and +inf must reach
+the loss and the gradient at the entries, in every form of the kernels."""
 import numpy as np
 import pytest
 import torch
 
 import token_plain as P
 from paper_2311_16883_amd import binding as B
-from test_gpu_token_ops import DT, check, f64
+from test_gpu_token_ops import DT, check, f64, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +70,16 @@ def test_a_teachers_nan_and_infinity_reach_the_loss_and_the_gradient(dtype, N, V
             assert float(loss[n]) == 0 and not got[n].any()
         check(loss[8:10], want, e_loss)
         check(got[8:10], whole, e_whole, dtype)
+
+
+@pytest.mark.parametrize("dtype,N,V", SHAPES)
+def test_an_entry_at_a_masked_column_costs_infinitely_much_whatever_its_share(dtype, N, V):
+    """Down to shares and temperatures whose product is less than any binary32 number."""
+    z, dloss = randn(1, N, V, dtype=dtype), torch.ones(N)
+    ids = torch.arange(3)[None].repeat(N, 1)
+    z[:, 2] = -INF
+    for tau, t in ((2.0 ** -60, [0.0, -1.0 * 2.0 ** -61, -70.0 * 2.0 ** -60]), (2.0 ** -40, [0.0, 0.0, -80.0 * 2.0 ** -40]),
+                   (1.0, [3.0, 2.0, -50.0])):
+        teacher = torch.tensor(t)[None].repeat(N, 1)
+        for loss, grad in three_calls(z, ids, teacher, dloss, tau):
+            assert bool((loss == INF).all()) and bool(torch.isfinite(grad).all())
