@@ -423,6 +423,13 @@ Dense matrix_like(const at::Tensor &x, const char *what, const at::Tensor &like)
   return d;
 }
 
+// The workspace of a token operator: the caller's, whose extent the library takes at its word, or a new one.
+template <typename F>
+Workspace token_workspace(PyObject *given, F need, const at::Tensor &like) {
+  if (given != Py_None && packed(given, "ws", like).scalar_type() != at::kByte) value_error("ws must be uint8");
+  return Workspace(given, given == Py_None ? need() : 0, like);
+}
+
 // BSR_I32 / BSR_I64, or BSR_ERR_DTYPE.
 int index_code(const at::Tensor &t) {
   const auto s = t.scalar_type();
@@ -472,7 +479,7 @@ PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const CallStream stream(a[7], dY);
     int64_t ldde;
     const Output dE = matrix_output(a[4], "dE", V, y.cols, at::kFloat, dY, &ldde);
-    const Workspace ws(a[6], a[6] == Py_None ? bsr_embedding_grad_workspace_bytes(y.rows, V, y.cols) : 0, dY);
+    const Workspace ws = token_workspace(a[6], [&] { return bsr_embedding_grad_workspace_bytes(y.rows, V, y.cols); }, dY);
     const int rc = released([&] {
       return bsr_embedding_grad(pointer(tokens), index, y.rows, pointer(dY), code, y.cols, y.ld, (float)scale, V,
                                 typed<float>(dE.get()), ldde, accumulate ? 1 : 0, ws.p, ws.bytes, stream.handle());
@@ -506,7 +513,7 @@ PyObject *expert_sort(PyObject *, PyObject *const *a, Py_ssize_t n) {
       order = packed_output(a[5], "order", {rows}, at::kInt, ids);
       slots = packed_output(a[6], "slots", ids.sizes(), at::kInt, ids);
     }
-    const Workspace ws(a[7], a[7] == Py_None ? bsr_expert_sort_workspace_bytes(entries, E) : 0, ids);
+    const Workspace ws = token_workspace(a[7], [&] { return bsr_expert_sort_workspace_bytes(entries, E); }, ids);
     const int rc = released([&] {
       return bsr_expert_sort(pointer(ids), index, entries, E, align, typed<int32_t>(offsets.get()), typed<int32_t>(counts.get()),
                              typed<int32_t>(order.get()), typed<int32_t>(slots.get()), ws.p, ws.bytes, stream.handle());
@@ -632,7 +639,7 @@ PyObject *distill_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
       loss = packed_output(a[4], "loss", {c.z.rows}, at::kFloat, c.logits);
       stats = packed_output(a[5], "stats", {c.z.rows, 2}, at::kFloat, c.logits);
     }
-    const Workspace ws(a[6], a[6] == Py_None ? c.workspace() : 0, c.logits);
+    const Workspace ws = token_workspace(a[6], [&] { return c.workspace(); }, c.logits);
     const int rc = released([&] {
       return bsr_distill_loss(pointer(c.logits), c.code, c.z.rows, c.z.cols, c.z.ld, pointer(c.ids), c.index, pointer(c.teacher),
                               c.teacher_code, c.K, c.temperature, typed<float>(loss.get()), typed<float>(stats.get()), ws.p,
@@ -674,7 +681,7 @@ PyObject *distill_loss_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const Output loss = packed_output(a[5], "loss", {c.z.rows}, at::kFloat, c.logits);
     int64_t ldd;
     const Output dlogits = matrix_output(a[6], "dlogits", c.z.rows, c.z.cols, c.logits.scalar_type(), c.logits, &ldd);
-    const Workspace ws(a[7], a[7] == Py_None ? c.workspace() : 0, c.logits);
+    const Workspace ws = token_workspace(a[7], [&] { return c.workspace(); }, c.logits);
     const int rc = released([&] {
       return bsr_distill_loss_grad(pointer(c.logits), c.code, c.z.rows, c.z.cols, c.z.ld, pointer(c.ids), c.index,
                                    pointer(c.teacher), c.teacher_code, c.K, c.temperature, typed<float>(dloss),
