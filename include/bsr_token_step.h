@@ -35,6 +35,9 @@ extern "C" {
 
 enum { BSR_I32 = 0, BSR_I64 = 1 };
 
+/* experts of a sort; rows of a token table whose gradient is wanted */
+enum { BSR_MAX_EXPERTS = 1024, BSR_MAX_VOCAB = (1 << 30) - 1 };
+
 enum { BSR_ERR_VALUE = -9 /* a number is outside its range: temperature outside [2^-60, 2^60], scale not finite */ };
 
 /*
@@ -55,7 +58,7 @@ int bsr_embedding_lookup(const void *table, int dtype, int64_t V, int64_t D,
  * do not occur), otherwise only rows of tokens that occur are touched, and added to.
  * Positions whose token is outside [0, V) have no gradient.  (A long sum is cut into
  * pieces of consecutive positions, which are added in order.)
- * T < 2^31, V < 2^30 (BSR_ERR_SHAPE).  Workspace: the function below (0 for invalid sizes).
+ * T < 2^31, V <= BSR_MAX_VOCAB (BSR_ERR_SHAPE).  Workspace: the function below (0 for invalid sizes).
  */
 size_t bsr_embedding_grad_workspace_bytes(int64_t T, int64_t V, int64_t D);
 int bsr_embedding_grad(const void *tokens, int index_type, int64_t T,
@@ -81,7 +84,7 @@ int64_t bsr_expert_capacity(int64_t n, int64_t E, int64_t align);
  *   order   [rows]  entry that a row holds, -1 for rows of padding (also behind the last
  *                   segment); rows = bsr_expert_capacity(n, E, align);
  *   slots   [n]     row that holds an entry, -1 for a dropped one.
- * E <= 1024 (BSR_ERR_LIMIT beyond).  Workspace: the function below.
+ * E <= BSR_MAX_EXPERTS (BSR_ERR_LIMIT beyond).  Workspace: the function below.
  */
 size_t bsr_expert_sort_workspace_bytes(int64_t n, int64_t E);
 int bsr_expert_sort(const void *expert_ids, int index_type, int64_t n, int64_t E,

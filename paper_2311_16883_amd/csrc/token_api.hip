@@ -9,7 +9,6 @@ namespace bsr {
 namespace {
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;          // rows, entries and columns are counted in 32 bits by the kernels
-constexpr int64_t kMaxTokens = (int64_t(1) << 30) - 1;        // rows of a token table whose gradient is wanted
 constexpr int64_t kMaxWidth = int64_t(1) << 40;
 
 bool misaligned(const void *p, size_t a) { return p != nullptr && (uintptr_t)p % a != 0; }
@@ -91,7 +90,7 @@ int bsr_embedding_lookup(const void *table, int dtype, int64_t V, int64_t D, int
 }
 
 size_t bsr_embedding_grad_workspace_bytes(int64_t T, int64_t V, int64_t D) {
-  if (check_matrix(T, D, D) != BSR_OK || check_matrix(V, D, D) != BSR_OK || V > kMaxTokens) return 0;
+  if (check_matrix(T, D, D) != BSR_OK || check_matrix(V, D, D) != BSR_OK || V > BSR_MAX_VOCAB) return 0;
   return T == 0 || V == 0 || D == 0 ? 0 : embedding_grad_ws_bytes(T, V, D);
 }
 
@@ -100,7 +99,7 @@ int bsr_embedding_grad(const void *tokens, int index_type, int64_t T, const void
   BSR_REQUIRE(check_types(dtype, index_type));
   BSR_REQUIRE(check_matrix(T, D, lddy));
   BSR_REQUIRE(check_matrix(V, D, ldde));
-  if (V > kMaxTokens) return BSR_ERR_SHAPE;
+  if (V > BSR_MAX_VOCAB) return BSR_ERR_SHAPE;
   if (!std::isfinite(scale)) return BSR_ERR_VALUE;
   if (V == 0 || D == 0 || (T == 0 && accumulate)) return BSR_OK;
   if (dE == nullptr || (T > 0 && (tokens == nullptr || dY == nullptr))) return BSR_ERR_NULL;

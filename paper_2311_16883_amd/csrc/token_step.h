@@ -21,7 +21,7 @@ int launch_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t 
                                void *dYs, int64_t lddys, float *dweights, hipStream_t s);
 
 // token_sort.hip: stable sorts by key.
-constexpr int kMaxExperts = 1024;
+constexpr int kMaxExperts = BSR_MAX_EXPERTS;
 size_t expert_sort_ws_bytes(int64_t n, int64_t E);
 int launch_expert_sort(const void *ids, int index_type, int64_t n, int64_t E, int64_t align, int32_t *offsets, int32_t *counts,
                        int32_t *order, int64_t rows, int32_t *slots, void *ws, hipStream_t s);

@@ -476,6 +476,7 @@ PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (a[4] == Py_None && accumulate) value_error("accumulate needs an existing dE");
     const int code = dtype_code(dY), index = index_code(tokens);
     if (code < 0 || index < 0) return code_result(BSR_ERR_DTYPE);
+    if (V > BSR_MAX_VOCAB) return code_result(BSR_ERR_SHAPE);      // (and in expert_sort: before outputs of that size are made)
     const CallStream stream(a[7], dY);
     int64_t ldde;
     const Output dE = matrix_output(a[4], "dE", V, y.cols, at::kFloat, dY, &ldde);
@@ -499,6 +500,7 @@ PyObject *expert_sort(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (index < 0) return code_result(BSR_ERR_DTYPE);
     const int64_t rows = bsr_expert_capacity(entries, E, align);
     if (rows < 0) return code_result(BSR_ERR_SHAPE);
+    if (E > BSR_MAX_EXPERTS) return code_result(BSR_ERR_LIMIT);
     const CallStream stream(a[8], ids);
     Output offsets, counts, order, slots;
     if (a[3] == Py_None && a[4] == Py_None && a[5] == Py_None && a[6] == Py_None) {

@@ -38,3 +38,17 @@ def test_a_workspace_is_packed_bytes_on_the_device(which):
     with pytest.raises(B.BsrError) as e:
         call(whole[:need - 1])
     assert e.value.code == B.BSR_ERR_WORKSPACE
+
+
+def test_sizes_beyond_the_limits_are_refused_before_anything_of_their_size_is_allocated():
+    ids, empty = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(0, dtype=torch.int64, device="cuda")
+    x = torch.zeros(4, 8, device="cuda")
+    for experts in (1025, 1 << 34, 1 << 40, (1 << 63) - 1):
+        with pytest.raises(B.BsrError) as e:
+            B.bsr_expert_sort(ids, experts)
+        assert e.value.code == B.BSR_ERR_LIMIT
+    for vocab in (1 << 30, 1 << 34, 1 << 40, 1 << 61, (1 << 63) - 1):
+        for tokens, rows in ((ids, x), (empty, x[:0])):
+            with pytest.raises(B.BsrError) as e:
+                B.bsr_embedding_grad(tokens, rows, vocab)
+            assert e.value.code == B.BSR_ERR_SHAPE
