@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void window_sum_kernel(const uint2 *__res
                                                               float *__restrict__ partial, int64_t slices, int size) {
   typedef RowVec<T, VE> R;
   const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t unit = block_number() * (kThreads / 64) + (threadIdx.x >> 6);
   const int64_t window = unit / slices, slice = unit - window * slices;
   const int64_t lo = window * size;
   if (lo >= n) return;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const uint2 *__restrict_
   typedef RowVec<float, VE> R;
   __shared__ float parts[kWaves][64 * VE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
+  const int64_t block = block_number(), group = block / slices, slice = block - group * slices;
   // lane l: whether a run starts in window l of the group and goes on behind it, and whose it is
   const int64_t mine = group * kGroup + lane, lo = mine * size, behind = lo + size;
   uint32_t token = V;
@@ -248,7 +248,7 @@ int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const v
   const bool read = stream_rows(dY, T, D, lddy, dtype, kStreamBytes);
 #define BSR_CALL_(TY, VE, STREAM)                                                                                              \
   const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
-  hipLaunchKernelGGL((window_sum_kernel<TY, VE, STREAM>), dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))),         \
+  hipLaunchKernelGGL((window_sum_kernel<TY, VE, STREAM>), grid_of(ceil_div(windows * slices, (int64_t)(kThreads / 64))),                \
                      dim3(kThreads), 0, s, sorted, T, (uint32_t)V, static_cast<const TY *>(dY), D, lddy, scale, dE, ldde,      \
                      accumulate, partial, slices, size)
 #define BSR_CALL(TY, VE) \
@@ -264,7 +264,7 @@ int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const v
   if (rc != BSR_OK || windows == 1) return rc;
 #define BSR_JOIN(VE)                                                                                                           \
   const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
-  hipLaunchKernelGGL((join_kernel<VE>), dim3((unsigned)(ceil_div(windows, (int64_t)kGroup) * slices)), dim3(kThreads),         \
+  hipLaunchKernelGGL((join_kernel<VE>), grid_of(ceil_div(windows, (int64_t)kGroup) * slices), dim3(kThreads),                  \
                      0, s, sorted, T, (uint32_t)V, D, scale, dE, ldde, accumulate, partial, windows, slices, size)
   if (D >= 4) { BSR_JOIN(4); } else { BSR_JOIN(1); }
 #undef BSR_JOIN

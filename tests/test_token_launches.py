@@ -1,0 +1,96 @@
+"""What token operators launch at the largest sizes that they accept: the host code runs against a recorder of launches
+(tests/launch_lanes.c), so nothing of that size has to exist.  CPU only."""
+import json
+import subprocess
+import sys
+from pathlib import Path
+
+import pytest
+
+from paper_2311_16883_amd import binding as B
+
+HERE = Path(__file__).resolve().parent
+LIB = HERE.parent / "paper_2311_16883_amd" / "libbsr_actprune.so"
+F32, BF16, I32, I64 = 0, 1, 0, 1
+MOST = (1 << 31) - 1                                 # rows, positions, entries
+
+
+@pytest.fixture(scope="module")
+def record(tmp_path_factory):
+    so = tmp_path_factory.mktemp("recorder") / "liblaunch_lanes.so"
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", str(so), str(HERE / "launch_lanes.c")], check=True)
+    B.lib()                                          # built if it is not there yet
+
+    def run(*calls):
+        r = subprocess.run([sys.executable, str(HERE / "recorded_token_calls.py"), str(so), str(LIB)], input=json.dumps(calls),
+                           capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stderr
+        return json.loads(r.stdout)
+
+    return run
+
+
+def lookup(T, V, D, dtype=BF16):
+    return ["bsr_embedding_lookup", ["p", dtype, V, D, D, "p", I32, T, 1.0, "p", D, None]]
+
+
+def table_grad(T, V, D, dtype=BF16, accumulate=0, ldde=None):
+    return ["bsr_embedding_grad", ["p", I32, T, "p", dtype, D, D, 1.0, V, "p", ldde or D, accumulate, "ws", None]]
+
+
+def expert_sort(n, E, align=1):
+    return ["bsr_expert_sort", ["p", I32, n, E, align, "p", "p", "p", "p", "ws", None]]
+
+
+def gather(T, k, rows, D):
+    return ["bsr_expert_gather", ["p", BF16, T, D, D, "p", k, "p", rows, "p", D, None]]
+
+
+def combine(T, k, rows, D):
+    return ["bsr_expert_combine", ["p", BF16, rows, D, D, "p", T, k, None, "p", D, None]]
+
+
+def combine_grad(T, k, rows, D):
+    return ["bsr_expert_combine_grad", ["p", BF16, rows, D, D, "p", "p", T, k, "p", "p", D, "p", D, "p", None]]
+
+
+def distill_grad(N, V, K):
+    return ["bsr_distill_grad", ["p", BF16, N, V, V, "p", I32, "p", BF16, K, 1.0, "p", "p", "p", V, None]]
+
+
+def distill_both(N, V, K):
+    return ["bsr_distill_loss_grad", ["p", BF16, N, V, V, "p", I32, "p", BF16, K, 1.0, "p", "p", "p", V, "ws", None]]
+
+
+LARGEST = [
+    lookup(MOST, MOST, 1), lookup(MOST, 1000, 1024), lookup(MOST, 5, 8, F32),
+    table_grad(MOST, 1000, 1), table_grad(MOST, 1000, 8), table_grad(MOST, 1000, 3, F32), table_grad(MOST, 1000, 1, BF16, 1),
+    table_grad(MOST, 1, 1), table_grad(MOST - 31, (1 << 30) - 1, 1), table_grad(1 << 30, 50000, 512),
+    table_grad(1, (1 << 30) - 1, 64), table_grad(9000, (1 << 30) - 1, 3, F32, 0, 7),
+    expert_sort(MOST, 1024), expert_sort(MOST - 5, 1), expert_sort(1000, 7, 1 << 28),
+    gather(MOST, 1, MOST, 1), gather(1 << 28, 7, MOST, 512), combine(MOST, 1, MOST, 1), combine(1 << 28, 7, MOST, 512),
+    combine_grad(MOST, 1, MOST, 1), combine_grad(1 << 28, 7, MOST, 512),
+    distill_grad(1 << 27, 40, 3), distill_grad(2, MOST, 3), distill_both(1 << 27, 40, 3), distill_both(2, MOST, 3),
+    distill_both(1 << 20, 60000, 3), distill_both(70000, 600000, 3),
+]
+
+
+@pytest.mark.parametrize("i", range(len(LARGEST)), ids=lambda i: "%s-%d" % (LARGEST[i][0], i))
+def test_launches_of_the_largest_sizes_are_ones_that_the_hardware_takes(record, i):
+    """Lanes along a dimension are counted in 32 bits, workgroups along the second and third in 16."""
+    got, = record(LARGEST[i])
+    assert got["rc"] == 0 and got["launches"]
+    for l in got["launches"]:
+        assert all(0 < n < 1 << 32 for n in l["lanes"]), l
+        assert l["grid"][1] < 1 << 16 and l["grid"][2] < 1 << 16, l
+
+
+def test_every_position_of_the_largest_table_gradient_has_a_wave(record):
+    for T, size in ((MOST, 32), (MOST - 31, 32), (100000, 32)):
+        got, = record(table_grad(T, 1000, 1))
+        sums = [l for l in got["launches"] if "window_sum_kernel" in l["kernel"]]
+        joins = [l for l in got["launches"] if "join_kernel" in l["kernel"]]
+        windows = -(-T // size)
+        assert len(sums) == len(joins) == 1
+        assert sums[0]["lanes"][0] * sums[0]["lanes"][1] >= windows * 64
+        assert joins[0]["grid"][0] * joins[0]["grid"][1] >= -(-windows // 4)
