@@ -1,6 +1,7 @@
 """What token operators launch at the largest sizes that they accept: the host code runs against a recorder of launches
 (tests/launch_lanes.c), so nothing of that size has to exist.  CPU only."""
 import json
+import re
 import subprocess
 import sys
 from pathlib import Path
@@ -94,3 +95,36 @@ def test_every_position_of_the_largest_table_gradient_has_a_wave(record):
         assert len(sums) == len(joins) == 1
         assert sums[0]["lanes"][0] * sums[0]["lanes"][1] >= windows * 64
         assert joins[0]["grid"][0] * joins[0]["grid"][1] >= -(-windows // 4)
+
+
+def forms(got, kernel):
+    """The truth values among the template arguments of a launched kernel: whether it reads and writes past the caches."""
+    names = [l["kernel"] for l in got["launches"] if kernel in l["kernel"]]
+    assert len(names) == 1, got
+    return [c == "1" for c in re.findall(r"Lb([01])E", names[0])]
+
+
+MIB = 1 << 20
+
+
+def test_rows_pass_by_the_caches_from_the_stated_sizes_on(record):
+    """32 MiB written, 64 MiB read, 96 MiB of a table's gradients, in rows of whole 128-byte lines: what the tests of these sizes on the
+    GPU (test_gpu_token_large.py) mean to reach."""
+    D, row = 1024, 2048
+    for T, yes in ((32 * MIB // row, True), (32 * MIB // row - 1, False)):
+        got, = record(lookup(T, 3000, D))
+        assert forms(got, "embedding_lookup_kernel") == [yes]
+        got, = record(gather(T // 2 - 40, 2, T, D))
+        assert forms(got, "expert_gather_kernel") == [yes]
+    got, = record(lookup(32 * MIB // row + 100, 3000, D - 8))
+    assert forms(got, "embedding_lookup_kernel") == [False]
+    for T, rows, k, want in ((16384, 32768, 3, [True, True]), (16383, 32768, 2, [True, False]), (16384, 32767, 5, [False, True]),
+                             (16383, 32767, 1, [False, False])):
+        got, = record(combine(T, k, rows, D))
+        assert forms(got, "expert_combine_kernel") == want
+    for rows, want in ((32768, [True, True]), (32767, [False, True]), (16384, [False, True]), (16383, [False, False])):
+        got, = record(combine_grad(rows // 2, 2, rows, D))
+        assert forms(got, "expert_combine_grad_kernel") == want
+    for T, yes in ((96 * MIB // row, True), (96 * MIB // row - 1, False)):
+        got, = record(table_grad(T, 5000, D))
+        assert forms(got, "window_sum_kernel") == [yes]
