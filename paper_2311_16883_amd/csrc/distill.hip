@@ -189,16 +189,14 @@ struct RawEntry {
   }
 };
 
-// The teacher's logit x as a row's maximum takes it, which drops NaN: NaN counts as +inf there, so that a row with such an entry is none
-// without entries and its shares become NaN.
-__device__ __forceinline__ float as_top(float x) { return x != x ? __builtin_inff() : x; }
-
-// e_j in place of the teacher's logits; returns the lane's sum.  top: their maximum.
+// e_j in place of the teacher's logits; returns the lane's sum.  top: their maximum (without NaN).  The sum over the row is 0 where there are
+// no entries, or none but -inf, and 1 or more elsewhere, or NaN: with NaN or +inf among the logits.
 template <int THREADS>
 __device__ __forceinline__ float weigh_entries(const Distill &a, const Entries &en, float top) {
+  const float base = base_of(top);
   float sum = 0.0f;
   for (int j = threadIdx.x; j < a.K; j += THREADS) {
-    const float e = top == minus_inf() || en.at[j] < 0 ? 0.0f : exp2_of((en.share[j] - top) * a.c);
+    const float e = exp2_of((en.share[j] - base) * a.c);       // (0 for -inf)
     en.share[j] = e;
     sum += e;
   }
@@ -325,7 +323,7 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     entry.take(a, &v, &x);
     en.at[j] = (int32_t)v;
     en.share[j] = x;
-    tm = fmaxf(tm, as_top(x));
+    tm = fmaxf(tm, x);
     return v >= lo && v < hi ? v : lo;
   };
   int64_t z_at = lo;
@@ -337,8 +335,8 @@ __global__ __launch_bounds__(THREADS, R_ <= 8 ? 8 : 4) void distill_row_kernel(D
     if (hi > lo) en.z[j] = elem_to_float<T>(row[v]);
   }
   const float top = group_max<WAVES>(tm, red[0]);
-  const bool none = top == minus_inf();
   const float total = group_sum<WAVES>(weigh_entries<THREADS>(a, en, top), red[1]);
+  const bool none = total == 0.0f;
   if constexpr (MODE & kGrad) merge_entries<THREADS>(a, en, lo, hi);
   if constexpr (L > 0) {
 #pragma unroll
@@ -571,7 +569,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
     en.at[j] = (int32_t)v;
     en.share[j] = x;
     en.z[j] = picked[n * a.K + j];             // (the row's own may be overwritten by other chunks' workgroups by now)
-    tm = fmaxf(tm, as_top(x));
+    tm = fmaxf(tm, x);
   }
   float pm = minus_inf();
   for (int i = t; i < parts_per_row; i += kThreads) pm = fmaxf(pm, parts[n * parts_per_row + i].x);
@@ -584,8 +582,8 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill a, con
   const float s = group_sum<kWaves>(ps, red[1]);
   const float log_s = m == minus_inf() ? __builtin_nanf("") : logf(s);
   const float top = group_max<kWaves>(tm, red[2]);
-  const bool none = top == minus_inf();
   const float total = group_sum<kWaves>(weigh_entries<kThreads>(a, en, top), red[3]);
+  const bool none = total == 0.0f;
   if (blockIdx.x == 0) {
     const float x = group_sum<kWaves>(cross_entries<kThreads>(a, en, m, total), red[4]);
     if (t == 0) {
