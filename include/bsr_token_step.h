@@ -17,10 +17,11 @@
  * buffers (workspaces included) the caller's, work enqueued on `stream`, checks on
  * the host before anything is launched, BSR_ERR_* codes, dtype BSR_F32 or BSR_BF16,
  * matrices row-major with a leading dimension in elements.  Sums are binary32, in an
- * order that depends on the sizes and the data's positions alone, so results are
- * reproducible bit for bit; a bfloat16 result is rounded once, to nearest even, from
- * the binary32 sum.  No kernel reads an input row that it does not need: NaN in rows of
- * padding or of dropped tokens does not spread.
+ * order that depends on the sizes and the data's positions alone (for distillation also
+ * on the address of a row of logits modulo 16 bytes), so results are reproducible bit
+ * for bit; a bfloat16 result is rounded once, to nearest even, from the binary32 sum.
+ * Rows of padding and of dropped tokens have no part in any result, NaN in them
+ * included (some are read all the same).
  * Index arrays of the caller (tokens, expert_ids, ids) are int32 or int64 (index_type);
  * an index outside its range, -1 for instance, means "none" and is never followed.
  */
@@ -135,11 +136,15 @@ int bsr_expert_combine_grad(const void *Ys, int dtype, int64_t rows, int64_t D,
  *   loss[n]   = tau^2 * sum_j q_j * (log q_j - log p[ids_j])          (binary32)
  *   stats[n]  = (m, L): m = max_v z_v, L = log sum_v exp((z_v - m) / tau)   [N x 2], binary32
  *   dlogits[n, v] = dloss[n] * tau * (p_v - sum over j with ids_j == v of q_j), rounded to dtype.
- * An entry with q_j = 0 (a teacher logit of -inf) adds nothing.  A row without entries, or
- * whose entries are all -inf, has the loss 0 and the gradient 0, whatever its logits
- * (its statistics are still those of its logits).  A row with a NaN or +inf logit or with
- * nothing but -inf has no distribution: its L, loss and gradient are NaN.  Logits of -inf
- * or of the type's lowest value otherwise count as p = 0 (loss +inf where q is not 0).
+ * An entry with q_j = 0 adds nothing: a teacher logit of -inf, or one so far below the
+ * row's largest that exp of the difference over tau is less than 2^-126.  A row without
+ * entries, or whose entries are all -inf, has the loss 0 and the gradient 0, whatever its
+ * logits (its statistics are still those of its logits).  A row with a NaN or +inf logit
+ * or with nothing but -inf has no distribution: its L, loss and gradient are NaN.  Logits
+ * of -inf otherwise count as p = 0 (loss +inf where q is not 0).  So do logits of the
+ * type's lowest value in the gradient of a row with larger ones; an entry there costs
+ * tau * q * (m - z), which binary32 holds where tau * q < 1 and rounds to +inf from about
+ * there on.
  * A teacher logit of NaN or +inf makes its row's loss and the gradient at its entries NaN.
  * K = 1 with any finite teacher logit is the cross entropy of a class.
  * K <= 1024 (BSR_ERR_LIMIT beyond).

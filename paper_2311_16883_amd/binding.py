@@ -568,7 +568,8 @@ def bsr_expert_sort(expert_ids: torch.Tensor, experts: int, *, align: int = 1, o
                     counts: Optional[torch.Tensor] = None, order: Optional[torch.Tensor] = None,
                     slots: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """-> (offsets int32 [experts+1], counts int32 [experts], order int32 [rows], slots int32, as expert_ids): entries
-    sorted by expert, every expert's rows from a multiple of align on."""
+    sorted by expert, every expert's rows from a multiple of align on.  (Where none of them is given they are parts of one
+    allocation, which lives as long as any of them: clone what is kept for long.)"""
     r = (_native or _load_native()).expert_sort(expert_ids, experts, align, offsets, counts, order, slots, ws, stream)
     return r if type(r) is not int else _check(r, "bsr_expert_sort")
 
@@ -604,7 +605,8 @@ def bsr_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Ten
                      loss: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
                      ws: Optional[torch.Tensor] = None, stream=None):
     """-> (loss float32 [N], stats float32 [N x 2]): divergence of the student's softmax from the teacher's over its
-    entries (columns ids, logits teacher, both [N x K]), and what bsr_distill_grad needs of the logits."""
+    entries (columns ids, logits teacher, both [N x K]), and what bsr_distill_grad needs of the logits.  (Where neither is
+    given they are parts of one allocation.)"""
     r = (_native or _load_native()).distill_loss(logits, ids, teacher, temperature, loss, stats, ws, stream)
     return r if type(r) is not int else _failed(r, logits, "bsr_distill_loss")
 

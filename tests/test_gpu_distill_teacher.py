@@ -83,3 +83,21 @@ def test_an_entry_at_a_masked_column_costs_infinitely_much_whatever_its_share(dt
         teacher = torch.tensor(t)[None].repeat(N, 1)
         for loss, grad in three_calls(z, ids, teacher, dloss, tau):
             assert bool((loss == INF).all()) and bool(torch.isfinite(grad).all())
+
+
+@pytest.mark.parametrize("dtype,N,V", SHAPES)
+def test_an_entry_at_a_column_of_the_types_lowest_value_costs_what_the_formula_says(dtype, N, V):
+    """tau * q * (m - z) is a binary32 number where tau * q is small enough, and +inf elsewhere."""
+    z, dloss = randn(2, N, V, dtype=dtype), torch.ones(N)
+    ids = torch.arange(2)[None].repeat(N, 1)
+    z[:, 1] = torch.finfo(DT[dtype]).min
+    t = torch.tensor([[0.0, 0.0]]).repeat(N, 1)
+    part = list(range(10))
+    for tau in (1.0, 0.25, 8.0):
+        want, _, grad, e_loss, e_grad = P.distill(f64(z[part]), ids[part].numpy(), f64(t[part]), tau, f64(dloss[part]))
+        for loss, got in three_calls(z, ids, t, dloss, tau):
+            if tau * 0.5 > 1:
+                assert bool((loss == INF).all())
+            else:
+                check(loss[part], want, e_loss)
+            check(got[part], grad, e_grad, dtype)
