@@ -73,9 +73,11 @@ def step(model, batch, k=2, keep=0.5, scale=4.0, temperature=2.0):
     ys = torch.zeros_like(xs)
     for e, rows in part:
         torch.matmul(xs[rows], weights[e], out=ys[rows])
-    masks = B.bsr_score_select_batched(B.SelectBatch([xs[r] for _, r in part], [(BLOCK, BLOCK)] * len(part), [keep] * len(part)))
-    kept = [B.bsr_keep_count(m.numel(), keep) for m in masks]
-    saved = B.bsr_compress_batched(B.CompressBatch([(xs[r], BLOCK, BLOCK, m, n) for (_, r), m, n in zip(part, masks, kept)]))
+    saved = []
+    if part:                                            # (a batch of padding alone has no expert's rows)
+        masks = B.bsr_score_select_batched(B.SelectBatch([xs[r] for _, r in part], [(BLOCK, BLOCK)] * len(part), [keep] * len(part)))
+        kept = [B.bsr_keep_count(m.numel(), keep) for m in masks]
+        saved = B.bsr_compress_batched(B.CompressBatch([(xs[r], BLOCK, BLOCK, m, n) for (_, r), m, n in zip(part, masks, kept)]))
     y = B.bsr_expert_combine(ys, slots, w)
     logits = y @ out
     # backward: the gradient takes the logits' place
@@ -85,7 +87,7 @@ def step(model, batch, k=2, keep=0.5, scale=4.0, temperature=2.0):
     dy = dlogits @ out.t()
     dys, dw = B.bsr_expert_combine_grad(ys, slots, order, w, dy)
     grads = B.bsr_t_dense_matmul_batched(B.MatmulBatch(
-        [(*bsr, r.stop - r.start, dim, BLOCK, BLOCK, dys[r]) for (_, r), bsr in zip(part, saved)]))
+        [(*bsr, r.stop - r.start, dim, BLOCK, BLOCK, dys[r]) for (_, r), bsr in zip(part, saved)])) if part else []
     d_experts = [torch.zeros(dim, dim, device="cuda") for _ in range(experts)]
     dxs = torch.zeros_like(xs)
     for (e, rows), g in zip(part, grads):

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2311_16883_amd import binding as B
+from test_gpu_token_step import example
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +73,22 @@ def test_logits_of_nothing(dtype, N, V, K):
     else:
         assert bool((stats[:, 0] == 1).all()) and bool(((stats[:, 1] - 2.1972246).abs() < 1e-6).all())
     assert not B.bsr_distill_grad(z, ids, t, stats, dloss, dlogits=new(N, V, dtype=dtype)).any()
+
+
+@pytest.mark.parametrize("there", [0, 1])
+def test_training_step_of_hardly_any_token(there):
+    """The example's step where all positions are padding, or all but one: no expert, or two, have rows."""
+    ex = example()
+    model, batch = ex.make_model(300, 64, 4, torch.float32, seed=1), ex.make_batch(40, 300, 8, seed=2)
+    for name, none in (("tokens", -1), ("teacher_ids", -1), ("dloss", 0)):
+        batch[name][there:] = none
+    batch["tokens"][:there] = 7
+    batch["dloss"][:there] = 1.0
+    batch["teacher_ids"][:there] = torch.arange(8, device="cuda")
+    loss, grads = ex.step(model, batch, keep=0.5)
+    assert bool(torch.isfinite(loss)) and (float(loss) > 0) == (there > 0)
+    for n in ("table", "router", "out"):
+        assert bool(torch.isfinite(grads[n]).all()) and bool(grads[n].any()) == (there > 0)
+    assert sum(bool(g.any()) for g in grads["experts"]) == 2 * there
+    rows = torch.nonzero(grads["table"].abs().sum(dim=1))[:, 0].tolist()
+    assert rows == [7] * there
