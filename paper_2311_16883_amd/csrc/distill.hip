@@ -9,9 +9,9 @@
 // for (distill_row_kernel; the longest ones keep a quarter in LDS).  Long rows that are fewer than the compute units are cut into chunks
 // (row_chunks), so that every unit has some: one kernel leaves every chunk's (maximum, sum), the next joins those of its row and writes
 // its chunk of the gradient.  The gradient alone needs no row as a whole and goes by chunks always.
-// [8192 x 50000] bf16: loss 164 us (5.0 TB/s), gradient 299 (5.5), both 314 (5.2; a copy on this GPU 5.1, reading alone 6.2).  Rows
-// that take a compute unit whole pass their reads, arithmetic and writes one after the other, in rounds of as many rows as there are
-// units: [600 x 250007] both 177 us (3.4 TB/s).  Two passes over chunks are slower still (205).
+// [8192 x 50000] bf16, 50 entries: loss 162 us (5.1 TB/s), gradient 302 (5.4), both 311 (5.3; a copy on this GPU 5.1, reading alone 6.2),
+// in the logits' place 321.  Rows that take a compute unit whole pass their reads, arithmetic and writes one after the other, in rounds of
+// as many rows as there are units: [600 x 250007] both 171 us (3.5 TB/s).  Two passes over chunks are slower still (205).
 #include <type_traits>
 
 #include "buffer_access.h"
@@ -217,7 +217,8 @@ __device__ __forceinline__ float cross_entries(const Distill &a, const Entries &
   return sum;
 }
 
-// e_j of all entries of a column in [lo, hi) together, for every one of them; once all e_j are there.
+// e_j of all entries of a column in [lo, hi) together, for every one of them; once all e_j are there.  K comparisons for each: what bounds
+// calls with many entries ([8192 x 50000] bf16, both: 311 us with 50, 437 with 200, 1360 with 1024).
 template <int THREADS>
 __device__ __forceinline__ void merge_entries(const Distill &a, const Entries &en, int64_t lo, int64_t hi) {
   for (int j = threadIdx.x; j < a.K; j += THREADS) {
@@ -750,6 +751,9 @@ int run_both(const DistillArgs &d, const float *dloss, float *loss, float *stats
       return run_chunks<T, GRAD>(rest, dloss + whole, loss + whole, st, static_cast<T *>(dlogits) + whole * ldd, ldd, ws, s);
     }
   }
+  // The loss alone of such rows goes by chunks whatever their number, as its second launch reads no row again ([8 x 131072] bf16, 30 calls
+  // in a row, 10.8 us, with a workgroup per row 12.1, [256 x 131072] 18.3 and 19.7, [2048 x 131072] 106.5 and 132, [1000 x 180000] 73.4 and
+  // 96.4).
   return run_chunks<T, GRAD>(d, dloss, loss, st, dlogits, ldd, ws, s);
 }
 
@@ -765,6 +769,7 @@ int run_grad(const DistillArgs &d, const float *stats, const float *dloss, void 
 
 }  // namespace
 
+// (Of rows of any length, although none of up to 8192 vectors goes by chunks.)
 size_t distill_ws_bytes(int64_t N, int64_t V, int64_t K) {
   (void)V;
   return parts_bytes(N) + align_up((size_t)N * K * sizeof(float), 256);

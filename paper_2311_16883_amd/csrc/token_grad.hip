@@ -16,8 +16,8 @@ namespace bsr {
 namespace {
 
 constexpr int kAhead = 8;
-// dY read past the caches, which then hold more of the dE that was just cleared ([65536 x 1024] bf16 into 65536 rows 121 -> 98 us,
-// [30000 x 2048] 111 -> 92; but [65536 x 512] into 1000 rows 36 -> 38).
+// dY read past the caches, which then hold more of the dE that was just cleared ([65536 x 1024] bf16 into 65536 rows 96.5 -> 92.1 us,
+// into 1000 54.2 -> 51.0, [30000 x 2048] into 100000 185 -> 182, into 32768 95.0 -> 91.5; but [65536 x 512] into 1000 rows 36 -> 38).
 constexpr int64_t kStreamBytes = int64_t(96) << 20;
 constexpr int kGroup = 4;                      // windows whose runs a workgroup of the second kernel joins
 constexpr int kLong = 15;                      // windows of a run from which the waves share it

@@ -22,7 +22,8 @@ constexpr int kMaxBins = 1025;                 // kMaxExperts and the dropped en
 constexpr int kDigitBits = 10;
 constexpr int kFewSteps = 4, kManySteps = 16;  // times 64 entries that a wave takes
 // Workgroups from which each takes kManySteps, as each reads the counts of all ([1048576 x 4] choices of 256 experts, 32 columns, 216 us,
-// 444 with kFewSteps; but [25088 x 4] of 64 17 with kFewSteps and 27.5 with kManySteps).
+// 444 with kFewSteps; but [25088 x 4] of 64 17 with kFewSteps and 27.5 with kManySteps).  That reading grows with the square of the entries,
+// and from millions of them on it is most of the time.
 constexpr int kManyBlocks = 256;
 // Elements that a workgroup clears, or more where that takes more than kClearBlocks workgroups.  Past the caches one store per lane:
 // [65536 x 1024] bf16 into 65536 rows 98.8 us with kClear, 91.9 so, [30000 x 2048] into 100000 198 and 180, [8000 x 1024] into 32768 42.8
