@@ -1,14 +1,14 @@
 // Gradient of the token table: dE[v] (+)= scale * sum of the rows of dY whose token is v, positions ascending.
 //
 // The positions are sorted by token first (token_sort.hip; its launches also clear dE).  The sorted order is cut into windows of
-// 4 to 32 positions, whatever tokens they hold: a wave takes 64 vectors of columns of one window, walks its positions with
-// kAhead rows on their way, and keeps the sum of the current token's rows in registers.  A token whose positions all lie in one
+// 4 to 32 positions (62 of billions), whatever tokens they hold: a wave takes 64 vectors of columns of one window, walks its positions
+// with kAhead rows on their way, and keeps the sum of the current token's rows in registers.  A token whose positions all lie in one
 // window is written to dE straight away; of one that reaches into others every window leaves a partial sum, and a
 // second kernel adds these up window by window.  So the work per wave is the same however often a token occurs, and the order of
 // every sum follows from the tokens alone.  Bound by memory: dY once, dE once, and the rows of dE that occur a second time, as these
 // were cleared before it is known which do.
 // [65536 x 1024] bf16 into 65536 rows 92 us: the sort's four launches clear 268 MB in 46 of them (5.8 TB/s), the windows read 134 MB and write
-// the rows in 41, joining takes 7.  [2999 x 411] binary32 into 10007 16.5 us: three launches that wait for each other, 7 + 5 + 5.
+// the rows in 41, joining takes 7.  [2999 x 411] binary32 into 10007 15.8 us: three launches, each after the last, 7 + 5 + 5.
 #include "token_step.h"
 
 namespace bsr {
@@ -21,7 +21,7 @@ constexpr int kAhead = 8;
 constexpr int64_t kStreamBytes = int64_t(96) << 20;
 constexpr int kGroup = 4;                      // windows whose runs a workgroup of the second kernel joins
 constexpr int kLong = 15;                      // windows of a run from which the waves share it
-constexpr int kLeastWindow = 4;
+constexpr int kLeastWindow = 4, kMostWindow = 62;
 // (waves for each window size: window_size)
 constexpr int64_t kEnoughWaves = 2048, kEnoughLongRuns = 256, kOften = 32;
 constexpr int kThreads = 256;
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void window_sum_kernel(const uint2 *__res
                                                               float *__restrict__ partial, int64_t slices, int size) {
   typedef RowVec<T, VE> R;
   const int lane = threadIdx.x & 63;
-  const int64_t unit = block_number() * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
   const int64_t window = unit / slices, slice = unit - window * slices;
   const int64_t lo = window * size;
   if (lo >= n) return;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const uint2 *__restrict_
   typedef RowVec<float, VE> R;
   __shared__ float parts[kWaves][64 * VE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t block = block_number(), group = block / slices, slice = block - group * slices;
+  const int64_t group = blockIdx.x / slices, slice = blockIdx.x - group * slices;
   // lane l: whether a run starts in window l of the group and goes on behind it, and whose it is
   const int64_t mine = group * kGroup + lane, lo = mine * size, behind = lo + size;
   uint32_t token = V;
@@ -216,8 +216,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const uint2 *__restrict_
 // Positions of a window: 32, or fewer where that leaves too few waves (512 columns of a window each) to hide the loads' latency
 // ([16384 x 768] bf16 into 32768 rows 43 us, 48 with 1024 waves; but [65536 x 512] into 1000 rows 36 and, with 8192 waves, 52).
 // Where rows occur kOften times on the average, most windows leave partial sums, and fewer waves do ([8192 x 384] into 2 rows 50 -> 24,
-// [16384 x 64] binary32 into 50 25 -> 21).
+// [16384 x 64] binary32 into 50 25 -> 21).  Where windows of 32 would be more than 2^31 lanes (a launch takes fewer than 2^32: 2^31 positions of
+// up to 256 columns) they are as long as a wave's lanes hold beside the two neighbours.
 int window_size(int64_t T, int64_t V, int64_t D) {
+  if (ceil_div(T, (int64_t)32) * ceil_div(D, (int64_t)256) * 64 > (int64_t(1) << 31)) return kMostWindow;
   const int64_t enough = T / kOften >= V ? kEnoughLongRuns : kEnoughWaves;
   int size = 32;
   while (size > kLeastWindow && T > size / 2 && ceil_div(T, (int64_t)size) * ceil_div(D, (int64_t)512) < enough) size /= 2;
@@ -248,7 +250,7 @@ int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const v
   const bool read = stream_rows(dY, T, D, lddy, dtype, kStreamBytes);
 #define BSR_CALL_(TY, VE, STREAM)                                                                                              \
   const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
-  hipLaunchKernelGGL((window_sum_kernel<TY, VE, STREAM>), grid_of(ceil_div(windows * slices, (int64_t)(kThreads / 64))),                \
+  hipLaunchKernelGGL((window_sum_kernel<TY, VE, STREAM>), dim3((unsigned)ceil_div(windows * slices, (int64_t)(kThreads / 64))),         \
                      dim3(kThreads), 0, s, sorted, T, (uint32_t)V, static_cast<const TY *>(dY), D, lddy, scale, dE, ldde,      \
                      accumulate, partial, slices, size)
 #define BSR_CALL(TY, VE) \
@@ -264,7 +266,7 @@ int launch_embedding_grad(const void *tokens, int index_type, int64_t T, const v
   if (rc != BSR_OK || windows == 1) return rc;
 #define BSR_JOIN(VE)                                                                                                           \
   const int64_t slices = ceil_div(ceil_div(D, (int64_t)VE), (int64_t)64);                                                      \
-  hipLaunchKernelGGL((join_kernel<VE>), grid_of(ceil_div(windows, (int64_t)kGroup) * slices), dim3(kThreads),                  \
+  hipLaunchKernelGGL((join_kernel<VE>), dim3((unsigned)(ceil_div(windows, (int64_t)kGroup) * slices)), dim3(kThreads),         \
                      0, s, sorted, T, (uint32_t)V, D, scale, dE, ldde, accumulate, partial, windows, slices, size)
   if (D >= 4) { BSR_JOIN(4); } else { BSR_JOIN(1); }
 #undef BSR_JOIN

@@ -21,6 +21,9 @@ constexpr int kAhead = 4;          // vectors that a lane has on their way, per 
 constexpr int64_t kStreamRead = int64_t(64) << 20, kStreamWrite = int64_t(32) << 20;
 constexpr int kChoices = 8;        // choices of a token that are handled together
 
+// The workgroup's number in a grid of two dimensions (the lanes of the first are counted in 32 bits).
+__device__ __forceinline__ int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // out[t] = scale * table[tokens[t]]
 template <typename T, int VE, typename I, bool OUT>
 __global__ __launch_bounds__(kThreads) void embedding_lookup_kernel(const T *__restrict__ table, int64_t V, int64_t D,
@@ -229,6 +232,11 @@ __global__ __launch_bounds__(kThreads) void expert_combine_grad_kernel(
 int row_lanes(int64_t vecs) { return vecs > 32 ? 6 : vecs > 16 ? 5 : 4; }
 
 int64_t row_blocks(int64_t rows, int sh) { return ceil_div(rows << sh, (int64_t)kThreads); }
+
+dim3 grid_of(int64_t blocks) {
+  const int64_t x = blocks < 1 ? 1 : blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22;
+  return dim3((unsigned)x, (unsigned)ceil_div(blocks, x));
+}
 
 // Rows of the sorted matrix that one wave looks over for padding, one after the other: few where there are few rows.
 int padding_rows(int64_t rows) { return rows < 4096 ? 1 : rows < 32768 ? 4 : 16; }

@@ -68,17 +68,7 @@ inline bool stream_rows(const void *p, int64_t rows, int64_t D, int64_t ld, int 
   return (uintptr_t)p % 128 == 0 && D * e % 128 == 0 && ld * e % 128 == 0 && rows * D * e >= least;
 }
 
-// A grid of at least so many workgroups, in two dimensions where there are many: the lanes of the first are counted in 32 bits.  Workgroups
-// beyond the last have to leave.
-inline dim3 grid_of(int64_t blocks) {
-  const int64_t x = blocks < 1 ? 1 : blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22;
-  return dim3((unsigned)x, (unsigned)ceil_div(blocks, x));
-}
-
 // ---- device helpers ----
-
-// The workgroup's number in such a grid.
-__device__ __forceinline__ int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // Index i of an int32 or int64 array, as int64.
 template <typename I>

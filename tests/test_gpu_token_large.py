@@ -227,3 +227,18 @@ def test_the_longest_rows_of_logits_with_the_most_entries(dtype, V):
     want, _, g, el, eg = P.distill(f64(z[part]), ids[part].numpy(), f64(t[part]), float(np.float32(0.9)), f64(dloss[part]))
     check(loss[part], want, el)
     check(grad[part], g, eg, dtype)
+
+
+def test_table_gradient_of_more_than_a_billion_positions():
+    """Windows of the longest kind: a few tokens at either end and around 2^30, nothing in between."""
+    T, V, D = (1 << 30) + 777, 50, 2
+    tokens = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    dY = torch.full((T, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    at = torch.cat([torch.arange(a, a + 3000) for a in (0, (1 << 29) - 1500, (1 << 30) - 2300)]).cuda()
+    tokens[at] = text(len(at), V, "i32", 1).clamp_min(0).clamp_max(V - 1)
+    dY[at] = torch.randint(-8, 9, (len(at), D), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    got = B.bsr_embedding_grad(tokens, dY, V, scale=0.5)
+    want = torch.zeros(V, D, dtype=torch.float64, device="cuda").index_add_(0, tokens[at].long(), dY[at].double() * 0.5)
+    assert torch.equal(got.double(), want)                 # small whole numbers: exact in any order
+    del tokens, dY
+    torch.cuda.empty_cache()
