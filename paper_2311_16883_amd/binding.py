@@ -1,7 +1,7 @@
 """Binding of libbsr_actprune.so -- argument marshalling only.
 
 Every function here has the name of the C entry point it calls (see
-``include/bsr_actprune.h`` and, for the token operators, ``include/bsr_token_step.h``) and does nothing but turn torch tensors into device
+``include/bsr_actprune.h``, for the token operators ``include/bsr_token_step.h``, for the layer operators ``include/bsr_layer_ops.h``) and does nothing but turn torch tensors into device
 pointers, sizes and the current HIP stream, allocate missing output buffers
 with torch, and raise on a non-zero status.  The single-tensor calls do that in
 native code (``csrc/torch_calls.cpp``: they are short, and marshalling in Python
@@ -26,6 +26,8 @@ BSR_OK = 0
 BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_DTYPE, BSR_ERR_KEEP = -1, -2, -3, -4
 BSR_ERR_WORKSPACE, BSR_ERR_ALIGN, BSR_ERR_HIP, BSR_ERR_LIMIT = -5, -6, -7, -8
 BSR_ERR_VALUE = -9
+BSR_ACT_SILU, BSR_ACT_GELU, BSR_ACT_GELU_TANH, BSR_ACT_RELU = 0, 1, 2, 3
+BSR_MOMENTS_F32, BSR_MOMENTS_8BIT = 0, 1
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libbsr_actprune.so"
@@ -47,6 +49,13 @@ TOKEN_EXPORTS = (
     "bsr_expert_sort", "bsr_expert_sort_workspace_bytes", "bsr_expert_gather", "bsr_expert_combine",
     "bsr_expert_combine_grad", "bsr_distill_loss", "bsr_distill_grad", "bsr_distill_loss_grad",
     "bsr_distill_workspace_bytes",
+)
+
+# what include/bsr_layer_ops.h declares
+LAYER_EXPORTS = (
+    "bsr_layer_norm", "bsr_layer_norm_grad", "bsr_layer_norm_grad_workspace_bytes", "bsr_gated_ff",
+    "bsr_gated_ff_workspace_bytes", "bsr_gated_ff_grad", "bsr_gated_ff_grad_workspace_bytes", "bsr_adamw_batched",
+    "bsr_adamw_blocks", "bsr_adamw_state_values",
 )
 
 
@@ -145,6 +154,26 @@ def lib() -> C.CDLL:
     l.bsr_distill_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, flt, vp, vp, vp, i64, vp]
     l.bsr_distill_loss_grad.restype = i32
     l.bsr_distill_loss_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i32, i64, flt, vp, vp, vp, i64, vp, sz, vp]
+    l.bsr_layer_norm.restype = i32
+    l.bsr_layer_norm.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, flt, vp, i64, vp, vp]
+    l.bsr_layer_norm_grad_workspace_bytes.restype = sz
+    l.bsr_layer_norm_grad_workspace_bytes.argtypes = [i64, i64]
+    l.bsr_layer_norm_grad.restype = i32
+    l.bsr_layer_norm_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]
+    l.bsr_gated_ff_workspace_bytes.restype = sz
+    l.bsr_gated_ff_workspace_bytes.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64]
+    l.bsr_gated_ff.restype = i32
+    l.bsr_gated_ff.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, i32, vp, i64, vp, i64, vp, sz, vp]
+    l.bsr_gated_ff_grad_workspace_bytes.restype = sz
+    l.bsr_gated_ff_grad_workspace_bytes.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64]
+    l.bsr_gated_ff_grad.restype = i32
+    l.bsr_gated_ff_grad.argtypes = [vp, i32, i64, i64, i64, vp, i64, i32, vp, i64, i64, vp, i64, vp, i64, vp, sz, vp]
+    l.bsr_adamw_batched.restype = i32
+    l.bsr_adamw_batched.argtypes = [vp, i32, i32, i32, i32, vp, vp]
+    l.bsr_adamw_blocks.restype = i64
+    l.bsr_adamw_blocks.argtypes = [i64]
+    l.bsr_adamw_state_values.restype = i32
+    l.bsr_adamw_state_values.argtypes = [vp, vp, i64, i32, vp, i32, vp]
     l.bsr_static_scratch_init.restype = i32
     l.bsr_static_scratch_init.argtypes = []
     _lib = l
@@ -628,3 +657,179 @@ def bsr_distill_loss_grad(logits: torch.Tensor, ids: torch.Tensor, teacher: torc
 
 def bsr_distill_workspace_bytes(N: int, V: int, K: int) -> int:
     return int(lib().bsr_distill_workspace_bytes(N, V, K))
+
+
+# ---------------------------------------------------------------------------
+# layer operators
+# ---------------------------------------------------------------------------
+
+def bsr_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, *,
+                   eps: float = 1e-5, Y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                   want_stats: bool = False, stream=None):
+    """-> Y [M x D] (which may be X itself), or (Y, stats float32 [M x 2]: mean and 1 / sqrt(variance + eps) of every row,
+    what bsr_layer_norm_grad needs beside X)."""
+    r = (_native or _load_native()).layer_norm(X, gamma, beta, eps, Y, stats, want_stats, stream)
+    return r if type(r) is not int else _failed(r, X, "bsr_layer_norm")
+
+
+def bsr_layer_norm_grad(X: torch.Tensor, gamma: Optional[torch.Tensor], stats: torch.Tensor, dY: torch.Tensor, *,
+                        dX: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
+                        dbeta: Optional[torch.Tensor] = None, want_params: bool = True, accumulate: bool = False,
+                        ws: Optional[torch.Tensor] = None, stream=None):
+    """-> (dX [M x D], dgamma float32 [D], dbeta float32 [D]), or dX alone without want_params.  dX may be dY itself;
+    accumulate adds to dgamma and dbeta."""
+    r = (_native or _load_native()).layer_norm_grad(X, gamma, stats, dY, dX, dgamma, dbeta, want_params, accumulate, ws, stream)
+    return r if type(r) is not int else _failed(r, X, "bsr_layer_norm_grad")
+
+
+def bsr_layer_norm_grad_workspace_bytes(M: int, D: int) -> int:
+    return int(lib().bsr_layer_norm_grad_workspace_bytes(M, D))
+
+
+_ACTS = {"silu": BSR_ACT_SILU, "gelu": BSR_ACT_GELU, "gelu_tanh": BSR_ACT_GELU_TANH, "relu": BSR_ACT_RELU}
+
+
+def _act(act) -> int:
+    if isinstance(act, str):
+        if act not in _ACTS:
+            raise ValueError(f"act must be one of {', '.join(_ACTS)}")
+        return _ACTS[act]
+    return int(act)
+
+
+def bsr_gated_ff(X: torch.Tensor, W: torch.Tensor, *, act="silu", H: Optional[torch.Tensor] = None,
+                 GU: Optional[torch.Tensor] = None, want_GU: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
+    """-> H [M x F] = act(X Wg) * (X Wu) with W [D x 2F] = [Wg | Wu], or (H, GU [M x 2F]: both products, what
+    bsr_gated_ff_grad starts from).  act: "silu", "gelu" (erf), "gelu_tanh", "relu" or a BSR_ACT_* number."""
+    r = (_native or _load_native()).gated_ff(X, W, _act(act), H, GU, want_GU, ws, stream)
+    return r if type(r) is not int else _failed(r, X, "bsr_gated_ff")
+
+
+def bsr_gated_ff_workspace_bytes(X: torch.Tensor, W: torch.Tensor) -> int:
+    """Of bsr_gated_ff on these tensors (their types, extents, strides and addresses; nothing is read)."""
+    M, D, ldx = _dense2d(X, "X")
+    _, F2, ldw = _dense2d(W, "W")
+    return int(lib().bsr_gated_ff_workspace_bytes(_ptr(X), dtype_code(X.dtype), M, D, ldx, _ptr(W), F2 // 2, ldw))
+
+
+def bsr_gated_ff_grad(GU: torch.Tensor, dH: torch.Tensor, W: Optional[torch.Tensor], *, act="silu",
+                      dGU: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None, want_dX: bool = True,
+                      ws: Optional[torch.Tensor] = None, stream=None):
+    """-> (dX [M x D], dGU [M x 2F], which may be GU itself), or dGU alone without want_dX (W may be None then).  The
+    gradient of W is X^T dGU: bsr_t_dense_matmul of the pruned X with dGU as its dY."""
+    r = (_native or _load_native()).gated_ff_grad(GU, dH, W, _act(act), dGU, dX, want_dX, ws, stream)
+    return r if type(r) is not int else _failed(r, GU, "bsr_gated_ff_grad")
+
+
+def bsr_gated_ff_grad_workspace_bytes(dGU: torch.Tensor, W: torch.Tensor) -> int:
+    """Of bsr_gated_ff_grad into this dGU."""
+    M, F2, ldd = _dense2d(dGU, "dGU")
+    D, _, ldw = _dense2d(W, "W")
+    return int(lib().bsr_gated_ff_grad_workspace_bytes(_ptr(dGU), dtype_code(dGU.dtype), M, F2 // 2, ldd, _ptr(W), D, ldw))
+
+
+class _AdamWItem(C.Structure):
+    """Mirror of bsr_adamw_item."""
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("scales", C.c_void_p),
+                ("copy", C.c_void_p), ("n", C.c_int64), ("scales_stride", C.c_int64), ("weight_decay", C.c_float)]
+
+
+class AdamWBatch:
+    """The marshalled tensors of bsr_adamw_batched: build it once for tensors that stay where they are and pass it again every
+    step.  Holds references to them.  params, grads: contiguous tensors of any shape, all params of one dtype and all grads of one;
+    bits: 32 or 8, the moments' size; states: for every tensor (m, v) float32, or (m, v, scales) uint8 with scales [2 x
+    bsr_adamw_blocks(n)] (v holds the codes of its root; see include/bsr_layer_ops.h) -- made as zeros where not given; copies: bfloat16 tensors that receive the new params too
+    (None: none); weight_decay: a number, or one for every tensor."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, bits: int = 32,
+                 states: Optional[Sequence[tuple]] = None, copies: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 weight_decay=0.0):
+        n = len(params)
+        if n == 0 or len(grads) != n:
+            raise ValueError("one grad per param, and at least one")
+        if bits not in (8, 32):
+            raise ValueError("moments are held in 8 or 32 bits")
+        decays = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        copies = [None] * n if copies is None else list(copies)
+        if len(decays) != n or len(copies) != n or (states is not None and len(states) != n):
+            raise ValueError("one entry per param")
+        self.param_code, self.grad_code = dtype_code(params[0].dtype), dtype_code(grads[0].dtype)
+        self.device = params[0].device
+        self.bits, self.moments = bits, BSR_MOMENTS_8BIT if bits == 8 else BSR_MOMENTS_F32
+        if states is None:
+            states = []
+            for p in params:
+                if bits == 32:
+                    states.append((torch.zeros(p.shape, device=p.device), torch.zeros(p.shape, device=p.device)))
+                else:
+                    states.append((torch.zeros(p.shape, dtype=torch.uint8, device=p.device),
+                                   torch.zeros(p.shape, dtype=torch.uint8, device=p.device),
+                                   torch.zeros(2, bsr_adamw_blocks(p.numel()), dtype=torch.uint8, device=p.device)))
+        self.params, self.grads, self.states, self.copies = list(params), list(grads), [tuple(s) for s in states], copies
+        self.items = (_AdamWItem * n)()
+        places = []                                   # (first byte, end, whether it is written)
+
+        def flat(t, what, dtype, count):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != self.device:
+                raise ValueError(f"{what} must be tensors on one device")
+            if not t.is_contiguous() or t.dtype != dtype or t.numel() != count:
+                raise ValueError(f"{what} must be contiguous, {dtype}, and as large as its param")
+            if count:
+                places.append((t.data_ptr(), t.data_ptr() + count * t.element_size(), what != "grads"))
+            return _ptr(t)
+
+        for i, (p, g, s, c) in enumerate(zip(self.params, self.grads, self.states, copies)):
+            count = p.numel()
+            item = self.items[i]
+            item.param, item.grad = flat(p, "params", params[0].dtype, count), flat(g, "grads", grads[0].dtype, count)
+            item.copy = flat(c, "copies", torch.bfloat16, count) if c is not None else None
+            if len(s) != (2 if bits == 32 else 3):
+                raise ValueError("a state is (m, v), with 8 bits (m, v, scales)")
+            kind = torch.float32 if bits == 32 else torch.uint8
+            item.m, item.v = flat(s[0], "moments", kind, count), flat(s[1], "moments", kind, count)
+            if bits == 8:
+                scales, blocks = s[2], bsr_adamw_blocks(count)
+                if not scales.is_cuda or scales.device != self.device or scales.dtype != torch.uint8 or \
+                        tuple(scales.shape) != (2, blocks) or (blocks > 1 and scales.stride(1) != 1) or \
+                        (blocks > 0 and scales.stride(0) < blocks):
+                    raise ValueError("scales must be uint8 [2, bsr_adamw_blocks(n)] on the device, rows contiguous")
+                item.scales, item.scales_stride = _ptr(scales), scales.stride(0)
+                for row in range(2 if blocks else 0):
+                    at = scales.data_ptr() + row * scales.stride(0)
+                    places.append((at, at + blocks, True))
+            item.n, item.weight_decay = count, decays[i]
+        self.n = n
+        places.sort()
+        end = written = 0                             # of what lies before, of what is written before
+        for a, b, w in places:
+            if a < (end if w else written):
+                raise ValueError("tensors of a step overlap")
+            end, written = max(end, b), max(written, b) if w else written
+
+
+def bsr_adamw_batched(batch: AdamWBatch, *, lr, step, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                      grad_scale=1.0, seed: int = 0, stream=None) -> None:
+    """One AdamW step over the batch's tensors, in place.  lr, step (1 for the first) and grad_scale (multiplies every gradient)
+    are numbers, or tensors of one element on the device (float32, int64, float32) that the kernels read, for steps captured
+    into a graph; seed names the random numbers by which 8-bit moments are rounded."""
+    code = (_native or _load_native()).adamw_batched(batch.params[0], C.addressof(batch.items), batch.n, batch.param_code,
+                                                     batch.grad_code, batch.moments, lr, step, beta1, beta2, eps, grad_scale, seed,
+                                                     stream)
+    _check(code, "bsr_adamw_batched")
+
+
+def bsr_adamw_blocks(n: int) -> int:
+    """Scale bytes of n elements of an 8-bit moment."""
+    blocks = int(lib().bsr_adamw_blocks(n))
+    if blocks < 0:
+        raise BsrError(BSR_ERR_SHAPE, "bsr_adamw_blocks")
+    return blocks
+
+
+def bsr_adamw_state_values(codes: torch.Tensor, scales: torch.Tensor, which: str, *, dtype: torch.dtype = torch.float32,
+                           out: Optional[torch.Tensor] = None, stream=None):
+    """-> what 8-bit moments stand for, as codes: which is "m", or "r" for the root of v; scales is that moment's row."""
+    if which not in ("m", "r"):
+        raise ValueError('which must be "m" or "r"')
+    r = (_native or _load_native()).adamw_state_values(codes, scales, 0 if which == "m" else 1, out, dtype_code(dtype), stream)
+    return r if type(r) is not int else _check(r, "bsr_adamw_state_values")

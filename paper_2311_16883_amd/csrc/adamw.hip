@@ -1,0 +1,336 @@
+// One AdamW step over many tensors, moments in binary32 or in 8 bits.
+//
+// Bound by memory: 28 bytes per element with binary32 weights, gradients and moments, 16 with 8-bit moments.  The tensors of a call
+// are cut into chunks of 128-element blocks, a chunk to a workgroup; the list of tensors travels in the kernel's arguments, so
+// there is nothing to copy or to keep for the device.  A lane holds four consecutive elements of a block, 32 lanes a block, whose largest magnitudes
+// meet by lane exchanges.
+//
+// 8-bit moments: codes of 4 exponent bits in units of a power of two per block, so that scaling is exact and a value fits bfloat16.
+// sqrt(v) is held in place of v: half the range in the exponent, and the update needs the root anyway.  Rounding is to one of the two
+// neighbours with the probability of the distances, by bits of a counter hash: with beta2 = 0.999 a step changes sqrt(v) by 0.05 % of
+// itself, its codes are 3 to 6 % apart, and to nearest it would never move.  A positive root does not become 0, since the first moment
+// beside it may be larger than its smallest code and would be divided by eps.
+#include <algorithm>
+#include <cmath>
+
+#include "layer_ops.h"
+
+namespace bsr {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPerLane = 4;
+constexpr int kRound = kThreads * kPerLane;            // elements of a round of the workgroup: 8 blocks
+constexpr int kRounds = 4;                             // rounds of a chunk
+constexpr int64_t kChunk = (int64_t)kRound * kRounds;
+constexpr int kItems = 40;                             // tensors per launch: their list is 3.5 KB of arguments
+
+struct Item {
+  void *param;
+  const void *grad;
+  void *m, *v;
+  uint8_t *scale_m, *scale_v;
+  uint16_t *copy;
+  int64_t n, first;                                    // elements; number of the first one in the whole list
+  float decay;
+};
+struct Options {
+  float lr, b1, c1, b2, c2, eps, grad_scale;           // c = 1 - b
+  float first_full, root;                              // 1 / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
+  uint32_t key;
+  double beta1, beta2;
+  const float *lr_device, *grad_scale_device;
+  const int64_t *step_device;
+  uint64_t seed;
+};
+struct List {
+  Item it[kItems];
+  uint32_t chunk_begin[kItems + 1];
+  Options o;
+};
+
+__host__ __device__ inline uint32_t mix(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x85A308D3u;
+  x = (x ^ (x >> 15)) * 0xA4093823u;
+  return x ^ (x >> 16);
+}
+__host__ __device__ inline uint32_t key_of(uint64_t seed, int64_t step) {
+  return mix(mix((uint32_t)seed + 0x9E3779B1u * (uint32_t)step) ^ (uint32_t)(seed >> 32));
+}
+__host__ __device__ inline double power(double b, int64_t n) {
+  double r = 1.0;
+  for (; n > 0; n >>= 1, b *= b)
+    if (n & 1) r *= b;
+  return r;
+}
+__host__ __device__ inline void step_numbers(Options &o, int64_t step) {
+  o.first_full = (float)(1.0 / (1.0 - power(o.beta1, step)));
+  o.root = (float)(1.0 / sqrt(1.0 - power(o.beta2, step)));
+  o.key = key_of(o.seed, step);
+}
+
+// Four numbers from element i on; `left` of them are there.
+template <typename T>
+struct Any4 {
+  typedef uint32_t __attribute__((ext_vector_type(sizeof(T)))) Words;      // 4 * sizeof(T) bytes
+  struct __attribute__((packed, aligned(1))) Loose { Words w; };
+};
+template <>
+struct Any4<uint8_t> {
+  typedef uint32_t Words;
+  struct __attribute__((packed, aligned(1))) Loose { Words w; };
+};
+template <typename T>
+__device__ __forceinline__ void load4(const T *p, int left, T *out) {
+  if (left >= 4) {
+    const auto w = reinterpret_cast<const typename Any4<T>::Loose *>(p)->w;
+    __builtin_memcpy(out, &w, 4 * sizeof(T));
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) out[q] = q < left ? p[q] : (T)0;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T *p, int left, const T *v) {
+  if (left >= 4) {
+    typename Any4<T>::Words w;
+    __builtin_memcpy(&w, v, 4 * sizeof(T));
+    reinterpret_cast<typename Any4<T>::Loose *>(p)->w = w;
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (q < left) p[q] = v[q];
+  }
+}
+
+// The magnitude that a code stands for, in the block's units of 2^(scale - 127 - 14 - BITS); scale 255: NaN.
+template <int BITS>
+__device__ __forceinline__ float decode(uint32_t magnitude, uint32_t scale) {
+  const uint32_t e = magnitude >> BITS, f = magnitude & ((1u << BITS) - 1u);
+  const uint32_t n = e != 0u ? f + (1u << BITS) : f;
+  const float x = ldexpf((float)n, (int)scale - (127 + 14 + BITS) + (e != 0u ? (int)e - 1 : 0));
+  return scale == 255u ? __uint_as_float(0x7FC00000u) : x;
+}
+
+// The scale byte of a block whose largest magnitude has these bits: the exponent of the smallest power of two above which the
+// largest code lies.
+template <int BITS>
+__device__ __forceinline__ uint32_t scale_of(uint32_t most) {
+  const uint32_t b = (most + (0x7FFFFFu >> (BITS + 0))) >> 23;
+  return b < 32u ? 0u : b > 255u ? 255u : b;
+}
+
+// |x| rounded to one of its two neighbours by u in [0, 1).
+template <int BITS>
+__device__ __forceinline__ uint32_t encode(float a, uint32_t scale, float u) {
+  const int least = (int)scale - (127 + 14 + BITS);
+  const int own = (int)(__float_as_uint(a) >> 23) - 127 - BITS;
+  const int ex = max(own, least);
+  uint32_t n = (uint32_t)floorf(ldexpf(a, -ex) + u);
+  if (BITS == 4 && a > 0.0f) n = max(n, 1u);
+  const uint32_t code = min(n + ((uint32_t)(ex - least) << BITS), BITS == 3 ? 127u : 255u);
+  return scale == 0u || scale == 255u ? 0u : code;
+}
+
+template <typename P, typename G, bool SMALL, bool COPY>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
+  // this workgroup's tensor
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (blockIdx.x >= list.chunk_begin[mid]) lo = mid;
+    else hi = mid;
+  }
+  const Item &it = list.it[lo];
+  const int64_t chunk0 = (int64_t)(blockIdx.x - list.chunk_begin[lo]) * kChunk;
+  Options o = list.o;
+  if (o.step_device != nullptr) step_numbers(o, *o.step_device);
+  if (o.lr_device != nullptr) o.lr = *o.lr_device;
+  if (o.grad_scale_device != nullptr) o.grad_scale = *o.grad_scale_device;
+  P *const param = static_cast<P *>(it.param);
+  const G *const grad = static_cast<const G *>(it.grad);
+  const float keep = 1.0f - o.lr * it.decay, rate = o.lr * o.first_full;
+  for (int r = 0; r < kRounds; ++r) {
+    const int64_t i = chunk0 + (int64_t)r * kRound + threadIdx.x * kPerLane;
+    if (chunk0 + (int64_t)r * kRound >= it.n) break;
+    const int left = it.n - i >= 4 ? 4 : it.n > i ? (int)(it.n - i) : 0;
+    P p0[4];
+    G g0[4];
+    float m[4], root[4], p[4];
+    load4(param + i, left, p0);
+    load4(grad + i, left, g0);
+    const int64_t block = i / kMomentBlock;
+    if constexpr (SMALL) {
+      uint8_t cm[4], cv[4];
+      load4(static_cast<const uint8_t *>(it.m) + i, left, cm);
+      load4(static_cast<const uint8_t *>(it.v) + i, left, cv);
+      const uint32_t sm = left > 0 ? it.scale_m[block] : 0u, sv = left > 0 ? it.scale_v[block] : 0u;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        m[q] = decode<3>(cm[q] & 127u, sm);
+        m[q] = (cm[q] & 128u) ? -m[q] : m[q];
+        root[q] = decode<4>(cv[q], sv);
+      }
+    } else {
+      load4(static_cast<const float *>(it.m) + i, left, m);
+      load4(static_cast<const float *>(it.v) + i, left, root);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float g = elem_to_float<G>(g0[q]) * o.grad_scale;
+      m[q] = o.b1 * m[q] + o.c1 * g;
+      const float v = o.b2 * (SMALL ? root[q] * root[q] : root[q]) + o.c2 * g * g;
+      const float rt = sqrtf(v);
+      p[q] = elem_to_float<P>(p0[q]) * keep - rate * m[q] / (rt * o.root + o.eps);
+      root[q] = SMALL ? rt : v;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) p0[q] = from_float<P>(p[q]);
+    store4(param + i, left, p0);
+    if constexpr (COPY) {
+      uint16_t c[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) c[q] = from_float<uint16_t>(p[q]);
+      store4(it.copy + i, left, c);
+    }
+    if constexpr (SMALL) {
+      uint32_t most_m = 0u, most_v = 0u;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bool there = q < left;
+        most_m = max(most_m, there ? __float_as_uint(m[q]) & 0x7FFFFFFFu : 0u);
+        most_v = max(most_v, there ? __float_as_uint(root[q]) & 0x7FFFFFFFu : 0u);
+      }
+      const uint32_t sm = scale_of<3>(group_max<5>(most_m)), sv = scale_of<4>(group_max<5>(most_v));
+      uint8_t cm[4], cv[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint64_t number = (uint64_t)(it.first + i + q);
+        const uint32_t h = mix((uint32_t)number * 0x9E3779B1u + (uint32_t)(number >> 32) * 0x7F4A7C15u + o.key);
+        const float a = fabsf(m[q]);
+        const uint32_t c = encode<3>(a, sm, (float)(h & 0xFFFFu) * 0x1p-16f);
+        cm[q] = (uint8_t)(c != 0u && m[q] < 0.0f ? c + 128u : c);
+        cv[q] = (uint8_t)encode<4>(root[q], sv, (float)(h >> 16) * 0x1p-16f);
+      }
+      store4(static_cast<uint8_t *>(it.m) + i, left, cm);
+      store4(static_cast<uint8_t *>(it.v) + i, left, cv);
+      if (threadIdx.x % (kMomentBlock / kPerLane) == 0 && left > 0) {
+        it.scale_m[block] = (uint8_t)sm;
+        it.scale_v[block] = (uint8_t)sv;
+      }
+    } else {
+      store4(static_cast<float *>(it.m) + i, left, m);
+      store4(static_cast<float *>(it.v) + i, left, root);
+    }
+  }
+}
+
+template <typename T, int BITS>
+__global__ __launch_bounds__(kThreads) void state_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+                                                                int64_t n, T *__restrict__ out) {
+  for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * kRound) {
+    const int left = n - i >= 4 ? 4 : (int)(n - i);
+    uint8_t c[4];
+    load4(codes + i, left, c);
+    const uint32_t scale = scales[i / kMomentBlock];
+    T v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float a = decode<BITS>(BITS == 3 ? c[q] & 127u : c[q], scale);
+      v[q] = from_float<T>(BITS == 3 && (c[q] & 128u) ? -a : a);
+    }
+    store4(out + i, left, v);
+  }
+}
+
+template <typename P, typename G, bool SMALL, bool COPY>
+void launch_list(const List &list, int n, uint32_t chunks, hipStream_t s) {
+  adamw_kernel<P, G, SMALL, COPY><<<dim3(chunks), kThreads, 0, s>>>(list, n);
+}
+
+}  // namespace
+
+int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_dtype, int moments, const bsr_adamw_options &opt,
+                 hipStream_t s) {
+  List list;
+  Options &o = list.o;
+  o.b1 = (float)opt.beta1;
+  o.c1 = (float)(1.0 - opt.beta1);
+  o.b2 = (float)opt.beta2;
+  o.c2 = (float)(1.0 - opt.beta2);
+  o.eps = (float)opt.eps;
+  o.grad_scale = (float)opt.grad_scale;
+  o.beta1 = opt.beta1;
+  o.beta2 = opt.beta2;
+  o.seed = opt.seed;
+  o.lr_device = opt.lr_device;
+  o.grad_scale_device = opt.grad_scale_device;
+  o.step_device = opt.step_device;
+  o.lr = (float)opt.lr;
+  step_numbers(o, opt.step);
+  const bool small = moments == BSR_MOMENTS_8BIT;
+  int64_t first = 0;
+  int held = 0;
+  bool copies = false;
+  uint32_t chunks = 0;
+  auto flush = [&]() {
+    if (held == 0) return (int)BSR_OK;
+    list.chunk_begin[held] = chunks;
+    auto go = [&](auto p, auto g) {
+      typedef decltype(p) P;
+      typedef decltype(g) G;
+      if (small) copies ? launch_list<P, G, true, true>(list, held, chunks, s) : launch_list<P, G, true, false>(list, held, chunks, s);
+      else copies ? launch_list<P, G, false, true>(list, held, chunks, s) : launch_list<P, G, false, false>(list, held, chunks, s);
+    };
+    if (param_dtype == BSR_F32) grad_dtype == BSR_F32 ? go(float(), float()) : go(float(), uint16_t());
+    else grad_dtype == BSR_F32 ? go(uint16_t(), float()) : go(uint16_t(), uint16_t());
+    held = 0;
+    chunks = 0;
+    return check_launch();
+  };
+  for (int i = 0; i < n; ++i) {
+    const bsr_adamw_item &x = items[i];
+    if (x.n > 0) {
+      // chunks of a launch: its lanes are counted in 32 bits; a tensor beyond that goes in parts of whole blocks
+      constexpr int64_t kMostChunks = int64_t(1) << 23;
+      for (int64_t at = 0; at < x.n; at += kMostChunks * kChunk) {
+        const int64_t part = std::min(x.n - at, kMostChunks * kChunk), needs = ceil_div(part, kChunk);
+        const bool copy = x.copy != nullptr;
+        if (held == kItems || (held > 0 && (copy != copies || chunks + needs > kMostChunks)))
+          if (const int rc = flush(); rc != BSR_OK) return rc;
+        copies = copy;
+        const int64_t pe = elem_bytes(param_dtype) * at, ge = elem_bytes(grad_dtype) * at, me = (small ? 1 : 4) * at;
+        Item &it = list.it[held];
+        it.param = static_cast<char *>(x.param) + pe;
+        it.grad = static_cast<const char *>(x.grad) + ge;
+        it.m = static_cast<char *>(x.m) + me;
+        it.v = static_cast<char *>(x.v) + me;
+        it.scale_m = small ? x.scales + at / kMomentBlock : nullptr;
+        it.scale_v = small ? x.scales + x.scales_stride + at / kMomentBlock : nullptr;
+        it.copy = copy ? static_cast<uint16_t *>(x.copy) + at : nullptr;
+        it.n = part;
+        it.first = first + at;
+        it.decay = x.weight_decay;
+        list.chunk_begin[held++] = chunks;
+        chunks += (uint32_t)needs;
+      }
+    }
+    first += ceil_div(x.n, (int64_t)kMomentBlock) * kMomentBlock;
+  }
+  return flush();
+}
+
+int launch_adamw_state_values(const uint8_t *codes, const uint8_t *scales, int64_t n, int which, void *out, int dtype, hipStream_t s) {
+  const dim3 grid((uint32_t)std::min(ceil_div(n, (int64_t)kRound), int64_t(1) << 23));
+  if (dtype == BSR_F32) {
+    if (which == 0) state_values_kernel<float, 3><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<float *>(out));
+    else state_values_kernel<float, 4><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<float *>(out));
+  } else {
+    if (which == 0) state_values_kernel<uint16_t, 3><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<uint16_t *>(out));
+    else state_values_kernel<uint16_t, 4><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<uint16_t *>(out));
+  }
+  return check_launch();
+}
+
+}  // namespace bsr

@@ -23,6 +23,7 @@
 
 #include "bsr_actprune.h"
 #include "bsr_token_step.h"
+#include "bsr_layer_ops.h"
 
 namespace {
 
@@ -694,6 +695,208 @@ PyObject *distill_loss_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- layer operators ----
+
+// gamma or beta of a norm over D columns: null for None.
+const at::Tensor *norm_param(PyObject *o, const char *what, const at::Tensor &like, int64_t D) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor &t = packed(o, what, like);
+  if (t.dim() != 1 || t.size(0) != D) value_error(std::string(what) + " must be 1-D, a number for each column");
+  return &t;
+}
+
+// (X, gamma or None, beta or None, eps, Y, stats, want_stats, stream) -> Y or (Y, stats)
+PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &X = tensor(a[0], "X");
+    const Dense x = dense2d(X, "X");
+    const at::Tensor *gamma = norm_param(a[1], "gamma", X, x.cols), *beta = norm_param(a[2], "beta", X, x.cols);
+    if (gamma != nullptr && beta != nullptr && gamma->scalar_type() != beta->scalar_type()) value_error("gamma and beta differ in dtype");
+    const double eps = real(a[3]);
+    const bool with_stats = a[5] != Py_None || truth(a[6]);
+    const at::Tensor *param = gamma != nullptr ? gamma : beta;
+    const int code = dtype_code(X), pcode = param != nullptr ? dtype_code(*param) : BSR_F32;
+    if (code < 0 || pcode < 0) return code_result(BSR_ERR_DTYPE);
+    const CallStream stream(a[7], X);
+    int64_t ldy;
+    const Output Y = matrix_output(a[4], "Y", x.rows, x.cols, X.scalar_type(), X, &ldy);
+    Output stats;
+    if (with_stats) stats = packed_output(a[5], "stats", {x.rows, 2}, at::kFloat, X);
+    const int rc = released([&] {
+      return bsr_layer_norm(pointer(X), code, x.rows, x.cols, x.ld, gamma != nullptr ? pointer(*gamma) : nullptr,
+                            beta != nullptr ? pointer(*beta) : nullptr, pcode, (float)eps, pointer(Y.get()), ldy,
+                            with_stats ? typed<float>(stats.get()) : nullptr, stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return with_stats ? Py_BuildValue("(NN)", Y.result(), stats.result()) : Y.result();
+  });
+}
+
+// (X, gamma or None, stats, dY, dX, dgamma, dbeta, want_params, accumulate, ws, stream) -> (dX, dgamma, dbeta) or dX
+PyObject *layer_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 11)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &X = tensor(a[0], "X"), &dY = tensor(a[3], "dY");
+    const Dense x = dense2d(X, "X"), y = matrix_like(dY, "dY", X);
+    if (y.rows != x.rows || y.cols != x.cols) value_error("dY must have the shape of X");
+    const at::Tensor *gamma = norm_param(a[1], "gamma", X, x.cols);
+    const at::Tensor &stats = packed(a[2], "stats", X, at::kFloat, {x.rows, 2});
+    const bool params = truth(a[7]), accumulate = truth(a[8]);
+    if (!params && (a[5] != Py_None || a[6] != Py_None)) value_error("dgamma and dbeta are not wanted");
+    if (accumulate && params && (a[5] == Py_None || a[6] == Py_None)) value_error("accumulate needs existing dgamma and dbeta");
+    const int code = dtype_code(X), pcode = gamma != nullptr ? dtype_code(*gamma) : BSR_F32;
+    if (code < 0 || pcode < 0) return code_result(BSR_ERR_DTYPE);
+    const CallStream stream(a[10], X);
+    int64_t ldx;
+    const Output dX = matrix_output(a[4], "dX", x.rows, x.cols, X.scalar_type(), X, &ldx);
+    Output dgamma, dbeta;
+    if (params && a[5] == Py_None && a[6] == Py_None) {
+      const at::Tensor both = new_tensor({2 * x.cols}, at::kFloat, X);
+      dgamma.own = part_of(both, 0, {x.cols});
+      dbeta.own = part_of(both, x.cols, {x.cols});
+    } else if (params) {
+      dgamma = packed_output(a[5], "dgamma", {x.cols}, at::kFloat, X);
+      dbeta = packed_output(a[6], "dbeta", {x.cols}, at::kFloat, X);
+    }
+    const Workspace ws = token_workspace(a[9], [&] { return params ? bsr_layer_norm_grad_workspace_bytes(x.rows, x.cols) : 0; }, X);
+    const int rc = released([&] {
+      return bsr_layer_norm_grad(pointer(X), code, x.rows, x.cols, x.ld, gamma != nullptr ? pointer(*gamma) : nullptr, pcode,
+                                 typed<float>(stats), pointer(dY), y.ld, pointer(dX.get()), ldx,
+                                 params ? typed<float>(dgamma.get()) : nullptr, params ? typed<float>(dbeta.get()) : nullptr,
+                                 accumulate ? 1 : 0, ws.p, ws.bytes, stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return params ? Py_BuildValue("(NNN)", dX.result(), dgamma.result(), dbeta.result()) : dX.result();
+  });
+}
+
+// The weights of a gated block: [D x 2F].
+Dense gated_weights(const at::Tensor &W, const at::Tensor &like) {
+  const Dense w = matrix_like(W, "W", like);
+  if (w.cols % 2 != 0) value_error("W must have two columns for each of H: the gate's, then the other projection's");
+  return w;
+}
+
+// (X, W, act, H, GU, want_GU, ws, stream) -> H or (H, GU)
+PyObject *gated_ff(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &X = tensor(a[0], "X"), &W = tensor(a[1], "W");
+    const Dense x = dense2d(X, "X"), w = gated_weights(W, X);
+    if (w.rows != x.cols) value_error("W must have a row for each column of X");
+    const int act = (int)integer(a[2]);
+    const int64_t F = w.cols / 2;
+    const bool save = a[4] != Py_None || truth(a[5]);
+    const int code = dtype_code(X);
+    if (code < 0) return code_result(code);
+    const CallStream stream(a[7], X);
+    int64_t ldh, ldgu = 0;
+    const Output H = matrix_output(a[3], "H", x.rows, F, X.scalar_type(), X, &ldh);
+    Output GU;
+    if (save) GU = matrix_output(a[4], "GU", x.rows, 2 * F, X.scalar_type(), X, &ldgu);
+    const Workspace ws = token_workspace(
+        a[6], [&] { return bsr_gated_ff_workspace_bytes(pointer(X), code, x.rows, x.cols, x.ld, pointer(W), F, w.ld); }, X);
+    const int rc = released([&] {
+      return bsr_gated_ff(pointer(X), code, x.rows, x.cols, x.ld, pointer(W), F, w.ld, act, pointer(H.get()), ldh,
+                          save ? pointer(GU.get()) : nullptr, ldgu, ws.p, ws.bytes, stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return save ? Py_BuildValue("(NN)", H.result(), GU.result()) : H.result();
+  });
+}
+
+// (GU, dH, W, act, dGU, dX, want_dX, ws, stream) -> (dX, dGU) or dGU
+PyObject *gated_ff_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 9)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &GU = tensor(a[0], "GU"), &dH = tensor(a[1], "dH");
+    const Dense gu = dense2d(GU, "GU"), h = matrix_like(dH, "dH", GU);
+    if (gu.cols != 2 * h.cols || gu.rows != h.rows) value_error("GU must have the rows of dH and twice its columns");
+    const int act = (int)integer(a[3]);
+    const bool with_x = truth(a[6]);
+    if (!with_x && a[5] != Py_None) value_error("dX is not wanted");
+    const at::Tensor *W = with_x ? &tensor(a[2], "W") : nullptr;
+    Dense w{0, gu.cols, gu.cols};
+    if (with_x) {
+      w = gated_weights(*W, GU);
+      if (w.cols != gu.cols) value_error("W must have the columns of GU");
+    }
+    const int code = dtype_code(GU);
+    if (code < 0) return code_result(code);
+    const CallStream stream(a[8], GU);
+    int64_t ldd, ldx = 0;
+    const Output dGU = matrix_output(a[4], "dGU", gu.rows, gu.cols, GU.scalar_type(), GU, &ldd);
+    Output dX;
+    if (with_x) dX = matrix_output(a[5], "dX", gu.rows, w.rows, GU.scalar_type(), GU, &ldx);
+    const Workspace ws = token_workspace(
+        a[7],
+        [&] {
+          return with_x ? bsr_gated_ff_grad_workspace_bytes(pointer(dGU.get()), code, gu.rows, h.cols, ldd, pointer(*W), w.rows, w.ld) : 0;
+        },
+        GU);
+    const int rc = released([&] {
+      return bsr_gated_ff_grad(pointer(GU), code, gu.rows, h.cols, gu.ld, pointer(dH), h.ld, act, with_x ? pointer(*W) : nullptr, w.rows,
+                               w.ld, pointer(dGU.get()), ldd, with_x && w.rows > 0 ? pointer(dX.get()) : nullptr, ldx, ws.p, ws.bytes,
+                               stream.handle());
+    });
+    if (rc != BSR_OK) return code_result(rc);
+    return with_x ? Py_BuildValue("(NN)", dX.result(), dGU.result()) : dGU.result();
+  });
+}
+
+// A number of an optimizer step: a Python number, or one element on the device.
+template <typename T>
+const T *device_number(PyObject *o, const char *what, const at::Tensor &like, at::ScalarType type) {
+  if (!THPVariable_Check(o)) return nullptr;
+  const at::Tensor &t = packed(o, what, like);
+  if (t.scalar_type() != type || t.numel() != 1) value_error(std::string(what) + " on the device must be one number of type " + c10::toString(type));
+  return typed<T>(t);
+}
+
+// (like, address of the items, items, param code, grad code, moments, lr, step, beta1, beta2, eps, grad_scale, seed, stream) -> code
+PyObject *adamw_batched(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 14)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &like = tensor(a[0], "params");
+    const auto *items = static_cast<const bsr_adamw_item *>(PyLong_AsVoidPtr(a[1]));
+    bsr_adamw_options o = {};
+    o.lr_device = device_number<float>(a[6], "lr", like, at::kFloat);
+    o.step_device = device_number<int64_t>(a[7], "step", like, at::kLong);
+    o.grad_scale_device = device_number<float>(a[11], "grad_scale", like, at::kFloat);
+    o.lr = o.lr_device != nullptr ? 0.0 : real(a[6]);
+    o.step = o.step_device != nullptr ? 1 : integer(a[7]);
+    o.beta1 = real(a[8]);
+    o.beta2 = real(a[9]);
+    o.eps = real(a[10]);
+    o.grad_scale = o.grad_scale_device != nullptr ? 1.0 : real(a[11]);
+    o.seed = PyLong_AsUnsignedLongLong(a[12]);
+    if (PyErr_Occurred()) throw PythonError();
+    const int count = (int)integer(a[2]), param = (int)integer(a[3]), grad = (int)integer(a[4]), moments = (int)integer(a[5]);
+    const CallStream stream(a[13], like);
+    return code_result(released([&] { return bsr_adamw_batched(items, count, param, grad, moments, &o, stream.handle()); }));
+  });
+}
+
+// (codes, scales, which, out, dtype, stream) -> out
+PyObject *adamw_state_values(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 6)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const at::Tensor &codes = tensor(a[0], "codes");
+    if (!codes.is_cuda() || codes.scalar_type() != at::kByte || !codes.is_contiguous()) value_error("codes must be a contiguous uint8 tensor on the device");
+    const int64_t count = codes.numel();
+    const at::Tensor &scales = packed(a[1], "scales", codes, at::kByte, {bsr_adamw_blocks(count)});
+    const int which = (int)integer(a[2]), code = (int)integer(a[4]);
+    if (code != BSR_F32 && code != BSR_BF16) return code_result(BSR_ERR_DTYPE);
+    const CallStream stream(a[5], codes);
+    const Output out = packed_output(a[3], "out", codes.sizes(), code == BSR_F32 ? at::kFloat : at::kBFloat16, codes);
+    const int rc = released([&] {
+      return bsr_adamw_state_values(typed<uint8_t>(codes), typed<uint8_t>(scales), count, which, pointer(out.get()), code, stream.handle());
+    });
+    return rc != BSR_OK ? code_result(rc) : out.result();
+  });
+}
+
 // () -> handle of the current stream of the current device
 PyObject *current_stream(PyObject *, PyObject *) {
   return guarded([&]() -> PyObject * { return PyLong_FromVoidPtr(c10::hip::getCurrentHIPStream().stream()); });
@@ -714,6 +917,12 @@ PyMethodDef methods[] = {
     {"distill_loss", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(distill_loss)), METH_FASTCALL, nullptr},
     {"distill_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(distill_grad)), METH_FASTCALL, nullptr},
     {"distill_loss_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(distill_loss_grad)), METH_FASTCALL, nullptr},
+    {"layer_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(layer_norm)), METH_FASTCALL, nullptr},
+    {"layer_norm_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(layer_norm_grad)), METH_FASTCALL, nullptr},
+    {"gated_ff", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(gated_ff)), METH_FASTCALL, nullptr},
+    {"gated_ff_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(gated_ff_grad)), METH_FASTCALL, nullptr},
+    {"adamw_batched", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(adamw_batched)), METH_FASTCALL, nullptr},
+    {"adamw_state_values", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(adamw_state_values)), METH_FASTCALL, nullptr},
     {"current_stream", current_stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
