@@ -303,13 +303,16 @@ def _plain_adamw(s):
 
 def _own_adamw(B, s):
     if "batch" not in s:                              # a program's tensors stay where they are, and so does the list of them
+        # (whole blocks: what fills a buffer up to the next tensor is stepped with the tensor before it, as the plain form does)
+        ends = [at + -(-n // BLOCK) * BLOCK for at, n, _ in s["segments"]]
+        parts = [slice(at, end) for (at, _, _), end in zip(s["segments"], ends)]
+
         def part(flat):
-            return [flat[at:at + n] for at, n, _ in s["segments"]]
+            return [flat[x] for x in parts]
         if s["bits"] == 32:
             states = list(zip(part(s["m"]), part(s["v"])))
         else:
-            states = [(s["m"][at:at + n], s["r"][at:at + n], s["scales"][:, at // BLOCK:(at + n + BLOCK - 1) // BLOCK])
-                      for at, n, _ in s["segments"]]
+            states = [(s["m"][x], s["r"][x], s["scales"][:, x.start // BLOCK:x.stop // BLOCK]) for x in parts]
         s["batch"] = B.AdamWBatch(part(s["param"]), part(s["grad_flat"]), bits=s["bits"], states=states,
                                   copies=part(s["copy_flat"]) if s["copy_flat"] is not None else None,
                                   weight_decay=[d for _, _, d in s["segments"]])
