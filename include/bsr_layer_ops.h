@@ -57,6 +57,9 @@ int bsr_layer_norm_grad(const void *X, int dtype, int64_t M, int64_t D, int64_t 
                         float *dgamma, float *dbeta, int accumulate, void *ws,
                         size_t ws_bytes, void *stream);
 
+/* widest rows of the gated block: D and 2F (BSR_ERR_LIMIT beyond) */
+enum { BSR_MAX_GATED_WIDTH = (1 << 20) };
+
 /* Activations of the gated block. */
 enum {
   BSR_ACT_SILU = 0,      /* g / (1 + exp(-g)) */

@@ -39,6 +39,7 @@ int check_gated(const GatedArgs &a) {
   if (!known_type(a.dtype)) return BSR_ERR_DTYPE;
   if (a.F < 0 || a.F > kMaxRows / 2) return BSR_ERR_SHAPE;
   BSR_REQUIRE(check_matrix(a.D, 2 * a.F, a.ldw));
+  if (a.D > BSR_MAX_GATED_WIDTH || 2 * a.F > BSR_MAX_GATED_WIDTH) return BSR_ERR_LIMIT;
   return a.act < BSR_ACT_SILU || a.act > BSR_ACT_RELU ? BSR_ERR_VALUE : BSR_OK;
 }
 

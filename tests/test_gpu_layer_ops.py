@@ -147,6 +147,23 @@ def test_gated_ff_grad(dtype, M, D, F):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gated_many_tiles(dtype):
+    """More tiles than compute units, ragged in both directions."""
+    M, D, F = 3077, 72, 2120
+    x, w = randn(1, M, D, dtype=dtype), randn(2, D, 2 * F, dtype=dtype, scale=D ** -0.5)
+    H, GU = B.bsr_gated_ff(x.cuda(), w.cuda(), act="silu", want_GU=True)
+    h, e_h, gu, e_gu = P.gated(f64(x), f64(w), "silu", dtype)
+    check(GU, gu, e_gu, dtype, "GU")
+    check(H, h, e_h, dtype, "H")
+    M, D, F = 3077, 4200, 36
+    gu, dh, w = randn(1, M, 2 * F, dtype=dtype), randn(2, M, F, dtype=dtype), randn(3, D, 2 * F, dtype=dtype)
+    dX, dGU = B.bsr_gated_ff_grad(gu.cuda(), dh.cuda(), w.cuda(), act="silu")
+    d = f64(dGU)
+    size = np.abs(d) @ np.abs(f64(w)).T
+    check(dX, d @ f64(w).T, ((2 * F + 1) if dtype == "bf16" else (12 * F + 4)) * P.U * size, dtype, "dX")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("name", ["silu", "gelu", "gelu_tanh", "relu"])
 def test_activations_over_their_range(dtype, name):
     g = torch.cat((torch.linspace(-12, 12, 4001), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 50.0, -50.0, 200.0, -200.0, 1e4, -1e4]))).to(DT[dtype])

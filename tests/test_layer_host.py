@@ -62,6 +62,8 @@ def test_gated_refusals():
         return lib.bsr_gated_ff(X, dtype, M, D, ldx, W, F, ldw, act, H, ldh, GU, ldgu, ws, nbytes, None)
     assert ff(dtype=2) == B.BSR_ERR_DTYPE
     assert ff(ldx=15) == ff(ldw=15) == ff(ldh=7) == ff(ldgu=15) == ff(M=-1) == ff(F=-1) == ff(M=big) == ff(F=1 << 30, ldw=big) == B.BSR_ERR_SHAPE
+    wide = (1 << 20) + 2
+    assert ff(D=wide, ldx=wide) == ff(F=wide // 2, ldw=wide, ldh=wide, ldgu=wide) == B.BSR_ERR_LIMIT
     assert ff(act=-1) == ff(act=4) == B.BSR_ERR_VALUE
     assert ff(X=None) == ff(W=None) == ff(H=None) == B.BSR_ERR_NULL
     assert ff(X=ODD) == ff(W=ODD) == ff(H=ODD) == ff(GU=ODD) == B.BSR_ERR_ALIGN
