@@ -16,10 +16,9 @@ namespace {
 // Sum over the lanes of a wave whose numbers are equal modulo V.
 template <int V>
 __device__ __forceinline__ float sum_strided(float v) {
-  v += dpp_of<0x128>(v);                             // rotations within 16 lanes: by 8, 4, 2, 1
+  static_assert(V == 4 || V == 8, "");
+  v += dpp_of<0x128>(v);                             // rotations within 16 lanes
   if constexpr (V <= 4) v += dpp_of<0x124>(v);
-  if constexpr (V <= 2) v += dpp_of<0x122>(v);
-  if constexpr (V <= 1) v += dpp_of<0x121>(v);
   v += other_row(v);
   return v + other_half(v);
 }
@@ -45,26 +44,30 @@ __global__ __launch_bounds__(kFewThreads) void gated_few_kernel(int act, const T
   float acc[kSums];
 #pragma unroll
   for (int i = 0; i < kSums; ++i) acc[i] = 0.0f;
+  typename R::Raw g[kTogether], u[kTogether];
+  auto load = [&](int64_t k0, int k1, int here) {
+#pragma unroll
+    for (int t = 0; t < kTogether; ++t) {
+      const int k = k1 + t * kStep;
+      g[t] = u[t] = R::zero();
+      if (there && k < here) {
+        const T *p = W + (k0 + k) * ldw + at;
+        g[t] = R::load(p);
+        u[t] = R::load(p + F);
+      }
+    }
+  };
   for (int64_t k0 = 0; k0 < D; k0 += kFewK) {
-    const int here = D - k0 < kFewK ? (int)(D - k0) : kFewK;
-    __syncthreads();
+    const int here = D - k0 < kFewK ? (int)(D - k0) : kFewK, first = wave * kRows + row;
+    load(k0, first, here);                           // on their way while X is copied
+    if (k0 > 0) __syncthreads();
     for (int i = threadIdx.x; i < MR * kFewK; i += kFewThreads) {
       const int m = i / kFewK, k = i % kFewK;
       xs[m][k] = m < M && k < here ? elem_to_float<T>(X[m * ldx + k0 + k]) : 0.0f;
     }
     __syncthreads();
-    for (int k1 = wave * kRows + row; k1 < here; k1 += kTogether * kStep) {
-      typename R::Raw g[kTogether], u[kTogether];
-#pragma unroll
-      for (int t = 0; t < kTogether; ++t) {
-        const int k = k1 + t * kStep;
-        g[t] = u[t] = R::zero();
-        if (there && k < here) {
-          const T *p = W + (k0 + k) * ldw + at;
-          g[t] = R::load(p);
-          u[t] = R::load(p + F);
-        }
-      }
+    for (int k1 = first; k1 < here; k1 += kTogether * kStep) {
+      if (k1 != first) load(k0, k1, here);
 #pragma unroll
       for (int t = 0; t < kTogether; ++t) {
         const int k = k1 + t * kStep;
@@ -293,8 +296,8 @@ struct Layout {
   size_t a = 0, b = 0, partial = 0, all = 0;         // bytes of the packed operands (0: taken in place), of the parts, together
 };
 
-// Rows that gated_few_kernel takes.
-constexpr int64_t kFewRows = 4;
+// Rows that gated_few_kernel takes (with four, its sums leave registers for half as many waves: 19 us, the matrix cores 16).
+constexpr int64_t kFewRows = 2;
 bool few_rows(const GatedArgs &g) { return g.M <= kFewRows && g.F >= 16 / elem_bytes(g.dtype) && g.D > 0; }
 
 Layout forward_layout(const GatedArgs &g) {
@@ -333,12 +336,12 @@ void run_few(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, h
   };
   auto rows = [&](auto v) {
     if (g.M == 1) go(std::integral_constant<int, 1>(), v);
-    else if (g.M == 2) go(std::integral_constant<int, 2>(), v);
-    else go(std::integral_constant<int, 4>(), v);
+    else go(std::integral_constant<int, 2>(), v);
   };
-  if (vecs >= 8 * kCus) rows(std::integral_constant<int, 8>());
-  else if (vecs >= 4 * kCus) rows(std::integral_constant<int, 4>());
-  else rows(std::integral_constant<int, 2>());
+  // whole lines as soon as half of the compute units have some: 2048 x [2 x 5504] in 172 workgroups of 64 bytes 11.0 us, in 86 of 128 bytes
+  // 12.1, in 344 of 32 bytes 19.4; 4096 x [2 x 11008] in 172 of 128 bytes 38.6 (4.7 TB/s), in 344 of 64 bytes 54
+  if (vecs >= 4 * kCus) rows(std::integral_constant<int, 8>());
+  else rows(std::integral_constant<int, 4>());
 }
 
 template <typename T>
