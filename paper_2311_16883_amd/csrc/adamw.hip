@@ -1,7 +1,7 @@
 // One AdamW step over many tensors, moments in binary32 or in 8 bits.
 //
 // Bound by memory: 28 bytes per element with binary32 weights, gradients and moments, 16 with 8-bit moments.  The tensors of a call
-// are cut into chunks of 128-element blocks, a chunk to a workgroup; the list of tensors travels in the kernel's arguments, so
+// are cut into chunks of whole blocks, a chunk to a workgroup; the list of tensors travels in the kernel's arguments, so
 // there is nothing to copy or to keep for the device.  A lane holds four consecutive elements of a block, 32 lanes a block, whose largest magnitudes
 // meet by lane exchanges.
 //
@@ -22,8 +22,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPerLane = 4;
 constexpr int kRound = kThreads * kPerLane;            // elements of a round of the workgroup: 8 blocks
-constexpr int kRounds = 4;                             // rounds of a chunk
-constexpr int64_t kChunk = (int64_t)kRound * kRounds;
+constexpr int64_t kManyElements = int64_t(4) << 20;    // from here on a workgroup takes four rounds, below one
 constexpr int kItems = 40;                             // tensors per launch: their list is 3.5 KB of arguments
 
 struct Item {
@@ -104,37 +103,32 @@ __device__ __forceinline__ void store4(T *p, int left, const T *v) {
   }
 }
 
-// The magnitude that a code stands for, in the block's units of 2^(scale - 127 - 14 - BITS); scale 255: NaN.
+// A code's exponent and fraction are those of a binary32 number when they are moved to its place, the codes without an exponent among
+// the subnormals: x = that number * 2^(scale - 15).  Scale 255: NaN.
 template <int BITS>
-__device__ __forceinline__ float decode(uint32_t magnitude, uint32_t scale) {
-  const uint32_t e = magnitude >> BITS, f = magnitude & ((1u << BITS) - 1u);
-  const uint32_t n = e != 0u ? f + (1u << BITS) : f;
-  const float x = ldexpf((float)n, (int)scale - (127 + 14 + BITS) + (e != 0u ? (int)e - 1 : 0));
-  return scale == 255u ? __uint_as_float(0x7FC00000u) : x;
+__device__ __forceinline__ float decode(uint32_t code, uint32_t scale) {
+  const uint32_t w = BITS == 3 ? (code & 127u) << 20 | (code & 128u) << 24 : code << 19;
+  return __uint_as_float(__float_as_uint(ldexpf(__uint_as_float(w), (int)scale - 15)) | (scale == 255u ? 0x7FC00000u : 0u));
 }
 
 // The scale byte of a block whose largest magnitude has these bits: the exponent of the smallest power of two above which the
 // largest code lies.
 template <int BITS>
 __device__ __forceinline__ uint32_t scale_of(uint32_t most) {
-  const uint32_t b = (most + (0x7FFFFFu >> (BITS + 0))) >> 23;
+  const uint32_t b = (most + (0x7FFFFFu >> BITS)) >> 23;
   return b < 32u ? 0u : b > 255u ? 255u : b;
 }
 
-// |x| rounded to one of its two neighbours by u in [0, 1).
+// a >= 0 rounded to one of its two neighbours by u in [0, 2^16): the bits below a code's last are added to and cut off.  (The scale
+// leaves room for it: the largest of a block is not above the largest code.)
 template <int BITS>
-__device__ __forceinline__ uint32_t encode(float a, uint32_t scale, float u) {
-  const int least = (int)scale - (127 + 14 + BITS);
-  const int own = (int)(__float_as_uint(a) >> 23) - 127 - BITS;
-  const int ex = max(own, least);
-  uint32_t n = (uint32_t)floorf(ldexpf(a, -ex) + u);
-  if (BITS == 4 && a > 0.0f) n = max(n, 1u);
-  const uint32_t code = min(n + ((uint32_t)(ex - least) << BITS), BITS == 3 ? 127u : 255u);
-  return scale == 0u || scale == 255u ? 0u : code;
+__device__ __forceinline__ uint32_t encode(float a, uint32_t scale, uint32_t u) {
+  const uint32_t code = (__float_as_uint(ldexpf(a, 15 - (int)scale)) + (u << (7 - BITS))) >> (23 - BITS);
+  return scale == 0u || scale == 255u ? 0u : BITS == 4 ? max(code, min(__float_as_uint(a), 1u)) : code;
 }
 
 template <typename P, typename G, bool SMALL, bool COPY>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
+__global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int rounds) {
   // this workgroup's tensor
   int lo = 0, hi = n;
   while (hi - lo > 1) {
@@ -143,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
     else hi = mid;
   }
   const Item &it = list.it[lo];
-  const int64_t chunk0 = (int64_t)(blockIdx.x - list.chunk_begin[lo]) * kChunk;
+  const int64_t chunk0 = (int64_t)(blockIdx.x - list.chunk_begin[lo]) * rounds * kRound;
   Options o = list.o;
   if (o.step_device != nullptr) step_numbers(o, *o.step_device);
   if (o.lr_device != nullptr) o.lr = *o.lr_device;
@@ -151,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
   P *const param = static_cast<P *>(it.param);
   const G *const grad = static_cast<const G *>(it.grad);
   const float keep = 1.0f - o.lr * it.decay, rate = o.lr * o.first_full;
-  for (int r = 0; r < kRounds; ++r) {
+  for (int r = 0; r < rounds; ++r) {
     const int64_t i = chunk0 + (int64_t)r * kRound + threadIdx.x * kPerLane;
     if (chunk0 + (int64_t)r * kRound >= it.n) break;
     const int left = it.n - i >= 4 ? 4 : it.n > i ? (int)(it.n - i) : 0;
@@ -168,8 +162,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
       const uint32_t sm = left > 0 ? it.scale_m[block] : 0u, sv = left > 0 ? it.scale_v[block] : 0u;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        m[q] = decode<3>(cm[q] & 127u, sm);
-        m[q] = (cm[q] & 128u) ? -m[q] : m[q];
+        m[q] = decode<3>(cm[q], sm);
         root[q] = decode<4>(cv[q], sv);
       }
     } else {
@@ -179,10 +172,11 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float g = elem_to_float<G>(g0[q]) * o.grad_scale;
-      m[q] = o.b1 * m[q] + o.c1 * g;
-      const float v = o.b2 * (SMALL ? root[q] * root[q] : root[q]) + o.c2 * g * g;
-      const float rt = sqrtf(v);
-      p[q] = elem_to_float<P>(p0[q]) * keep - rate * m[q] / (rt * o.root + o.eps);
+      // (rounded product by product: what a code's border decides does not hang on which of them are fused)
+      m[q] = __fadd_rn(__fmul_rn(o.b1, m[q]), __fmul_rn(o.c1, g));
+      const float v = __fadd_rn(SMALL ? __fmul_rn(__fmul_rn(o.b2, root[q]), root[q]) : __fmul_rn(o.b2, root[q]), __fmul_rn(__fmul_rn(o.c2, g), g));
+      const float rt = SMALL ? __fsqrt_rn(v) : __builtin_amdgcn_sqrtf(v);
+      p[q] = elem_to_float<P>(p0[q]) * keep - rate * m[q] * __builtin_amdgcn_rcpf(rt * o.root + o.eps);
       root[q] = SMALL ? rt : v;
     }
 #pragma unroll
@@ -204,14 +198,14 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
       }
       const uint32_t sm = scale_of<3>(group_max<5>(most_m)), sv = scale_of<4>(group_max<5>(most_v));
       uint8_t cm[4], cv[4];
+      const uint64_t number = (uint64_t)(it.first + i);       // (a multiple of 4: its high half is that of all four)
+      const uint32_t base = (uint32_t)number * 0x9E3779B1u + (uint32_t)(number >> 32) * 0x7F4A7C15u + o.key;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint64_t number = (uint64_t)(it.first + i + q);
-        const uint32_t h = mix((uint32_t)number * 0x9E3779B1u + (uint32_t)(number >> 32) * 0x7F4A7C15u + o.key);
-        const float a = fabsf(m[q]);
-        const uint32_t c = encode<3>(a, sm, (float)(h & 0xFFFFu) * 0x1p-16f);
-        cm[q] = (uint8_t)(c != 0u && m[q] < 0.0f ? c + 128u : c);
-        cv[q] = (uint8_t)encode<4>(root[q], sv, (float)(h >> 16) * 0x1p-16f);
+        const uint32_t h = mix(base + (uint32_t)q * 0x9E3779B1u);
+        const uint32_t c = encode<3>(fabsf(m[q]), sm, h & 0xFFFFu);
+        cm[q] = (uint8_t)(c | (c != 0u && m[q] < 0.0f ? 128u : 0u));
+        cv[q] = (uint8_t)encode<4>(root[q], sv, h >> 16);
       }
       store4(static_cast<uint8_t *>(it.m) + i, left, cm);
       store4(static_cast<uint8_t *>(it.v) + i, left, cv);
@@ -226,27 +220,32 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n) {
   }
 }
 
+// Sixteen codes to a lane.
 template <typename T, int BITS>
 __global__ __launch_bounds__(kThreads) void state_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                 int64_t n, T *__restrict__ out) {
-  for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * kRound) {
-    const int left = n - i >= 4 ? 4 : (int)(n - i);
-    uint8_t c[4];
-    load4(codes + i, left, c);
+  for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 16; i < n; i += (int64_t)gridDim.x * kThreads * 16) {
     const uint32_t scale = scales[i / kMomentBlock];
-    T v[4];
+    if (n - i >= 16) {
+      struct __attribute__((packed, aligned(1))) Codes { Words4 w; };
+      struct __attribute__((packed, aligned(2))) Out { Words4 w; };
+      const Words4 c = reinterpret_cast<const Codes *>(codes + i)->w;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float a = decode<BITS>(BITS == 3 ? c[q] & 127u : c[q], scale);
-      v[q] = from_float<T>(BITS == 3 && (c[q] & 128u) ? -a : a);
+      for (int v = 0; v < 16; v += 16 / (int)sizeof(T)) {
+        float f[16 / sizeof(T)];
+#pragma unroll
+        for (int q = 0; q < 16 / (int)sizeof(T); ++q) f[q] = decode<BITS>(c[(v + q) / 4] >> (8 * ((v + q) % 4)) & 255u, scale);
+        reinterpret_cast<Out *>(out + i + v)->w = pack_row<T, 16 / (int)sizeof(T)>(f);
+      }
+    } else {
+      for (int64_t j = i; j < n; ++j) out[j] = from_float<T>(decode<BITS>(codes[j], scale));
     }
-    store4(out + i, left, v);
   }
 }
 
 template <typename P, typename G, bool SMALL, bool COPY>
-void launch_list(const List &list, int n, uint32_t chunks, hipStream_t s) {
-  adamw_kernel<P, G, SMALL, COPY><<<dim3(chunks), kThreads, 0, s>>>(list, n);
+void launch_list(const List &list, int n, uint32_t chunks, int rounds, hipStream_t s) {
+  adamw_kernel<P, G, SMALL, COPY><<<dim3(chunks), kThreads, 0, s>>>(list, n, rounds);
 }
 
 }  // namespace
@@ -274,14 +273,18 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
   int held = 0;
   bool copies = false;
   uint32_t chunks = 0;
+  int64_t all = 0;
+  for (int i = 0; i < n; ++i) all += items[i].n;
+  const int rounds = all >= kManyElements ? 4 : 1;
+  const int64_t chunk = (int64_t)kRound * rounds;
   auto flush = [&]() {
     if (held == 0) return (int)BSR_OK;
     list.chunk_begin[held] = chunks;
     auto go = [&](auto p, auto g) {
       typedef decltype(p) P;
       typedef decltype(g) G;
-      if (small) copies ? launch_list<P, G, true, true>(list, held, chunks, s) : launch_list<P, G, true, false>(list, held, chunks, s);
-      else copies ? launch_list<P, G, false, true>(list, held, chunks, s) : launch_list<P, G, false, false>(list, held, chunks, s);
+      if (small) copies ? launch_list<P, G, true, true>(list, held, chunks, rounds, s) : launch_list<P, G, true, false>(list, held, chunks, rounds, s);
+      else copies ? launch_list<P, G, false, true>(list, held, chunks, rounds, s) : launch_list<P, G, false, false>(list, held, chunks, rounds, s);
     };
     if (param_dtype == BSR_F32) grad_dtype == BSR_F32 ? go(float(), float()) : go(float(), uint16_t());
     else grad_dtype == BSR_F32 ? go(uint16_t(), float()) : go(uint16_t(), uint16_t());
@@ -294,8 +297,8 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
     if (x.n > 0) {
       // chunks of a launch: its lanes are counted in 32 bits; a tensor beyond that goes in parts of whole blocks
       constexpr int64_t kMostChunks = int64_t(1) << 23;
-      for (int64_t at = 0; at < x.n; at += kMostChunks * kChunk) {
-        const int64_t part = std::min(x.n - at, kMostChunks * kChunk), needs = ceil_div(part, kChunk);
+      for (int64_t at = 0; at < x.n; at += kMostChunks * chunk) {
+        const int64_t part = std::min(x.n - at, kMostChunks * chunk), needs = ceil_div(part, chunk);
         const bool copy = x.copy != nullptr;
         if (held == kItems || (held > 0 && (copy != copies || chunks + needs > kMostChunks)))
           if (const int rc = flush(); rc != BSR_OK) return rc;
@@ -322,7 +325,7 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
 }
 
 int launch_adamw_state_values(const uint8_t *codes, const uint8_t *scales, int64_t n, int which, void *out, int dtype, hipStream_t s) {
-  const dim3 grid((uint32_t)std::min(ceil_div(n, (int64_t)kRound), int64_t(1) << 23));
+  const dim3 grid((uint32_t)std::min(ceil_div(n, (int64_t)kThreads * 16), int64_t(1) << 23));
   if (dtype == BSR_F32) {
     if (which == 0) state_values_kernel<float, 3><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<float *>(out));
     else state_values_kernel<float, 4><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<float *>(out));
