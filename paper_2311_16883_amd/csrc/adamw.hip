@@ -20,8 +20,9 @@ namespace bsr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPerLane = 4;
-constexpr int kRound = kThreads * kPerLane;            // elements of a round of the workgroup: 8 blocks
+// Consecutive elements of a lane: 16 bytes of the largest kind of number that is read.  (49 million bfloat16 weights and gradients, 8-bit
+// moments: four a lane 134 us, eight 116; moments in binary32: 212 and 219.)
+constexpr int per_lane(size_t param_bytes, bool small) { return param_bytes == 2 && small ? 8 : 4; }
 constexpr int64_t kManyElements = int64_t(4) << 20;    // from here on a workgroup takes four rounds, below one
 constexpr int kItems = 40;                             // tensors per launch: their list is 3.5 KB of arguments
 
@@ -69,36 +70,38 @@ __host__ __device__ inline void step_numbers(Options &o, int64_t step) {
   o.key = key_of(o.seed, step);
 }
 
-// Four numbers from element i on; `left` of them are there.
-template <typename T>
-struct Any4 {
-  typedef uint32_t __attribute__((ext_vector_type(sizeof(T)))) Words;      // 4 * sizeof(T) bytes
-  struct __attribute__((packed, aligned(1))) Loose { Words w; };
+// N consecutive numbers, of which `left` are there (the others: 0), at any alignment.
+template <int BYTES>
+struct __attribute__((packed, aligned(1))) AnyBytes {
+  typename RawWords<BYTES>::type w;
 };
-template <>
-struct Any4<uint8_t> {
-  typedef uint32_t Words;
-  struct __attribute__((packed, aligned(1))) Loose { Words w; };
-};
-template <typename T>
-__device__ __forceinline__ void load4(const T *p, int left, T *out) {
-  if (left >= 4) {
-    const auto w = reinterpret_cast<const typename Any4<T>::Loose *>(p)->w;
-    __builtin_memcpy(out, &w, 4 * sizeof(T));
+template <int N, typename T>
+__device__ __forceinline__ void load_some(const T *p, int left, T *out) {
+  constexpr int kBytes = N * sizeof(T), kEach = kBytes < 16 ? kBytes : 16;
+  if (left >= N) {
+#pragma unroll
+    for (int b = 0; b < kBytes; b += kEach) {
+      const auto w = reinterpret_cast<const AnyBytes<kEach> *>(reinterpret_cast<const char *>(p) + b)->w;
+      __builtin_memcpy(reinterpret_cast<char *>(out) + b, &w, kEach);
+    }
   } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) out[q] = q < left ? p[q] : (T)0;
+    for (int q = 0; q < N; ++q) out[q] = q < left ? p[q] : (T)0;
   }
 }
-template <typename T>
-__device__ __forceinline__ void store4(T *p, int left, const T *v) {
-  if (left >= 4) {
-    typename Any4<T>::Words w;
-    __builtin_memcpy(&w, v, 4 * sizeof(T));
-    reinterpret_cast<typename Any4<T>::Loose *>(p)->w = w;
+template <int N, typename T>
+__device__ __forceinline__ void store_some(T *p, int left, const T *v) {
+  constexpr int kBytes = N * sizeof(T), kEach = kBytes < 16 ? kBytes : 16;
+  if (left >= N) {
+#pragma unroll
+    for (int b = 0; b < kBytes; b += kEach) {
+      typename RawWords<kEach>::type w;
+      __builtin_memcpy(&w, reinterpret_cast<const char *>(v) + b, kEach);
+      reinterpret_cast<AnyBytes<kEach> *>(reinterpret_cast<char *>(p) + b)->w = w;
+    }
   } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < N; ++q)
       if (q < left) p[q] = v[q];
   }
 }
@@ -129,6 +132,7 @@ __device__ __forceinline__ uint32_t encode(float a, uint32_t scale, uint32_t u) 
 
 template <typename P, typename G, bool SMALL, bool COPY>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int rounds) {
+  constexpr int PL = per_lane(sizeof(P), SMALL), kGroup = PL == 8 ? 4 : 5;      // lanes of a block: 2^kGroup
   // this workgroup's tensor
   int lo = 0, hi = n;
   while (hi - lo > 1) {
@@ -137,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
     else hi = mid;
   }
   const Item &it = list.it[lo];
-  const int64_t chunk0 = (int64_t)(blockIdx.x - list.chunk_begin[lo]) * rounds * kRound;
+  const int64_t chunk0 = (int64_t)(blockIdx.x - list.chunk_begin[lo]) * rounds * (kThreads * PL);
   Options o = list.o;
   if (o.step_device != nullptr) step_numbers(o, *o.step_device);
   if (o.lr_device != nullptr) o.lr = *o.lr_device;
@@ -146,31 +150,31 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
   const G *const grad = static_cast<const G *>(it.grad);
   const float keep = 1.0f - o.lr * it.decay, rate = o.lr * o.first_full;
   for (int r = 0; r < rounds; ++r) {
-    const int64_t i = chunk0 + (int64_t)r * kRound + threadIdx.x * kPerLane;
-    if (chunk0 + (int64_t)r * kRound >= it.n) break;
-    const int left = it.n - i >= 4 ? 4 : it.n > i ? (int)(it.n - i) : 0;
-    P p0[4];
-    G g0[4];
-    float m[4], root[4], p[4];
-    load4(param + i, left, p0);
-    load4(grad + i, left, g0);
+    const int64_t i = chunk0 + (int64_t)r * (kThreads * PL) + threadIdx.x * PL;
+    if (chunk0 + (int64_t)r * (kThreads * PL) >= it.n) break;
+    const int left = it.n - i >= PL ? PL : it.n > i ? (int)(it.n - i) : 0;
+    P p0[PL];
+    G g0[PL];
+    float m[PL], root[PL], p[PL];
+    load_some<PL>(param + i, left, p0);
+    load_some<PL>(grad + i, left, g0);
     const int64_t block = i / kMomentBlock;
     if constexpr (SMALL) {
-      uint8_t cm[4], cv[4];
-      load4(static_cast<const uint8_t *>(it.m) + i, left, cm);
-      load4(static_cast<const uint8_t *>(it.v) + i, left, cv);
+      uint8_t cm[PL], cv[PL];
+      load_some<PL>(static_cast<const uint8_t *>(it.m) + i, left, cm);
+      load_some<PL>(static_cast<const uint8_t *>(it.v) + i, left, cv);
       const uint32_t sm = left > 0 ? it.scale_m[block] : 0u, sv = left > 0 ? it.scale_v[block] : 0u;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < PL; ++q) {
         m[q] = decode<3>(cm[q], sm);
         root[q] = decode<4>(cv[q], sv);
       }
     } else {
-      load4(static_cast<const float *>(it.m) + i, left, m);
-      load4(static_cast<const float *>(it.v) + i, left, root);
+      load_some<PL>(static_cast<const float *>(it.m) + i, left, m);
+      load_some<PL>(static_cast<const float *>(it.v) + i, left, root);
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < PL; ++q) {
       const float g = elem_to_float<G>(g0[q]) * o.grad_scale;
       // (rounded product by product: what a code's border decides does not hang on which of them are fused)
       m[q] = __fadd_rn(__fmul_rn(o.b1, m[q]), __fmul_rn(o.c1, g));
@@ -180,42 +184,42 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
       root[q] = SMALL ? rt : v;
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) p0[q] = from_float<P>(p[q]);
-    store4(param + i, left, p0);
+    for (int q = 0; q < PL; ++q) p0[q] = from_float<P>(p[q]);
+    store_some<PL>(param + i, left, p0);
     if constexpr (COPY) {
-      uint16_t c[4];
+      uint16_t c[PL];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) c[q] = from_float<uint16_t>(p[q]);
-      store4(it.copy + i, left, c);
+      for (int q = 0; q < PL; ++q) c[q] = from_float<uint16_t>(p[q]);
+      store_some<PL>(it.copy + i, left, c);
     }
     if constexpr (SMALL) {
       uint32_t most_m = 0u, most_v = 0u;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < PL; ++q) {
         const bool there = q < left;
         most_m = max(most_m, there ? __float_as_uint(m[q]) & 0x7FFFFFFFu : 0u);
         most_v = max(most_v, there ? __float_as_uint(root[q]) & 0x7FFFFFFFu : 0u);
       }
-      const uint32_t sm = scale_of<3>(group_max<5>(most_m)), sv = scale_of<4>(group_max<5>(most_v));
-      uint8_t cm[4], cv[4];
-      const uint64_t number = (uint64_t)(it.first + i);       // (a multiple of 4: its high half is that of all four)
+      const uint32_t sm = scale_of<3>(group_max<kGroup>(most_m)), sv = scale_of<4>(group_max<kGroup>(most_v));
+      uint8_t cm[PL], cv[PL];
+      const uint64_t number = (uint64_t)(it.first + i);       // (its high half is that of all)
       const uint32_t base = (uint32_t)number * 0x9E3779B1u + (uint32_t)(number >> 32) * 0x7F4A7C15u + o.key;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < PL; ++q) {
         const uint32_t h = mix(base + (uint32_t)q * 0x9E3779B1u);
         const uint32_t c = encode<3>(fabsf(m[q]), sm, h & 0xFFFFu);
         cm[q] = (uint8_t)(c | (c != 0u && m[q] < 0.0f ? 128u : 0u));
         cv[q] = (uint8_t)encode<4>(root[q], sv, h >> 16);
       }
-      store4(static_cast<uint8_t *>(it.m) + i, left, cm);
-      store4(static_cast<uint8_t *>(it.v) + i, left, cv);
-      if (threadIdx.x % (kMomentBlock / kPerLane) == 0 && left > 0) {
+      store_some<PL>(static_cast<uint8_t *>(it.m) + i, left, cm);
+      store_some<PL>(static_cast<uint8_t *>(it.v) + i, left, cv);
+      if (threadIdx.x % (kMomentBlock / PL) == 0 && left > 0) {
         it.scale_m[block] = (uint8_t)sm;
         it.scale_v[block] = (uint8_t)sv;
       }
     } else {
-      store4(static_cast<float *>(it.m) + i, left, m);
-      store4(static_cast<float *>(it.v) + i, left, root);
+      store_some<PL>(static_cast<float *>(it.m) + i, left, m);
+      store_some<PL>(static_cast<float *>(it.v) + i, left, root);
     }
   }
 }
@@ -276,7 +280,7 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
   int64_t all = 0;
   for (int i = 0; i < n; ++i) all += items[i].n;
   const int rounds = all >= kManyElements ? 4 : 1;
-  const int64_t chunk = (int64_t)kRound * rounds;
+  const int64_t chunk = (int64_t)kThreads * rounds * per_lane((size_t)elem_bytes(param_dtype), small);
   auto flush = [&]() {
     if (held == 0) return (int)BSR_OK;
     list.chunk_begin[held] = chunks;
