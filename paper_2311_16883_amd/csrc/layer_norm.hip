@@ -22,10 +22,10 @@ struct RowRegs {
   typename RowVec<T, VE>::Raw x[NV];
 };
 
-// How the lanes of a workgroup share rows: groups of 2^LG lanes, or (WAVES > 1) all of its WAVES waves.
-template <int LG, int WAVES>
+// How the lanes of a workgroup share rows: groups of 2^LG lanes of its MANY waves, or (WAVES > 1) all of its WAVES waves.
+template <int LG, int WAVES, int MANY = 4>
 struct Share {
-  static constexpr int kThreads = WAVES > 1 ? 64 * WAVES : 256;
+  static constexpr int kThreads = 64 * (WAVES > 1 ? WAVES : MANY);
   static constexpr int kLanes = WAVES > 1 ? 64 * WAVES : 1 << LG;
   static constexpr int kRows = kThreads / kLanes;           // rows that a workgroup has in hand
   static __device__ __forceinline__ int lane() { return threadIdx.x & (kLanes - 1); }
@@ -194,15 +194,42 @@ __global__ __launch_bounds__(64 * kLongWaves) void layer_norm_long_kernel(const 
 
 // ---- backward ----
 
-// dX of the rows that a workgroup walks over, and (SUMS) their sums of dY * xh and dY by column: partial[workgroup] = 2 x D.
+// Sum over the groups of 2^LG lanes of a wave, lane by lane.
+template <int LG>
+__device__ __forceinline__ float sum_of_groups(float v) {
+  if constexpr (LG <= 3) v += dpp_of<0x128>(v);      // the other half of 16 lanes (rotation by 8)
+  if constexpr (LG <= 4) v += other_row(v);
+  if constexpr (LG <= 5) v += other_half(v);
+  return v;
+}
+
+// dX of the rows that a workgroup walks over, and (SUMS) their sums of dY * xh and dY by column: partial[workgroup] = 2 x D, or, of one
+// workgroup alone, the results themselves.
+struct Sums {
+  float *partial, *dgamma, *dbeta;                   // partial null: the results
+  int32_t accumulate;
+  __device__ __forceinline__ void put(int64_t D, int64_t c, float g, float b) const {
+    if (partial != nullptr) {
+      float *out = partial + (int64_t)blockIdx.x * 2 * D;
+      out[c] = g;
+      out[D + c] = b;
+    } else {
+      if (dgamma != nullptr) dgamma[c] = accumulate ? dgamma[c] + g : g;
+      if (dbeta != nullptr) dbeta[c] = accumulate ? dbeta[c] + b : b;
+    }
+  }
+};
+// Waves of a workgroup whose rows are one wave's or less: as many as LDS has sums for (64 KB).
+template <int VE, int NV>
+constexpr int walking_waves() { return VE * NV <= 16 ? 8 : 4; }
 template <typename T, int VE, int NV, int LG, int WAVES, bool RAGGED, bool SUMS>
-__global__ __launch_bounds__((Share<LG, WAVES>::kThreads)) void layer_norm_grad_kernel(
+__global__ __launch_bounds__((Share<LG, WAVES, walking_waves<VE, NV>()>::kThreads)) void layer_norm_grad_kernel(
     const T *X, int64_t M, int64_t D, int64_t ldx, const void *__restrict__ gamma, bool bf16, const float *__restrict__ stats,
-    const T *dY, int64_t lddy, T *dX, int64_t lddx, float *__restrict__ partial) {
+    const T *dY, int64_t lddy, T *dX, int64_t lddx, Sums out) {
   typedef RowVec<T, VE> R;
-  typedef Share<LG, WAVES> S;
+  typedef Share<LG, WAVES, walking_waves<VE, NV>()> S;
   __shared__ float lds[4 * WAVES];
-  extern __shared__ float columns[];                 // SUMS: 2 x D
+  extern __shared__ float columns[];                 // SUMS, rows of one wave or less: 2 x D for each wave
   int turn = 0;
   const int li = S::lane();
   const int vecs = (int)((D + VE - 1) / VE);
@@ -265,27 +292,54 @@ __global__ __launch_bounds__((Share<LG, WAVES>::kThreads)) void layer_norm_grad_
     }
   }
   if constexpr (SUMS) {
-    // the groups of the workgroup add their columns to the workgroup's, one after the other
-    for (int turn2 = 0; turn2 < S::kRows; ++turn2) {
-      if (S::row() == turn2) {
+    if constexpr (WAVES > 1) {                       // every column is some lane's alone
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
-          const int v = li + u * S::kLanes;
-          if (v >= vecs) continue;
-          const int64_t c = vector_start(v, VE, D);
-          const int front = RAGGED ? shared_front(v, VE, D) : 0;
+      for (int u = 0; u < NV; ++u) {
+        const int v = li + u * S::kLanes;
+        if (v >= vecs) continue;
+        const int64_t c = vector_start(v, VE, D);
+        if (out.partial != nullptr && VE >= 4) {     // (two vectors' shared columns: whoever writes last has the same sums)
+          float *to = out.partial + (int64_t)blockIdx.x * 2 * D + c;
 #pragma unroll
-          for (int q = 0; q < VE; ++q) {
-            if (RAGGED && q < front) continue;
-            columns[c + q] = turn2 == 0 ? dg[u][q] : columns[c + q] + dg[u][q];
-            columns[D + c + q] = turn2 == 0 ? db[u][q] : columns[D + c + q] + db[u][q];
+          for (int q = 0; q < VE; q += 4) {
+            RowVec<float, 4>::store(to + q, pack_row<float, 4>(dg[u] + q));
+            RowVec<float, 4>::store(to + D + q, pack_row<float, 4>(db[u] + q));
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < VE; ++q)
+            if (!RAGGED || q >= shared_front(v, VE, D)) out.put(D, c + q, dg[u][q], db[u][q]);
+        }
+      }
+    } else {
+      constexpr int kWaves = S::kThreads / 64;
+      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+      float *mine = columns + (int64_t)wave * 2 * D;
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        const int v = li + u * S::kLanes;
+#pragma unroll
+        for (int q = 0; q < VE; ++q) {
+          dg[u][q] = sum_of_groups<LG>(dg[u][q]);
+          db[u][q] = sum_of_groups<LG>(db[u][q]);
+          if (lane < S::kLanes && v < vecs && (!RAGGED || q >= shared_front(v, VE, D))) {
+            const int64_t c = vector_start(v, VE, D) + q;
+            mine[c] = dg[u][q];
+            mine[D + c] = db[u][q];
           }
         }
       }
       __syncthreads();
+      for (int64_t c = threadIdx.x; c < D; c += S::kThreads) {
+        float g = 0.0f, b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          g += columns[(int64_t)w * 2 * D + c];
+          b += columns[(int64_t)w * 2 * D + D + c];
+        }
+        out.put(D, c, g, b);
+      }
     }
-    float *out = partial + (int64_t)blockIdx.x * 2 * D;
-    for (int64_t c = threadIdx.x; c < 2 * D; c += S::kThreads) out[c] = columns[c];
   }
 }
 
@@ -364,27 +418,26 @@ __global__ __launch_bounds__(256) void layer_norm_columns_kernel(const T *__rest
   out[D + c] = db;
 }
 
-// dgamma, dbeta = (accumulate ? themselves : 0) + the sum of the partial sums: 64 columns and 16 slices of them to a workgroup.
+// dgamma, dbeta = (accumulate ? themselves : 0) + the sum of the partial sums: 32 columns and 32 slices of them to a workgroup.
 __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float *__restrict__ partial, int64_t parts, int64_t D,
                                                                float *__restrict__ dgamma, float *__restrict__ dbeta, int accumulate) {
-  __shared__ float sums[16][64];
-  const int col = threadIdx.x & 63, slice = threadIdx.x >> 6;
-  for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < 2 * D; c0 += (int64_t)gridDim.x * 64) {
+  __shared__ float sums[32][33];
+  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  for (int64_t c0 = (int64_t)blockIdx.x * 32; c0 < 2 * D; c0 += (int64_t)gridDim.x * 32) {
     const int64_t c = c0 + col;
     float sum = 0.0f;
     if (c < 2 * D) {
-      const int64_t per = (parts + 15) / 16, first = slice * per, last = first + per < parts ? first + per : parts;
 #pragma unroll 8
-      for (int64_t p = first; p < last; ++p) sum += partial[p * 2 * D + c];
+      for (int64_t p = slice; p < parts; p += 32) sum += partial[p * 2 * D + c];
     }
     sums[slice][col] = sum;
     __syncthreads();
-    if (slice == 0 && c < 2 * D) {
-      sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum += sums[i][col];
-      float *out = c < D ? dgamma : dbeta;
-      const int64_t at = c < D ? c : c - D;
+    // 32 lanes to a column: two columns to a wave
+    sum = group_sum<5>(sums[col][slice]);
+    const int64_t mine = c0 + slice;
+    if (col == 0 && mine < 2 * D) {
+      float *out = mine < D ? dgamma : dbeta;
+      const int64_t at = mine < D ? mine : mine - D;
       if (out != nullptr) out[at] = accumulate ? out[at] + sum : sum;
     }
     __syncthreads();
@@ -394,13 +447,18 @@ __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float *__re
 // ---- which form ----
 
 constexpr int64_t kMostWorkgroups = int64_t(1) << 20;      // rows beyond what they have in hand are taken in turn
-constexpr int64_t kWalkers = 512;                          // workgroups that walk over the rows of a backward pass, at most
-constexpr int64_t kSumColumns = 8192;                      // longest row whose column sums LDS holds (64 KB)
+// Workgroups that walk over the rows of a backward pass where columns are added up: rows in hand for each where there are few, then
+// as many rows for each of about 512 (of 16 waves: 256), as more of them have more sums to add up.
+constexpr int64_t kWalkers = 512;
+int64_t walkers(int64_t groups, int waves) {
+  const int64_t most = waves == 16 ? kWalkers / 2 : kWalkers;
+  return groups <= 2 * most ? groups : ceil_div(groups, ceil_div(groups, most));
+}
 
 // Calls f with the form of a row of `vecs` vectors: f(NV, LG, WAVES), false if rows are longer than registers hold.
 template <int N>
 using Int = std::integral_constant<int, N>;
-template <int MOST, typename F>
+template <bool WALK, typename F>
 bool with_row_form(int64_t vecs, F f) {
   if (vecs <= 8) f(Int<1>(), Int<3>(), Int<1>());
   else if (vecs <= 16) f(Int<1>(), Int<4>(), Int<1>());
@@ -409,8 +467,10 @@ bool with_row_form(int64_t vecs, F f) {
   else if (vecs <= 128) f(Int<2>(), Int<6>(), Int<1>());
   else if (vecs <= 192) f(Int<3>(), Int<6>(), Int<1>());
   else if (vecs <= 256) f(Int<4>(), Int<6>(), Int<1>());
-  else if (vecs <= 512) f(Int<2>(), Int<6>(), Int<4>());
-  else if (vecs <= 1024) f(Int<4>(), Int<6>(), Int<4>());
+  else if (!WALK && vecs <= 512) f(Int<2>(), Int<6>(), Int<4>());
+  else if (!WALK && vecs <= 1024) f(Int<4>(), Int<6>(), Int<4>());
+  else if (WALK && vecs <= 512) f(Int<1>(), Int<6>(), Int<8>());
+  else if (WALK && vecs <= 1024) f(Int<1>(), Int<6>(), Int<16>());
   else if (vecs <= 2048) f(Int<2>(), Int<6>(), Int<16>());
   else if (vecs <= 4096) f(Int<4>(), Int<6>(), Int<16>());
   else return false;
@@ -430,7 +490,7 @@ int norm_of(const T *X, int64_t M, int64_t D, int64_t ldx, const void *gamma, co
   if (D < VE) {
     launch(Int<1>(), Int<1>(), Int<3>(), Int<1>(), std::false_type());
   } else {
-    const bool found = with_row_form<0>(ceil_div(D, (int64_t)VE), [&](auto nv, auto lg, auto waves) {
+    const bool found = with_row_form<false>(ceil_div(D, (int64_t)VE), [&](auto nv, auto lg, auto waves) {
       if (D % VE) launch(Int<VE>(), nv, lg, waves, std::true_type());
       else launch(Int<VE>(), nv, lg, waves, std::false_type());
     });
@@ -442,41 +502,46 @@ int norm_of(const T *X, int64_t M, int64_t D, int64_t ldx, const void *gamma, co
 }
 
 // Workgroups whose partial sums a backward pass adds up.
-int64_t partial_sums(int64_t M) { return std::min<int64_t>(kWalkers, std::max<int64_t>(M, 1)); }
+int64_t partial_sums(int64_t M) { return std::min<int64_t>(2 * kWalkers, std::max<int64_t>(M, 1)); }
 
 template <typename T>
 int norm_grad_of(const T *X, int64_t M, int64_t D, int64_t ldx, const void *gamma, bool bf16, const float *stats, const T *dY,
                  int64_t lddy, T *dX, int64_t lddx, float *dgamma, float *dbeta, int accumulate, float *partial, hipStream_t s) {
   constexpr int VE = 16 / sizeof(T);
   const bool sums = dgamma != nullptr || dbeta != nullptr;
+  const int64_t vecs = ceil_div(D, (int64_t)VE);
+  // bfloat16 rows of more vectors than this would take more registers for their sums than 16 waves have
+  const bool apart = sums && vecs > (VE == 8 ? 2048 : 4096);
   int64_t parts = 0;
-  bool apart = sums && D > kSumColumns;
   if (apart) {
-    const int64_t per = ceil_div(M, partial_sums(M));
+    const int64_t per = ceil_div(M, std::min<int64_t>(M, 64));
     parts = ceil_div(M, per);
     layer_norm_columns_kernel<T><<<dim3((uint32_t)ceil_div(D, (int64_t)256), (uint32_t)parts), 256, 0, s>>>(X, M, D, ldx, stats, dY, lddy,
                                                                                                  partial, per);
     if (const int rc = check_launch(); rc != BSR_OK) return rc;
   }
   auto launch = [&](auto ve, auto nv, auto lg, auto waves, auto ragged) {
-    typedef Share<decltype(lg)::value, decltype(waves)::value> S;
+    constexpr int WAVES = decltype(waves)::value;
+    typedef Share<decltype(lg)::value, WAVES, walking_waves<decltype(ve)::value, decltype(nv)::value>()> S;
     const int64_t groups = ceil_div(M, (int64_t)S::kRows);
     auto go = [&](auto with) {
       constexpr bool SUMS = decltype(with)::value;
-      const int64_t grid = std::min(groups, SUMS ? kWalkers : kMostWorkgroups);
+      // a few rows more than a workgroup has in hand: one does them all, and nothing is left to add up
+      const int64_t grid = !SUMS ? std::min(groups, kMostWorkgroups) : groups <= 2 ? 1 : walkers(groups, WAVES);
+      Sums out = {grid > 1 ? partial : nullptr, dgamma, dbeta, accumulate};
       if (SUMS) parts = grid;
-      layer_norm_grad_kernel<T, decltype(ve)::value, decltype(nv)::value, decltype(lg)::value, decltype(waves)::value,
-                             decltype(ragged)::value, SUMS>
-          <<<dim3((uint32_t)grid), S::kThreads, SUMS ? (size_t)(2 * D * 4) : 0, s>>>(X, M, D, ldx, gamma, bf16, stats, dY, lddy, dX,
-                                                                                   lddx, partial);
+      layer_norm_grad_kernel<T, decltype(ve)::value, decltype(nv)::value, decltype(lg)::value, WAVES, decltype(ragged)::value, SUMS>
+          <<<dim3((uint32_t)grid), S::kThreads, SUMS && WAVES == 1 ? (size_t)(S::kThreads / 64 * 2 * D * 4) : 0, s>>>(
+              X, M, D, ldx, gamma, bf16, stats, dY, lddy, dX, lddx, out);
     };
-    if (sums && !apart) go(std::true_type());
+    if constexpr (decltype(ve)::value == 8 && WAVES == 16 && decltype(nv)::value == 4) go(std::false_type());
+    else if (sums) go(std::true_type());
     else go(std::false_type());
   };
   if (D < VE) {
     launch(Int<1>(), Int<1>(), Int<3>(), Int<1>(), std::false_type());
   } else {
-    const bool found = with_row_form<0>(ceil_div(D, (int64_t)VE), [&](auto nv, auto lg, auto waves) {
+    const bool found = with_row_form<true>(vecs, [&](auto nv, auto lg, auto waves) {
       if (D % VE) launch(Int<VE>(), nv, lg, waves, std::true_type());
       else launch(Int<VE>(), nv, lg, waves, std::false_type());
     });
@@ -484,8 +549,8 @@ int norm_grad_of(const T *X, int64_t M, int64_t D, int64_t ldx, const void *gamm
       layer_norm_grad_long_kernel<T><<<dim3((uint32_t)std::min(M, kMostWorkgroups)), 64 * kLongWaves, 0, s>>>(
           X, M, D, ldx, gamma, bf16, stats, dY, lddy, dX, lddx);
   }
-  if (const int rc = check_launch(); rc != BSR_OK || !sums) return rc;
-  const int64_t grid = std::min(ceil_div(2 * D, (int64_t)64), kMostWorkgroups);
+  if (const int rc = check_launch(); rc != BSR_OK || !sums || (parts == 1 && !apart)) return rc;
+  const int64_t grid = std::min(ceil_div(2 * D, (int64_t)32), kMostWorkgroups);
   layer_norm_join_kernel<<<dim3((uint32_t)grid), 1024, 0, s>>>(partial, parts, D, dgamma, dbeta, accumulate);
   return check_launch();
 }
