@@ -51,7 +51,7 @@ constexpr uint32_t kRange = 0x80000000u;           // bytes that a tile's offset
 struct ProductArgs {
   const void *A, *B;
   int64_t M, N, K, lda, ldb;       // N: columns of the result; of the gated product, of H
-  int64_t up;                      // gated: column of B from which U's weights are
+  int64_t up, cols;                // gated: column of B from which U's weights are, columns of B
   void *out, *gu;                  // result (H); GU or null
   float *partial;                  // split: [splits][M][N or 2N] binary32
   int64_t ldo, ldgu;
@@ -78,6 +78,6 @@ inline int32_t blocks_for(int64_t threads) { return (int32_t)std::min(ceil_div(t
 
 // gated_bf16.hip, gated_f32.hip: the product and, of a split contraction, the sum of the parts.
 int launch_product_bf16(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s);
-int launch_product_f32(const Plan &p, const ProductArgs &a, bool gated, bool loose, hipStream_t s);
+int launch_product_f32(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s);
 
 }  // namespace bsr

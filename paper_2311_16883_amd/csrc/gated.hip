@@ -3,7 +3,7 @@
 //   forward   [G | U] = X W,  H = act(G) * U         (W as it is stored, [D x 2F]: the contraction is its slow axis)
 //   backward  dGU from GU and dH, then dX = dGU W^T  (both operands contiguous along the contraction)
 //
-// Operands whose rows are not whole 16-byte vectors are copied into the workspace first, rows padded; then so is the contraction,
+// bfloat16 operands whose rows are not whole words are copied into the workspace first, rows padded; then so is the contraction,
 // with zeros.  Where there are few tiles the contraction is split and a second kernel adds the parts up, in order.
 #include "gated.h"
 
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kFewThreads) void gated_few_kernel(int act, const T
   }
 }
 
-// ---- operands in whole vectors ----
+// ---- operands in whole words ----
 
 // Columns [from, from + cols) of a matrix into rows of `pitch` elements from column `to` on, zeros up to column `to + padded`.
 struct PackJob {
@@ -220,14 +220,10 @@ int64_t padded(int64_t n, int dtype) {
   return ceil_div(n, ve) * ve;
 }
 
-// Whether a product takes an operand as it is: rows of whole vectors at 16 bytes (binary32: of any kind, by 4-byte copies), and
-// offsets of a tile within its range.
-bool whole_vectors(const void *p, int dtype, int64_t ld, int64_t inner) {
-  const int64_t e = elem_bytes(dtype);
-  return (uintptr_t)p % 16 == 0 && ld * e % 16 == 0 && inner * e % 16 == 0;
-}
+// Whether a product takes an operand as it is: rows of whole words at whole words (binary32 always), offsets of a tile within its range.
 bool in_place(const void *p, int dtype, int64_t ld, int64_t inner) {
-  return ld * elem_bytes(dtype) * 256 < (int64_t)kRange && (dtype == BSR_F32 || whole_vectors(p, dtype, ld, inner));
+  const int64_t e = elem_bytes(dtype);
+  return (uintptr_t)p % 4 == 0 && ld * e % 4 == 0 && inner * e % 4 == 0 && ld * e * 256 < (int64_t)kRange;
 }
 
 // Tiles that are never the best of their kind are not there: binary32 is bound by the matrix cores in any of them (8192 rows: 125
@@ -242,13 +238,13 @@ bool has_tile(Tile t, int dtype, bool gated) {
 // 2999 x 3080 x 808 in 128 x 128 tiles alone in their unit 33, otherwise 45).  A tile's beginning and end cost as much as some more
 // of the contraction.  (Whether GU is written has no part in it: H would have other bits with GU than without.)
 double estimate_us(Tile t, int64_t M, int64_t N, int64_t K, int dtype, bool gated, int64_t splits) {
-  const double rates[2][6][2] = {{{4.9, 4.9}, {4.6, 4.4}, {2.4, 3.9}, {3.4, 3.4}, {2.9, 3.3}, {1.0, 1.8}},
-                                 {{0.54, 0.54}, {0.5, 0.54}, {0.46, 0.53}, {0.46, 0.46}, {0.45, 0.5}, {0.3, 0.45}}};
+  const double rates[2][6][2] = {{{4.9, 4.9}, {4.6, 4.4}, {2.4, 3.9}, {3.4, 3.4}, {2.9, 2.8}, {1.0, 1.8}},
+                                 {{0, 0}, {0, 0}, {0.46, 0.53}, {0, 0}, {0.45, 0.47}, {0.3, 0.45}}};
   const TileSize &s = kTiles[t];
   const bool f32 = dtype == BSR_F32;
   const int64_t tiles = ceil_div(M, (int64_t)s.rows) * ceil_div(N, (int64_t)(gated ? s.cols / 2 : s.cols)) * splits;
   const int64_t each = ceil_div(tiles, (int64_t)kCus);
-  const double rate = rates[f32][t][each > 1 && t != kTile256 && t != kTile128Alone];
+  const double rate = rates[f32][t][each > 1];
   const double more = (f32 ? 24.0 : 128.0) * (gated && splits == 1 ? 2.0 : 1.0);
   double us = 3.0 + (double)each * s.rows * s.cols * 2.0 * (ceil_div(K, splits) + more) / (rate * 1e6);
   if (splits > 1) us += 4.0 + (double)splits * M * N * (gated ? 2 : 1) * 8.0 / 4e6;
@@ -285,9 +281,9 @@ size_t partial_bytes(const Plan &p, int64_t M, int64_t N, bool gated) {
 }
 
 template <typename T>
-int product_of(const Plan &p, const ProductArgs &a, bool gated, bool loose, hipStream_t s) {
+int product_of(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s) {
   if constexpr (sizeof(T) == 2) return launch_product_bf16(p, a, gated, s);
-  else return launch_product_f32(p, a, gated, loose, s);
+  else return launch_product_f32(p, a, gated, s);
 }
 
 // What goes into the workspace, in this order.
@@ -358,6 +354,7 @@ int forward(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, vo
   a.B = g.W;
   a.ldb = g.ldw;
   a.up = g.F;
+  a.cols = 2 * g.F;
   a.M = g.M;
   a.N = g.F;
   a.K = g.D;
@@ -376,7 +373,7 @@ int forward(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, vo
   if (l.b != 0) {
     a.B = at + l.a;
     a.up = padded(g.F, g.dtype);
-    a.ldb = 2 * a.up;
+    a.ldb = a.cols = 2 * a.up;
     for (int i = 0; i < 2; ++i) add(g.W, g.D, g.ldw, i * g.F, g.F, at + l.a, a.ldb, i * a.up, a.up);
   }
   if (n > 0) {
@@ -390,9 +387,8 @@ int forward(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, vo
   a.gu = GU;
   a.ldgu = ldgu;
   a.partial = reinterpret_cast<float *>(at + l.a + l.b);
-  const bool loose = g.D > 0 && !(whole_vectors(a.A, g.dtype, a.lda, g.D) && whole_vectors(a.B, g.dtype, a.ldb, a.up));
   a.act = g.act;
-  return product_of<T>(l.plan, a, true, loose, s);
+  return product_of<T>(l.plan, a, true, s);
 }
 
 template <typename T>
@@ -429,8 +425,7 @@ int backward(const GatedArgs &g, const void *GU, int64_t ldgu, const void *dH, i
   a.out = dX;
   a.ldo = lddx;
   a.partial = reinterpret_cast<float *>(at + l.a + l.b);
-  const bool loose = g.F > 0 && !(whole_vectors(a.A, g.dtype, a.lda, 2 * g.F) && whole_vectors(a.B, g.dtype, a.ldb, 2 * g.F));
-  return product_of<T>(l.plan, a, false, loose, s);
+  return product_of<T>(l.plan, a, false, s);
 }
 
 }  // namespace

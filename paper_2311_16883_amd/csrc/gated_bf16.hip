@@ -4,7 +4,7 @@
 namespace bsr {
 
 int launch_product_bf16(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s) {
-  return gated ? run_product<uint16_t, true>(p, a, false, s) : run_product<uint16_t, false>(p, a, false, s);
+  return gated ? run_product<uint16_t, true>(p, a, s) : run_product<uint16_t, false>(p, a, s);
 }
 
 }  // namespace bsr

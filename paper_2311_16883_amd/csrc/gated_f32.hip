@@ -3,8 +3,8 @@
 
 namespace bsr {
 
-int launch_product_f32(const Plan &p, const ProductArgs &a, bool gated, bool loose, hipStream_t s) {
-  return gated ? run_product<float, true>(p, a, loose, s) : run_product<float, false>(p, a, loose, s);
+int launch_product_f32(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s) {
+  return gated ? run_product<float, true>(p, a, s) : run_product<float, false>(p, a, s);
 }
 
 }  // namespace bsr

@@ -90,19 +90,16 @@ __device__ __forceinline__ void store_tile(T *out, int64_t ld, int64_t m, int64_
 }
 
 // GATED: B is W [K x 2N], contraction the slow axis, and the result act(G) * U; otherwise B is [N x K] and the result A B^T.
-// A wave's tile is TM x TN fragments of 32 x 32; WM x WN waves; RING stages of ROW bytes of the contraction in LDS.  LOOSE: copies of
-// 4 bytes a lane, for binary32 rows that are not whole vectors (four times as many copies, which binary32 has the time for).
-template <typename T, bool GATED, int TM, int TN, int WM, int WN, int RING, int ROW, bool LOOSE, bool SPLIT>
+// A wave's tile is TM x TN fragments of 32 x 32; WM x WN waves; RING stages of ROW bytes of the contraction in LDS.  WHOLE: the contraction
+// and the rows of B end with whole vectors (what it takes where they do not costs the others 2 to 10 %).
+template <typename T, bool GATED, int TM, int TN, int WM, int WN, int RING, int ROW, bool WHOLE, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN, (TM * TN > 8 ? 1 : 2)) void product_kernel(ProductArgs a) {
   constexpr int kWaves = WM * WN;
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN;            // BN: columns of B in a tile; of a gated tile half belong to G
   constexpr int kStageBytes = (BM + BN) * ROW;
   constexpr int kCopiesA = BM * ROW / 1024, kCopiesB = BN * ROW / 1024, kCopies = kCopiesA + kCopiesB;
-  constexpr int kBytes = LOOSE ? 4 : 16, kParts = 16 / kBytes;   // bytes of a lane per copy, copies per KB
-  constexpr int kBlocks = (kCopies + kWaves - 1) / kWaves;       // KBs of a wave per stage; the last waves have one less
-  constexpr int kLess = kBlocks * kWaves - kCopies;
-  constexpr int kMine = kBlocks * kParts;                        // copies of a wave per stage
-  static_assert(!LOOSE || sizeof(T) == 4, "4-byte copies are for binary32");
+  constexpr int kMine = (kCopies + kWaves - 1) / kWaves;         // copies of a wave per stage; the last waves have one less
+  constexpr int kLess = kMine * kWaves - kCopies;
   constexpr int SK = ROW / (int)sizeof(T), VE = kVec<T>;        // contraction of a stage
   constexpr int kPhases = ROW / 32;                              // parts of a stage that are multiplied at a time
   __shared__ __attribute__((aligned(1024))) uint8_t ring[RING * kStageBytes];
@@ -135,47 +132,79 @@ __global__ __launch_bounds__(64 * WM * WN, (TM * TN > 8 ? 1 : 2)) void product_k
   const uint8_t *const baseB = static_cast<const uint8_t *>(a.B) +
                                (GATED ? first_stage * SK * a.ldb + n0 : n0 * a.ldb + first_stage * SK) * (int64_t)sizeof(T);
   const int64_t stepA = SK * (int64_t)sizeof(T), stepB = GATED ? SK * a.ldb * (int64_t)sizeof(T) : SK * (int64_t)sizeof(T);
+  const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)ring;
+  const int32_t k_all = (int32_t)(a.K - first_stage * SK);       // contraction from the first stage on
+  // bytes from the tile's part of B to the end of the matrix: whole vectors of its last row may lie in part beyond it
+  const int64_t endB = ((a.K - 1 - first_stage * SK) * a.ldb + a.cols - n0) * (int64_t)sizeof(T);
+  // the stage in which the contraction ends inside a vector, if it does
+  const int32_t tail = !WHOLE && a.K % VE != 0 ? (int32_t)(a.K / SK - first_stage) : -1;
   uint32_t voff[kMine];          // per-lane offset of a copy
   int32_t kfirst[kMine];         // first index of the contraction (within the stage) that the lane's bytes belong to
 #pragma unroll
   for (int i = 0; i < kMine; ++i) {
-    const int c = wave + i / kParts * kWaves;
-    const int at = i % kParts * 64 * kBytes + lane * kBytes;      // place of the lane's bytes in the KB
-    const int word = at % 16 / 4;                                 // (LOOSE) element of a 16-byte chunk
+    const int c = wave + i * kWaves;
     if (c < kCopiesA || !GATED) {
       // rows of ROW bytes
       const bool isA = c < kCopiesA;
-      const int row = (isA ? c : c - kCopiesA) * (1024 / ROW) + at / ROW;
+      const int row = (isA ? c : c - kCopiesA) * (1024 / ROW) + lane / (ROW / 16);
       const int64_t last = (isA ? a.M - m0 : a.N - n0) - 1;
-      kfirst[i] = ((at % ROW / 16) ^ permuted(row)) * VE + word;
+      kfirst[i] = (lane % (ROW / 16) ^ permuted(row)) * VE;
       voff[i] = (uint32_t)((min((int64_t)row, last) * (isA ? a.lda : a.ldb) + kfirst[i]) * (int64_t)sizeof(T));
+      kfirst[i] += VE - 1;       // (a vector in which the contraction ends: issue_tail)
     } else {
       // rows of 128 bytes of a panel: the first half of the panels from G's columns, the others from U's
       constexpr int kPanelCols = 128 / (int)sizeof(T), kPanels = BN / kPanelCols, kPerPanel = SK / 8;
-      const int p = (c - kCopiesA) / kPerPanel, r = ((c - kCopiesA) % kPerPanel) * 8 + at / 128;
-      const int chunk = at % 128 / 16;
-      const int64_t col = (p % (kPanels / 2)) * kPanelCols + (sizeof(T) == 2 ? chunk ^ (4 * ((r >> 1) & 1)) : chunk) * VE + word;
-      const bool there = n0 + col < a.N;
-      voff[i] = there ? (uint32_t)((r * a.ldb + (p >= kPanels / 2 ? a.up : 0) + col) * (int64_t)sizeof(T)) : kBeyond;
+      const int p = (c - kCopiesA) / kPerPanel, r = ((c - kCopiesA) % kPerPanel) * 8 + (lane >> 3);
+      const int chunk = sizeof(T) == 2 ? (lane & 7) ^ (4 * ((r >> 1) & 1)) : lane & 7;
+      const int64_t col = (p % (kPanels / 2)) * kPanelCols + chunk * VE;
+      voff[i] = n0 + col < a.N ? (uint32_t)((r * a.ldb + (p >= kPanels / 2 ? a.up : 0) + col) * (int64_t)sizeof(T)) : kBeyond;
       kfirst[i] = r;
     }
   }
-  const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)ring;
-  const int32_t k_all = (int32_t)(a.K - first_stage * SK);       // contraction from the first stage on
-  const bool with_last = kLess == 0 || wave + (kBlocks - 1) * kWaves < kCopies;
+  const bool with_last = kLess == 0 || wave + (kMine - 1) * kWaves < kCopies;
+  // The range of B's part of a stage: the hardware reads words beyond it as zeros.
+  auto range_of = [&](bool isA, int stage) -> uint32_t {
+    if (WHOLE || !GATED || isA) return kRange;
+    const int64_t left = endB - stage * stepB;
+    return left < 0 ? 0u : left < (int64_t)kRange ? (uint32_t)left : kRange;
+  };
   auto issue = [&](int stage, uint32_t slot, int i) {           // copy i of this wave's of a stage
-    const int c = wave + i / kParts * kWaves;
+    const int c = wave + i * kWaves;
     const uint32_t v = kfirst[i] < k_all - stage * SK ? voff[i] : kBeyond;
-    if (kLess != 0 && i / kParts == kBlocks - 1 && !with_last) return;
+    if (kLess != 0 && i == kMine - 1 && !with_last) return;
     // (known at compile time where the waves share A's copies evenly)
-    const bool isA = kCopiesA % kWaves == 0 ? i / kParts < kCopiesA / kWaves : c < kCopiesA;
+    const bool isA = kCopiesA % kWaves == 0 ? i < kCopiesA / kWaves : c < kCopiesA;
     const uint8_t *const base = isA ? baseA + stage * stepA : baseB + stage * stepB;
-    copy_to_lds<kBytes>(make_rsrc(base, kRange), ring_lds + slot * kStageBytes + (uint32_t)(c * 1024 + i % kParts * 64 * kBytes), v);
+    copy_to_lds<16>(make_rsrc(base, range_of(isA, stage)), ring_lds + slot * kStageBytes + (uint32_t)c * 1024u, v);
+  };
+  // The stage in which the contraction ends inside a vector: rows along it word by word, the words behind its end as zeros.  (More
+  // copies than the waits below count on, which then wait for more than they need.)
+  auto issue_tail = [&](int stage, uint32_t slot) {
+    const int32_t left = k_all - stage * SK;
+    for (int c = wave; c < kCopies; c += kWaves) {
+      const bool isA = c < kCopiesA;
+      const uint8_t *const base = isA ? baseA + stage * stepA : baseB + stage * stepB;
+      const uint32_t to = ring_lds + slot * kStageBytes + (uint32_t)c * 1024u;
+      if (GATED && !isA) continue;
+      for (int part = 0; part < 4; ++part) {
+        const int at = part * 256 + lane * 4, row = (isA ? c : c - kCopiesA) * (1024 / ROW) + at / ROW;
+        const int64_t last = (isA ? a.M - m0 : a.N - n0) - 1;
+        const int k = ((at % ROW / 16) ^ permuted(row)) * VE + at % 16 / (int)sizeof(T);
+        const uint32_t v = (uint32_t)((min((int64_t)row, last) * (isA ? a.lda : a.ldb) + k) * (int64_t)sizeof(T));
+        copy_to_lds<4>(make_rsrc(base, kRange), to + (uint32_t)(part * 256), k < left ? v : kBeyond);
+      }
+    }
+  };
+  auto issue_any = [&](int stage, uint32_t slot, int i) {
+    if constexpr (WHOLE) return issue(stage, slot, i);
+    const bool isA = kCopiesA % kWaves == 0 ? i < kCopiesA / kWaves : wave + i * kWaves < kCopiesA;
+    if (stage != tail || (GATED && !isA)) issue(stage, slot, i);
+    if (stage == tail && i == kMine - 1) issue_tail(stage, slot);
   };
   // the copies of all but the last `STAGES` stages that this wave issued have landed
   auto wait_for = [&](auto stages_c) {
     constexpr int N = decltype(stages_c)::value;
-    if (!with_last) wait_copies<N * (kBlocks - 1) * kParts>();
+    if (!with_last) wait_copies<N * (kMine - 1)>();
     else wait_copies<N * kMine>();
   };
 
@@ -252,7 +281,7 @@ __global__ __launch_bounds__(64 * WM * WN, (TM * TN > 8 ? 1 : 2)) void product_k
   if (stages > 0) {
     for (int s = 0; s < RING; ++s)
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) issue(s, (uint32_t)s, i);
+      for (int i = 0; i < kMine; ++i) issue_any(s, (uint32_t)s, i);
     wait_for(std::integral_constant<int, RING - 1>());
     asm volatile("s_barrier" ::: "memory");
     Frags f0, f1;
@@ -271,7 +300,7 @@ __global__ __launch_bounds__(64 * WM * WN, (TM * TN > 8 ? 1 : 2)) void product_k
       const uint32_t next = slot == RING - 1 ? 0 : slot + 1;
       multiply(f1, std::integral_constant<int, TM + TN + kMine>(), [&](int k) {
         if (k < TM + TN) load_frag(f0, next, 0, k);
-        else issue(s + RING, slot, k - TM - TN);
+        else issue_any(s + RING, slot, k - TM - TN);
       });
       slot = next;
       held(f0);
@@ -367,33 +396,33 @@ __global__ __launch_bounds__(256) void join_kernel(int act, const float *__restr
   }
 }
 
-template <typename T, bool GATED, bool LOOSE, bool SPLIT>
+template <typename T, bool GATED, bool WHOLE, bool SPLIT>
 void launch_tile(Tile t, dim3 grid, const ProductArgs &a, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if constexpr (!SPLIT) {
       if (t == kTile256) {
-        product_kernel<T, GATED, 4, 2, 2, 4, 2, 128, LOOSE, SPLIT><<<grid, 512, 0, s>>>(a);
+        product_kernel<T, GATED, 4, 2, 2, 4, 2, 128, WHOLE, SPLIT><<<grid, 512, 0, s>>>(a);
         return;
       }
     }
     if constexpr (GATED) {
       if (t == kTileWide) {
-        product_kernel<T, GATED, 2, 2, 2, 4, 3, 64, LOOSE, SPLIT><<<grid, 512, 0, s>>>(a);
+        product_kernel<T, GATED, 2, 2, 2, 4, 3, 64, WHOLE, SPLIT><<<grid, 512, 0, s>>>(a);
         return;
       }
     }
     if (t == kTile128Alone) {
-      product_kernel<T, GATED, 2, 2, 2, 2, 3, 128, LOOSE, SPLIT><<<grid, 256, 0, s>>>(a);
+      product_kernel<T, GATED, 2, 2, 2, 2, 3, 128, WHOLE, SPLIT><<<grid, 256, 0, s>>>(a);
       return;
     }
   }
-  if (t == kTile128) product_kernel<T, GATED, 2, 2, 2, 2, 2, 128, LOOSE, SPLIT><<<grid, 256, 0, s>>>(a);
-  else if (t == kTile64) product_kernel<T, GATED, 1, 2, 2, 2, 3, 128, LOOSE, SPLIT><<<grid, 256, 0, s>>>(a);
-  else product_kernel<T, GATED, 1, 2, 1, 4, 4, 64, LOOSE, SPLIT><<<grid, 256, 0, s>>>(a);
+  if (t == kTile128) product_kernel<T, GATED, 2, 2, 2, 2, 2, 128, WHOLE, SPLIT><<<grid, 256, 0, s>>>(a);
+  else if (t == kTile64) product_kernel<T, GATED, 1, 2, 2, 2, 3, 128, WHOLE, SPLIT><<<grid, 256, 0, s>>>(a);
+  else product_kernel<T, GATED, 1, 2, 1, 4, 4, 64, WHOLE, SPLIT><<<grid, 256, 0, s>>>(a);
 }
 
 template <typename T, bool GATED>
-int run_product(const Plan &p, ProductArgs a, bool loose, hipStream_t s) {
+int run_product(const Plan &p, ProductArgs a, hipStream_t s) {
   a.tiles_n = p.tiles_n;
   a.splits = p.splits;
   a.stages_per_split = p.stages_per_split;
@@ -402,21 +431,17 @@ int run_product(const Plan &p, ProductArgs a, bool loose, hipStream_t s) {
   constexpr int64_t kMostItems = int64_t(1) << 22;
   const int64_t height = kTiles[p.tile].rows;
   const int64_t rows_at_once = p.splits > 1 ? a.M : std::max<int64_t>(1, kMostItems / p.tiles_n) * height;
-  const ProductArgs whole = a;
-  for (int64_t r = 0; r < whole.M; r += rows_at_once) {
-    a.M = std::min(whole.M - r, rows_at_once);
-    a.A = static_cast<const T *>(whole.A) + r * whole.lda;
-    a.out = static_cast<T *>(whole.out) + r * whole.ldo;
-    a.gu = whole.gu != nullptr ? static_cast<T *>(whole.gu) + r * whole.ldgu : nullptr;
+  const ProductArgs all = a;
+  for (int64_t r = 0; r < all.M; r += rows_at_once) {
+    a.M = std::min(all.M - r, rows_at_once);
+    a.A = static_cast<const T *>(all.A) + r * all.lda;
+    a.out = static_cast<T *>(all.out) + r * all.ldo;
+    a.gu = all.gu != nullptr ? static_cast<T *>(all.gu) + r * all.ldgu : nullptr;
     a.tiles_m = (int32_t)ceil_div(a.M, height);
     const dim3 grid((uint32_t)(ceil_div((int64_t)a.tiles_m * a.tiles_n * a.splits, (int64_t)8) * 8));
-    auto go = [&](auto loose_c) {
-      constexpr bool LOOSE = decltype(loose_c)::value && sizeof(T) == 4;
-      if (p.splits > 1) launch_tile<T, GATED, LOOSE, true>(p.tile, grid, a, s);
-      else launch_tile<T, GATED, LOOSE, false>(p.tile, grid, a, s);
-    };
-    if (loose) go(std::true_type());
-    else go(std::false_type());
+    const bool whole = a.K % kVec<T> == 0 && (!GATED || a.cols % (2 * kVec<T>) == 0);
+    if (p.splits > 1) whole ? launch_tile<T, GATED, true, true>(p.tile, grid, a, s) : launch_tile<T, GATED, false, true>(p.tile, grid, a, s);
+    else whole ? launch_tile<T, GATED, true, false>(p.tile, grid, a, s) : launch_tile<T, GATED, false, false>(p.tile, grid, a, s);
     if (const int rc = check_launch(); rc != BSR_OK) return rc;
     if (p.splits > 1) {
       auto join = [&](auto lg) {

@@ -101,7 +101,7 @@ def test_layer_norm_of_nothing():
 
 GATED_SIZES = [(1, 1, 1), (1, 64, 64), (1, 2048, 320), (2, 9, 3), (7, 33, 20), (16, 128, 64), (17, 65, 33), (31, 256, 100), (64, 96, 128), (65, 100, 129),
                (100, 411, 77), (128, 384, 256), (130, 264, 200), (257, 136, 130), (300, 520, 257), (513, 72, 300), (3, 5000, 48),
-               (4, 70, 2200), (2, 33, 4100), (4, 7, 9), (20, 1000, 136), (40, 2500, 72)]
+               (90, 130, 66), (70, 38, 34), (150, 250, 130), (200, 1030, 62), (33, 66, 1002), (4, 70, 2200), (2, 33, 4100), (4, 7, 9), (20, 1000, 136), (40, 2500, 72)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
