@@ -1,0 +1,359 @@
+"""The layer operators together, as a training step uses them: norm, pruned input, gated block, products of torch, the way back with
+the weights' block-sparse gradient, AdamW.  Against automatic differentiation in binary64 on the CPU, captured into graphs and replayed,
+on another stream, and over many steps with 8-bit moments beside 32-bit ones."""
+import numpy as np
+import pytest
+import torch
+
+import layer_plain as P
+from layer_plain import f64, randn
+from paper_2311_16883_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+M, D, F, OUT = 96, 64, 96, 48
+
+
+class Block:
+    """gamma, beta, W [D x 2F], V [F x OUT] in binary32 and their copies of the compute type, gradients, one AdamW batch over all."""
+
+    def __init__(self, dtype, bits, seed=0):
+        self.dtype = dtype
+        self.master = [randn(seed, D) * 0.1 + 1, randn(seed + 1, D) * 0.1, randn(seed + 2, D, 2 * F) * D ** -0.5, randn(seed + 3, F, OUT) * F ** -0.5]
+        self.master = [p.cuda() for p in self.master]
+        self.grads = [torch.zeros_like(p) for p in self.master]
+        self.copies = [p.bfloat16() for p in self.master]
+        self.batch = B.AdamWBatch(self.master, self.grads, bits=bits, copies=self.copies, weight_decay=[0.0, 0.0, 0.1, 0.1])
+        self.step_number = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def work(self):
+        return self.master if self.dtype == torch.float32 else self.copies
+
+    def gradients(self, x, t, keep=1.0):
+        """-> y, dX; the weights' gradients go to self.grads."""
+        gamma, beta, W, V = self.work()
+        xn, stats = B.bsr_layer_norm(x, gamma, beta, want_stats=True)
+        mask = B.bsr_score_select(xn, 32, 32, keep)
+        kept = B.bsr_compress(xn, 32, 32, mask, B.bsr_keep_count(mask.numel(), keep))
+        h, gu = B.bsr_gated_ff(xn, W, act="gelu", want_GU=True)
+        y = h @ V
+        dh = (t @ V.t()).contiguous()
+        torch.mm(h.t().float(), t.float(), out=self.grads[3])
+        dxn, dgu = B.bsr_gated_ff_grad(gu, dh, W, act="gelu", dGU=gu)
+        B.bsr_t_dense_matmul(*kept, M, D, 32, 32, dgu, dW=self.grads[2])
+        dx, _, _ = B.bsr_layer_norm_grad(x, gamma, stats, dxn, dX=dxn, dgamma=self.grads[0], dbeta=self.grads[1])
+        return y, dx
+
+    def update(self, step=None):
+        B.bsr_adamw_batched(self.batch, lr=1e-2, step=self.step_number if step is None else step, seed=11)
+
+    def state(self):
+        torch.cuda.synchronize()
+        return [t.clone() for t in (*self.master, *self.copies, *self.grads, *(s for st in self.batch.states for s in st))]
+
+
+def test_gradients_of_a_block_against_automatic_differentiation():
+    b = Block(torch.float32, 32)
+    x, t = randn(9, M, D), randn(10, M, OUT)
+    y, dx = b.gradients(x.cuda(), t.cuda())
+    p = [w.double().cpu().requires_grad_() for w in b.master]
+    xd = x.double().requires_grad_()
+    xn = torch.nn.functional.layer_norm(xd, (D,), p[0], p[1], float(np.float32(1e-5)))
+    g, u = (xn @ p[2]).split(F, dim=1)
+    want = (torch.nn.functional.gelu(g) * u) @ p[3]
+    want.backward(t.double())
+    # chains of four products of up to 192 binary32 terms of either sign: a few hundred roundings of the largest value
+    for got, ref in [(y, want.detach()), (dx, xd.grad)] + [(a, q.grad) for a, q in zip(b.grads, p)]:
+        assert float((got.double().cpu() - ref).abs().max()) <= 500 * P.U * float(ref.abs().max())
+    before = [w.double().cpu() for w in b.master]
+    b.update(step=1)
+    for w, old, q, decay in zip(b.master, before, p, (0.0, 0.0, 0.1, 0.1)):
+        # the first step: m / (1 - beta1) = g and v / (1 - beta2) = g^2
+        moved = 1e-2 * q.grad / (q.grad.abs() + 1e-8)
+        ref = old * (1 - 1e-2 * decay) - moved
+        sure = q.grad.abs() > 1e-3 * q.grad.abs().max()
+        assert float(((w.double().cpu() - ref).abs() * sure).max()) <= 1e-5      # (g itself is 500 U of the largest off, 3 % of 1e-3 of it at most)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_pruned_input_prunes_the_gradient_of_its_weights_alone(bits):
+    x, t = randn(9, M, D, dtype="bf16").cuda(), randn(10, M, OUT, dtype="bf16").cuda()
+    full, half = Block(torch.bfloat16, bits), Block(torch.bfloat16, bits)
+    (y0, dx0), (y1, dx1) = full.gradients(x, t), half.gradients(x, t, keep=0.5)
+    assert torch.equal(y0, y1) and torch.equal(dx0, dx1)
+    for i in (0, 1, 3):
+        assert torch.equal(full.grads[i], half.grads[i])
+    assert not torch.equal(full.grads[2], half.grads[2])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_steps_captured_and_replayed(dtype, bits):
+    """Whole steps as graphs, their number a tensor that the graph counts up; replays between eager work of the same kinds, against
+    eager steps from the same start."""
+    xs, ts = [randn(20 + i, M, D).to(dtype).cuda() for i in range(5)], [randn(30 + i, M, OUT).to(dtype).cuda() for i in range(5)]
+    eager = Block(dtype, bits)
+    states = []
+    for i in range(5):
+        eager.gradients(xs[i], ts[i], keep=0.5)
+        eager.update(step=i + 1)
+        states.append(eager.state())
+    b, other = Block(dtype, bits), Block(dtype, bits, seed=50)
+    x, t = xs[0].clone(), ts[0].clone()
+
+    def step(block):
+        block.step_number += 1
+        block.gradients(x, t, keep=0.5)
+        block.update()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(other)                                  # (libraries initialise what they need outside of the capture)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(b)
+    second = torch.cuda.CUDAGraph()                  # another graph in the same memory pool: its workspaces may be the first one's
+    with torch.cuda.graph(second, pool=graph.pool()):
+        step(other)
+    for i in range(5):
+        x.copy_(xs[i])
+        t.copy_(ts[i])
+        graph.replay()
+        got = b.state()
+        for k, (u, v) in enumerate(zip(got, states[i])):
+            assert torch.equal(u, v), (i, k)
+        second.replay()
+        other.gradients(xs[i], ts[i])
+        torch.cuda.synchronize()
+
+
+def test_every_operator_on_a_stream_of_its_own():
+    x, w = randn(1, 300, 200, dtype="bf16").cuda(), randn(2, 200, 600, dtype="bf16").cuda()
+    dh = randn(3, 300, 300, dtype="bf16").cuda()
+
+    def run(stream):
+        y, stats = B.bsr_layer_norm(x, want_stats=True, stream=stream)
+        h, gu = B.bsr_gated_ff(x, w, want_GU=True, stream=stream)
+        dx, dgu = B.bsr_gated_ff_grad(gu, dh, w, stream=stream)
+        d, g, b = B.bsr_layer_norm_grad(x, None, stats, x, stream=stream)
+        p, m = x.float().clone(), x.float().clone()
+        torch.cuda.synchronize()
+        batch = B.AdamWBatch([p], [m], bits=8)
+        torch.cuda.synchronize()
+        B.bsr_adamw_batched(batch, lr=0.1, step=3, stream=stream)
+        torch.cuda.synchronize()
+        v = B.bsr_adamw_state_values(batch.states[0][0], batch.states[0][2][0], "m", stream=stream)
+        torch.cuda.synchronize()
+        return y, stats, h, gu, dx, dgu, d, g, b, p, v
+    want = run(None)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    for s in (stream, stream.cuda_stream):
+        for a, b in zip(run(s), want):
+            assert torch.equal(a, b)
+
+
+def test_moments_in_8_bits_follow_those_in_32():
+    """600 steps on gradients with a mean and noise of their own per element: to the nearest, sqrt(v) would never leave its start
+    (a step changes it by 0.05 %, its codes are 3 to 6 % apart)."""
+    n = 4096
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    mean = torch.randn(n, generator=g, device="cuda") * torch.exp(torch.randn(n, generator=g, device="cuda"))
+    params = [torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")]
+    grads = [torch.empty(n, device="cuda") for _ in range(2)]
+    batches = [B.AdamWBatch(params[:1], grads[:1], bits=32), B.AdamWBatch(params[1:], grads[1:], bits=8)]
+    for step in range(1, 601):
+        grads[0].copy_(mean * (1 + 0.5 * torch.randn(n, generator=g, device="cuda")))
+        grads[1].copy_(grads[0])
+        for b in batches:
+            B.bsr_adamw_batched(b, lr=1e-3, step=step, seed=77)
+    root = torch.sqrt(batches[0].states[0][1])
+    m8, r8, scales = batches[1].states[0]
+    got = B.bsr_adamw_state_values(r8, scales[1], "r")
+    # One rounding of a root that moved by delta from a code has the variance f (1 - f) d^2 <= |delta| d, with d <= r / 16 the codes'
+    # distance and f = |delta| / d.  delta = r (1 - beta2) / 2 * (g^2 / r^2 - 1), of a size that is 0.85 r (1 - beta2) / 2 in the mean
+    # square for g = mean * (1 + n / 2) (r^2 = 1.25 mean^2, var(g^2) = (1 + 1/8) mean^4).  An error of the root shrinks by (1 - beta2) a
+    # step, so its variance settles at no more than (0.85 * 0.0005 / 16) / (2 * 0.001) = 0.0133: a spread of 11.6 %, without a mean
+    # (of second order: 0.0133 / 2).
+    off = (got / root - 1)
+    assert float(off.mean().abs()) < 0.0133 / 2 + 3 * 0.116 / n ** 0.5 and float(off.std()) < 0.116 * (1 + 3 / (2 * n) ** 0.5)
+    moved = (params[1] / params[0])
+    # both went 600 times about lr against the sign of the mean gradient; the root's error is the step's, nine in ten within 1.65 spreads
+    assert float((torch.sign(params[0]) == -torch.sign(mean)).float().mean()) > 0.95
+    assert abs(float(moved.median()) - 1) < 0.02 and float((moved - 1).abs().quantile(0.9)) < 1.65 * 0.116
+
+
+def test_moments_of_a_block_with_a_nan_or_an_infinity():
+    for bad in (float("nan"), float("inf")):
+        p, g = torch.ones(1000, device="cuda"), torch.full((1000,), 1e-3, device="cuda")
+        g[300] = bad
+        batch = B.AdamWBatch([p], [g], bits=8)
+        B.bsr_adamw_batched(batch, lr=0.1, step=1)
+        assert bool(p[300].isnan()) and int(p.isnan().sum()) == 1
+        m, r, scales = batch.states[0]
+        for row, code, which in ((0, m, "m"), (1, r, "r")):
+            v = B.bsr_adamw_state_values(code, scales[row], which)
+            assert bool(v[256:384].isnan().all()) and int(v.isnan().sum()) == 128 and bool((v[:256] > 0).all())
+        # and with clean gradients the rest goes on
+        g[300] = 1e-3
+        B.bsr_adamw_batched(batch, lr=0.1, step=2)
+        assert bool(p[256:384].isnan().all()) and int(p.isnan().sum()) == 128
+
+
+def test_tiny_gradients_beside_large_ones_do_not_explode():
+    """A first moment of one unit beside a root that its block's scale can hardly hold."""
+    n = 128 * 64
+    g = torch.full((n,), 1e-7, device="cuda")
+    g[::128] = 1.0
+    p = torch.zeros(n, device="cuda")
+    batch = B.AdamWBatch([p], [g], bits=8)
+    before = p.clone()
+    for step in range(1, 60):
+        if step == 30:
+            g[1::2] = 0.0
+        B.bsr_adamw_batched(batch, lr=1e-3, step=step, seed=step)
+        # |m| <= (sum of beta1^i) of what is held, at least a unit 2^-17 of the largest m; the root at least 2^-18 of the largest root, here
+        # sqrt(1 - beta2^t) of it: a step of an element is never more than 16 of a usual one
+        assert float((p - before).abs().max()) <= 16 * 1e-3 + 1e-6, step
+        before = p.clone()
+
+
+def test_many_tensors_with_and_without_copies():
+    """More tensors than a launch takes, runs of them with copies and without: every element as alone, its number counted over all."""
+    sizes = [1 + 37 * i for i in range(97)]
+    for bits in (32, 8):
+        def build():
+            params, grads = [randn(i, n).cuda() for i, n in enumerate(sizes)], [randn(1000 + i, n, dtype="bf16").cuda() for i, n in enumerate(sizes)]
+            copies = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") if i // 5 % 2 else None for i, n in enumerate(sizes)]
+            return params, grads, copies
+        params, grads, copies = build()
+        batch = B.AdamWBatch(params, grads, bits=bits, copies=copies)
+        for step in (1, 2):
+            B.bsr_adamw_batched(batch, lr=1e-2, step=step, seed=9)
+        # one buffer with all of them, each from a multiple of 128 on
+        starts = np.cumsum([0] + [-(-n // 128) * 128 for n in sizes])
+        p, g = torch.zeros(int(starts[-1]), device="cuda"), torch.zeros(int(starts[-1]), device="cuda", dtype=torch.bfloat16)
+        for (a, b), s, n in zip(zip(*build()[:2]), starts, sizes):
+            p[s:s + n], g[s:s + n] = a, b
+        whole = B.AdamWBatch([p], [g], bits=bits)
+        for step in (1, 2):
+            B.bsr_adamw_batched(whole, lr=1e-2, step=step, seed=9)
+        for i, (s, n) in enumerate(zip(starts, sizes)):
+            assert torch.equal(params[i], p[s:s + n])
+            if copies[i] is not None:
+                assert torch.equal(copies[i], params[i].bfloat16())
+            for k in range(2):
+                assert torch.equal(batch.states[i][k], whole.states[0][k][s:s + n])
+
+
+def test_numbers_on_the_device_are_those_of_the_host():
+    for kind in (32, 8):
+        results = []
+        for device in (False, True):
+            p, g = randn(1, 5000).cuda(), randn(2, 5000).cuda()
+            batch = B.AdamWBatch([p], [g], bits=kind, weight_decay=0.1)
+            for step in (1, 2, 1000):
+                o = dict(lr=3e-3, step=step, grad_scale=0.25)
+                if device:
+                    o = dict(lr=torch.tensor(3e-3, device="cuda"), step=torch.tensor([step], device="cuda"), grad_scale=torch.tensor([0.25], device="cuda"))
+                B.bsr_adamw_batched(batch, **o, seed=4)
+            results.append((p, *batch.states[0]))
+        for a, b in zip(*results):
+            assert torch.equal(a, b)
+
+
+def test_refusals_before_anything_is_launched():
+    x = torch.zeros(40, 24, device="cuda")
+    w = torch.zeros(24, 40, device="cuda")
+    stats = torch.zeros(40, 2, device="cuda")
+    with pytest.raises(ValueError, match="shape of X"):
+        B.bsr_layer_norm_grad(x, None, stats, x[:, :20])
+    with pytest.raises(ValueError, match="gamma must be"):
+        B.bsr_layer_norm(x, torch.zeros(23, device="cuda"))
+    with pytest.raises(ValueError, match="differ in dtype"):
+        B.bsr_layer_norm(x, torch.zeros(24, device="cuda"), torch.zeros(24, device="cuda").bfloat16())
+    with pytest.raises(ValueError, match="stats"):
+        B.bsr_layer_norm_grad(x, None, stats[:39], x)
+    with pytest.raises(ValueError, match="accumulate"):
+        B.bsr_layer_norm_grad(x, None, stats, x, accumulate=True)
+    with pytest.raises(ValueError, match="not wanted"):
+        B.bsr_layer_norm_grad(x, None, stats, x, want_params=False, dgamma=torch.zeros(24, device="cuda"))
+    with pytest.raises(B.BsrError):
+        B.bsr_layer_norm(x.half())
+    with pytest.raises(B.BsrError) as e:
+        B.bsr_layer_norm(x, eps=0.0)
+    assert e.value.code == B.BSR_ERR_VALUE
+    with pytest.raises(ValueError, match="row for each column"):
+        B.bsr_gated_ff(x, w[:23])
+    with pytest.raises(ValueError, match="two columns"):
+        B.bsr_gated_ff(x, w[:, :39])
+    with pytest.raises(ValueError, match="another dtype"):
+        B.bsr_gated_ff(x, w.bfloat16())
+    with pytest.raises(ValueError, match="twice its columns"):
+        B.bsr_gated_ff_grad(x, x[:, :11], w)
+    with pytest.raises(ValueError, match="columns of GU"):
+        B.bsr_gated_ff_grad(x, x[:, :12], w)
+    with pytest.raises(B.BsrError) as e:
+        B.bsr_gated_ff(x, w, act=7)
+    assert e.value.code == B.BSR_ERR_VALUE
+    for ws in (torch.empty(1 << 20, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[::2]):
+        for call in (lambda: B.bsr_gated_ff(x, w, ws=ws), lambda: B.bsr_gated_ff_grad(torch.zeros(40, 40, device="cuda"), torch.zeros(40, 20, device="cuda"), w, ws=ws),
+                     lambda: B.bsr_layer_norm_grad(x, None, stats, x, ws=ws)):
+            with pytest.raises(ValueError, match="ws must be"):
+                call()
+    need = B.bsr_layer_norm_grad_workspace_bytes(40, 24)
+    B.bsr_layer_norm_grad(x, None, stats, x, ws=torch.empty(need, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(B.BsrError) as e:
+        B.bsr_layer_norm_grad(x, None, stats, x, ws=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == B.BSR_ERR_WORKSPACE
+    odd = torch.zeros(24, 45, device="cuda", dtype=torch.bfloat16)[:, 1:43]
+    need = B.bsr_gated_ff_workspace_bytes(x.bfloat16(), odd)
+    assert need >= 24 * 42 * 2
+    B.bsr_gated_ff(x.bfloat16(), odd, ws=torch.empty(need, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(B.BsrError) as e:
+        B.bsr_gated_ff(x.bfloat16(), odd, ws=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == B.BSR_ERR_WORKSPACE
+
+
+def test_optimizer_refusals():
+    a, b = torch.zeros(300, device="cuda"), torch.zeros(300, device="cuda")
+    g = torch.zeros(300, device="cuda")
+    for params, grads in (([a, a], [g, g]), ([a[:200], a[100:]], [g[:200], g[100:]]), ([a], [a])):
+        with pytest.raises(ValueError, match="overlap"):
+            B.AdamWBatch(params, grads)
+    with pytest.raises(ValueError, match="overlap"):
+        B.AdamWBatch([a], [g], states=[(b, b)])
+    B.AdamWBatch([a[:200], a[200:]], [g[:200], g[:100]])                           # (gradients may be shared: they are read)
+    with pytest.raises(ValueError, match="contiguous"):
+        B.AdamWBatch([a[::2]], [g[:150]])
+    with pytest.raises(ValueError, match="as large"):
+        B.AdamWBatch([a], [g[:299]])
+    codes = [torch.zeros(300, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    for scales in (torch.zeros(2, 2, dtype=torch.uint8, device="cuda"), torch.zeros(3, 2, dtype=torch.uint8, device="cuda").t(),
+                   torch.zeros(2, 3, device="cuda"), torch.zeros(1, 3, dtype=torch.uint8, device="cuda").expand(2, 3), torch.zeros(2, 3, dtype=torch.uint8)):
+        with pytest.raises(ValueError, match="scales"):
+            B.AdamWBatch([a], [g], bits=8, states=[(*codes, scales)])
+    with pytest.raises(ValueError, match="copies|contiguous"):
+        B.AdamWBatch([a], [g], copies=[b])
+    batch = B.AdamWBatch([a], [g])
+    for bad in (dict(lr=float("nan"), step=1), dict(lr=0.1, step=0), dict(lr=0.1, step=1, beta2=1.0), dict(lr=0.1, step=1, eps=0.0)):
+        with pytest.raises(B.BsrError) as e:
+            B.bsr_adamw_batched(batch, **bad)
+        assert e.value.code == B.BSR_ERR_VALUE
+    with pytest.raises(ValueError, match="lr on the device"):
+        B.bsr_adamw_batched(batch, lr=torch.zeros(2, device="cuda"), step=1)
+    with pytest.raises(ValueError, match="step on the device"):
+        B.bsr_adamw_batched(batch, lr=0.1, step=torch.ones(1, device="cuda"))
+    with pytest.raises(ValueError, match="device"):
+        B.bsr_adamw_batched(batch, lr=torch.tensor(0.1), step=1)
+    with pytest.raises(TypeError):
+        B.bsr_adamw_batched(batch, lr=0.1, step=1.5)
+    with pytest.raises((OverflowError, TypeError)):
+        B.bsr_adamw_batched(batch, lr=0.1, step=1, seed=-1)
+    assert torch.equal(a, torch.zeros(300, device="cuda"))
+    with pytest.raises(ValueError):
+        B.bsr_adamw_state_values(codes[0], torch.zeros(2, dtype=torch.uint8, device="cuda"), "m")
+    with pytest.raises(ValueError):
+        B.bsr_adamw_state_values(codes[0].float(), torch.zeros(3, dtype=torch.uint8, device="cuda"), "m")
