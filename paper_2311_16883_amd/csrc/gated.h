@@ -68,6 +68,7 @@ constexpr TileSize kTiles[] = {{256, 256, 128}, {128, 256, 64}, {128, 128, 128},
 struct Plan {
   Tile tile;
   int32_t tiles_n, splits, stages_per_split;
+  double us;                       // estimated
 };
 
 // Floats between the rows of a part of a split contraction.

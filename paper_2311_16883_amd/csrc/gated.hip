@@ -252,7 +252,7 @@ double estimate_us(Tile t, int64_t M, int64_t N, int64_t K, int dtype, bool gate
 }
 
 Plan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool gated) {
-  Plan p = {kTile32, 0, 1, 0};
+  Plan p = {kTile32, 0, 1, 0, 0.0};
   double best = 0.0;
   int64_t splits = 1;
   for (int t = kTile256; t <= kTile32; ++t) {
@@ -268,6 +268,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool gated) {
       }
     }
   }
+  p.us = best;
   const TileSize &s = kTiles[p.tile];
   const int64_t stages = std::max<int64_t>(1, ceil_div(K, (int64_t)(s.row_bytes / elem_bytes(dtype))));
   p.tiles_n = (int32_t)ceil_div(N, (int64_t)(gated ? s.cols / 2 : s.cols));
@@ -308,13 +309,27 @@ Layout forward_layout(const GatedArgs &g) {
   return l;
 }
 
+// Elements between packed rows of `n`: whole lines.
+int64_t lines(int64_t n, int dtype) {
+  const int64_t le = 128 / elem_bytes(dtype);
+  return ceil_div(n, le) * le;
+}
+
 Layout backward_layout(const GatedArgs &g, const void *dGU, int64_t lddgu) {
   Layout l;
   l.plan = plan_product(g.M, g.D, 2 * g.F, g.dtype, false);
   const size_t e = (size_t)elem_bytes(g.dtype);
-  const int64_t pitch = padded(2 * g.F, g.dtype);
-  if (g.F > 0 && !in_place(dGU, g.dtype, lddgu, 2 * g.F)) l.a = align_up((size_t)g.M * (size_t)pitch * e, 256);
-  if (g.F > 0 && !in_place(g.W, g.dtype, g.ldw, 2 * g.F)) l.b = align_up((size_t)g.D * (size_t)pitch * e, 256);
+  const int64_t pitch = lines(2 * g.F, g.dtype);
+  const size_t a = align_up((size_t)g.M * (size_t)pitch * e, 256), b = align_up((size_t)g.D * (size_t)pitch * e, 256);
+  // Both operands' rows lie along the contraction and are read a line at a time.  Rows that are no whole lines make that two lines, which costs
+  // about a fifth of the product for each operand (4096 x 2048 x [2 x 4096]: 134 us, 159 with such a dGU, 179 with such a W too): there a
+  // copy in whole lines pays, written beside dGU, or read and written beside the slopes.  (Not in small products, which wait for other
+  // things: 1000 x 1000 x [2 x 1000] 20 us, copied 23.)
+  auto crooked = [&](const void *p, int64_t ld) { return g.dtype == BSR_BF16 && ((uintptr_t)p % 128 != 0 || ld * (int64_t)e % 128 != 0); };
+  auto pays = [&](double bytes) { return 0.2 * (l.plan.us - 12.0) > bytes / 5e6; };
+  if (g.F == 0) return l;                            // (zeros: nothing is read or added up)
+  if (!in_place(dGU, g.dtype, lddgu, 2 * g.F) || (crooked(dGU, lddgu) && pays((double)a))) l.a = a;
+  if (!in_place(g.W, g.dtype, g.ldw, 2 * g.F) || (crooked(g.W, g.ldw) && pays(2.0 * (double)b))) l.b = b;
   l.partial = partial_bytes(l.plan, g.M, g.D, false);
   l.all = l.a + l.b + l.partial;
   return l;
@@ -397,7 +412,7 @@ int backward(const GatedArgs &g, const void *GU, int64_t ldgu, const void *dH, i
   const bool product = dX != nullptr && g.D > 0;
   const Layout l = product ? backward_layout(g, dGU, lddgu) : Layout();
   uint8_t *const at = static_cast<uint8_t *>(ws);
-  const int64_t pitch = padded(2 * g.F, g.dtype);
+  const int64_t pitch = lines(2 * g.F, g.dtype);
   T *const also = l.a != 0 ? reinterpret_cast<T *>(at) : nullptr;
   PackJob job = {};
   int32_t packers = 0;
@@ -421,7 +436,7 @@ int backward(const GatedArgs &g, const void *GU, int64_t ldgu, const void *dH, i
   a.ldb = l.b != 0 ? pitch : g.ldw;
   a.M = g.M;
   a.N = g.D;
-  a.K = 2 * g.F;
+  a.K = l.a != 0 && l.b != 0 ? padded(2 * g.F, g.dtype) : 2 * g.F;      // (both are zeros behind their last column)
   a.out = dX;
   a.ldo = lddx;
   a.partial = reinterpret_cast<float *>(at + l.a + l.b);
