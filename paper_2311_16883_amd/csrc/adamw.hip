@@ -12,6 +12,7 @@
 // beside it may be larger than its smallest code and would be divided by eps.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "layer_ops.h"
 
@@ -24,6 +25,9 @@ constexpr int kThreads = 256;
 // moments: four a lane 134 us, eight 116; moments in binary32: 212 and 219.)
 constexpr int per_lane(size_t param_bytes, bool small) { return param_bytes == 2 && small ? 8 : 4; }
 constexpr int64_t kManyElements = int64_t(4) << 20;    // from here on a workgroup takes four rounds, below one
+// From here on everything is read and written past the caches, which hold none of it until the next step: 49 million elements with binary32 moments
+// 291 -> 271 us (5.4 TB/s), 180 million with 8-bit moments 592 -> 548; stores alone 290 and 580, loads alone 289 and 600; 4.8 million 28.8 -> 30.0.
+constexpr int64_t kStreamElements = int64_t(16) << 20;
 constexpr int kItems = 40;                             // tensors per launch: their list is 3.5 KB of arguments
 
 struct Item {
@@ -71,17 +75,15 @@ __host__ __device__ inline void step_numbers(Options &o, int64_t step) {
 }
 
 // N consecutive numbers, of which `left` are there (the others: 0), at any alignment.
-template <int BYTES>
-struct __attribute__((packed, aligned(1))) AnyBytes {
-  typename RawWords<BYTES>::type w;
-};
-template <int N, typename T>
+template <int N, bool STREAM, typename T>
 __device__ __forceinline__ void load_some(const T *p, int left, T *out) {
   constexpr int kBytes = N * sizeof(T), kEach = kBytes < 16 ? kBytes : 16;
   if (left >= N) {
 #pragma unroll
     for (int b = 0; b < kBytes; b += kEach) {
-      const auto w = reinterpret_cast<const AnyBytes<kEach> *>(reinterpret_cast<const char *>(p) + b)->w;
+      typedef typename RawWords<kEach>::type Loose __attribute__((aligned(1)));
+      const auto *at = reinterpret_cast<const Loose *>(reinterpret_cast<const char *>(p) + b);
+      const typename RawWords<kEach>::type w = STREAM ? __builtin_nontemporal_load(at) : *at;
       __builtin_memcpy(reinterpret_cast<char *>(out) + b, &w, kEach);
     }
   } else {
@@ -89,7 +91,7 @@ __device__ __forceinline__ void load_some(const T *p, int left, T *out) {
     for (int q = 0; q < N; ++q) out[q] = q < left ? p[q] : (T)0;
   }
 }
-template <int N, typename T>
+template <int N, bool STREAM, typename T>
 __device__ __forceinline__ void store_some(T *p, int left, const T *v) {
   constexpr int kBytes = N * sizeof(T), kEach = kBytes < 16 ? kBytes : 16;
   if (left >= N) {
@@ -97,7 +99,10 @@ __device__ __forceinline__ void store_some(T *p, int left, const T *v) {
     for (int b = 0; b < kBytes; b += kEach) {
       typename RawWords<kEach>::type w;
       __builtin_memcpy(&w, reinterpret_cast<const char *>(v) + b, kEach);
-      reinterpret_cast<AnyBytes<kEach> *>(reinterpret_cast<char *>(p) + b)->w = w;
+      typedef typename RawWords<kEach>::type Loose __attribute__((aligned(1)));
+      auto *at = reinterpret_cast<Loose *>(reinterpret_cast<char *>(p) + b);
+      if (STREAM) __builtin_nontemporal_store(w, at);
+      else *at = w;
     }
   } else {
 #pragma unroll
@@ -130,7 +135,7 @@ __device__ __forceinline__ uint32_t encode(float a, uint32_t scale, uint32_t u) 
   return scale == 0u || scale == 255u ? 0u : BITS == 4 ? max(code, min(__float_as_uint(a), 1u)) : code;
 }
 
-template <typename P, typename G, bool SMALL, bool COPY>
+template <typename P, typename G, bool SMALL, bool COPY, bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int rounds) {
   constexpr int PL = per_lane(sizeof(P), SMALL), kGroup = PL == 8 ? 4 : 5;      // lanes of a block: 2^kGroup
   // this workgroup's tensor
@@ -156,13 +161,13 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
     P p0[PL];
     G g0[PL];
     float m[PL], root[PL], p[PL];
-    load_some<PL>(param + i, left, p0);
-    load_some<PL>(grad + i, left, g0);
+    load_some<PL, STREAM>(param + i, left, p0);
+    load_some<PL, STREAM>(grad + i, left, g0);
     const int64_t block = i / kMomentBlock;
     if constexpr (SMALL) {
       uint8_t cm[PL], cv[PL];
-      load_some<PL>(static_cast<const uint8_t *>(it.m) + i, left, cm);
-      load_some<PL>(static_cast<const uint8_t *>(it.v) + i, left, cv);
+      load_some<PL, STREAM>(static_cast<const uint8_t *>(it.m) + i, left, cm);
+      load_some<PL, STREAM>(static_cast<const uint8_t *>(it.v) + i, left, cv);
       const uint32_t sm = left > 0 ? it.scale_m[block] : 0u, sv = left > 0 ? it.scale_v[block] : 0u;
 #pragma unroll
       for (int q = 0; q < PL; ++q) {
@@ -170,8 +175,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
         root[q] = decode<4>(cv[q], sv);
       }
     } else {
-      load_some<PL>(static_cast<const float *>(it.m) + i, left, m);
-      load_some<PL>(static_cast<const float *>(it.v) + i, left, root);
+      load_some<PL, STREAM>(static_cast<const float *>(it.m) + i, left, m);
+      load_some<PL, STREAM>(static_cast<const float *>(it.v) + i, left, root);
     }
 #pragma unroll
     for (int q = 0; q < PL; ++q) {
@@ -185,12 +190,12 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
     }
 #pragma unroll
     for (int q = 0; q < PL; ++q) p0[q] = from_float<P>(p[q]);
-    store_some<PL>(param + i, left, p0);
+    store_some<PL, STREAM>(param + i, left, p0);
     if constexpr (COPY) {
       uint16_t c[PL];
 #pragma unroll
       for (int q = 0; q < PL; ++q) c[q] = from_float<uint16_t>(p[q]);
-      store_some<PL>(it.copy + i, left, c);
+      store_some<PL, STREAM>(it.copy + i, left, c);
     }
     if constexpr (SMALL) {
       uint32_t most_m = 0u, most_v = 0u;
@@ -211,36 +216,32 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
         cm[q] = (uint8_t)(c | (c != 0u && m[q] < 0.0f ? 128u : 0u));
         cv[q] = (uint8_t)encode<4>(root[q], sv, h >> 16);
       }
-      store_some<PL>(static_cast<uint8_t *>(it.m) + i, left, cm);
-      store_some<PL>(static_cast<uint8_t *>(it.v) + i, left, cv);
+      store_some<PL, STREAM>(static_cast<uint8_t *>(it.m) + i, left, cm);
+      store_some<PL, STREAM>(static_cast<uint8_t *>(it.v) + i, left, cv);
       if (threadIdx.x % (kMomentBlock / PL) == 0 && left > 0) {
         it.scale_m[block] = (uint8_t)sm;
         it.scale_v[block] = (uint8_t)sv;
       }
     } else {
-      store_some<PL>(static_cast<float *>(it.m) + i, left, m);
-      store_some<PL>(static_cast<float *>(it.v) + i, left, root);
+      store_some<PL, STREAM>(static_cast<float *>(it.m) + i, left, m);
+      store_some<PL, STREAM>(static_cast<float *>(it.v) + i, left, root);
     }
   }
 }
 
 // Sixteen codes to a lane.
-template <typename T, int BITS>
+template <typename T, int BITS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void state_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                 int64_t n, T *__restrict__ out) {
   for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 16; i < n; i += (int64_t)gridDim.x * kThreads * 16) {
     const uint32_t scale = scales[i / kMomentBlock];
     if (n - i >= 16) {
-      struct __attribute__((packed, aligned(1))) Codes { Words4 w; };
-      struct __attribute__((packed, aligned(2))) Out { Words4 w; };
-      const Words4 c = reinterpret_cast<const Codes *>(codes + i)->w;
+      uint8_t c[16];
+      load_some<16, STREAM>(codes + i, 16, c);
+      T v[16];
 #pragma unroll
-      for (int v = 0; v < 16; v += 16 / (int)sizeof(T)) {
-        float f[16 / sizeof(T)];
-#pragma unroll
-        for (int q = 0; q < 16 / (int)sizeof(T); ++q) f[q] = decode<BITS>(c[(v + q) / 4] >> (8 * ((v + q) % 4)) & 255u, scale);
-        reinterpret_cast<Out *>(out + i + v)->w = pack_row<T, 16 / (int)sizeof(T)>(f);
-      }
+      for (int q = 0; q < 16; ++q) v[q] = from_float<T>(decode<BITS>(c[q], scale));
+      store_some<16, STREAM>(out + i, 16, v);
     } else {
       for (int64_t j = i; j < n; ++j) out[j] = from_float<T>(decode<BITS>(codes[j], scale));
     }
@@ -248,8 +249,9 @@ __global__ __launch_bounds__(kThreads) void state_values_kernel(const uint8_t *_
 }
 
 template <typename P, typename G, bool SMALL, bool COPY>
-void launch_list(const List &list, int n, uint32_t chunks, int rounds, hipStream_t s) {
-  adamw_kernel<P, G, SMALL, COPY><<<dim3(chunks), kThreads, 0, s>>>(list, n, rounds);
+void launch_list(const List &list, int n, uint32_t chunks, int rounds, bool stream, hipStream_t s) {
+  if (stream) adamw_kernel<P, G, SMALL, COPY, true><<<dim3(chunks), kThreads, 0, s>>>(list, n, rounds);
+  else adamw_kernel<P, G, SMALL, COPY, false><<<dim3(chunks), kThreads, 0, s>>>(list, n, rounds);
 }
 
 }  // namespace
@@ -280,6 +282,7 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
   int64_t all = 0;
   for (int i = 0; i < n; ++i) all += items[i].n;
   const int rounds = all >= kManyElements ? 4 : 1;
+  const bool stream = all >= kStreamElements;
   const int64_t chunk = (int64_t)kThreads * rounds * per_lane((size_t)elem_bytes(param_dtype), small);
   auto flush = [&]() {
     if (held == 0) return (int)BSR_OK;
@@ -287,8 +290,8 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
     auto go = [&](auto p, auto g) {
       typedef decltype(p) P;
       typedef decltype(g) G;
-      if (small) copies ? launch_list<P, G, true, true>(list, held, chunks, rounds, s) : launch_list<P, G, true, false>(list, held, chunks, rounds, s);
-      else copies ? launch_list<P, G, false, true>(list, held, chunks, rounds, s) : launch_list<P, G, false, false>(list, held, chunks, rounds, s);
+      if (small) copies ? launch_list<P, G, true, true>(list, held, chunks, rounds, stream, s) : launch_list<P, G, true, false>(list, held, chunks, rounds, stream, s);
+      else copies ? launch_list<P, G, false, true>(list, held, chunks, rounds, stream, s) : launch_list<P, G, false, false>(list, held, chunks, rounds, stream, s);
     };
     if (param_dtype == BSR_F32) grad_dtype == BSR_F32 ? go(float(), float()) : go(float(), uint16_t());
     else grad_dtype == BSR_F32 ? go(uint16_t(), float()) : go(uint16_t(), uint16_t());
@@ -330,13 +333,15 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
 
 int launch_adamw_state_values(const uint8_t *codes, const uint8_t *scales, int64_t n, int which, void *out, int dtype, hipStream_t s) {
   const dim3 grid((uint32_t)std::min(ceil_div(n, (int64_t)kThreads * 16), int64_t(1) << 23));
-  if (dtype == BSR_F32) {
-    if (which == 0) state_values_kernel<float, 3><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<float *>(out));
-    else state_values_kernel<float, 4><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<float *>(out));
-  } else {
-    if (which == 0) state_values_kernel<uint16_t, 3><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<uint16_t *>(out));
-    else state_values_kernel<uint16_t, 4><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<uint16_t *>(out));
-  }
+  auto go = [&](auto type, auto bits) {
+    typedef decltype(type) T;
+    if (n >= kStreamElements) state_values_kernel<T, decltype(bits)::value, true><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<T *>(out));
+    else state_values_kernel<T, decltype(bits)::value, false><<<grid, kThreads, 0, s>>>(codes, scales, n, static_cast<T *>(out));
+  };
+  typedef std::integral_constant<int, 3> M;
+  typedef std::integral_constant<int, 4> R;
+  if (dtype == BSR_F32) which == 0 ? go(float(), M()) : go(float(), R());
+  else which == 0 ? go(uint16_t(), M()) : go(uint16_t(), R());
   return check_launch();
 }
 
