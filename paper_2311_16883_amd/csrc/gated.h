@@ -60,11 +60,11 @@ struct ProductArgs {
 };
 
 // How a product is computed: the tile of a workgroup, and how many workgroups share the contraction of a tile.
-enum Tile { kTile256, kTileWide, kTile128, kTile128Alone, kTile64, kTile32 };
+enum Tile { kTile256, kTileWide, kTile128, kTile128Alone, kTile96Alone, kTile64, kTile32 };
 struct TileSize {
   int rows, cols, row_bytes;
 };
-constexpr TileSize kTiles[] = {{256, 256, 128}, {128, 256, 64}, {128, 128, 128}, {128, 128, 128}, {64, 128, 128}, {32, 256, 64}};
+constexpr TileSize kTiles[] = {{256, 256, 128}, {128, 256, 64}, {128, 128, 128}, {128, 128, 128}, {96, 128, 128}, {64, 128, 128}, {32, 256, 64}};
 struct Plan {
   Tile tile;
   int32_t tiles_n, splits, stages_per_split;

@@ -233,16 +233,16 @@ bool in_place(const void *p, int dtype, int64_t ld, int64_t inner) {
 // TFLOP/s in 128 x 256, 121 in 128 x 128, 95 in 256 x 256), and rows of 64 bytes of both operands are half of every line.
 bool has_tile(Tile t, int dtype, bool gated) {
   if (dtype == BSR_F32) return t == kTile128 || t == kTile64 || t == kTile32;
-  return t != kTileWide || gated;
+  return t == kTileWide ? gated : t == kTile96Alone ? !gated : true;
 }
 
 // Estimated microseconds, from what the kernels were measured to do: TFLOP/s of a compute unit with one workgroup in it and with two
 // (bfloat16: 8192 x 2048 x [2 x 5504] in 256 x 256 tiles 326 us, in 128 x 256 349, in 128 x 128 390; 2048 rows 97, 85, 93; 512 rows 42, 27, 29;
-// 2999 x 3080 x 808 in 128 x 128 tiles alone in their unit 33, otherwise 45).  A tile's beginning and end cost as much as some more
+// 2999 x 3080 x 808 in 96 x 128 tiles, 224 of them, 24, in 128 x 128, 168 of them, alone in their unit 26, otherwise 45).  A tile's beginning and end cost as much as some more
 // of the contraction.  (Whether GU is written has no part in it: H would have other bits with GU than without.)
 double estimate_us(Tile t, int64_t M, int64_t N, int64_t K, int dtype, bool gated, int64_t splits) {
-  const double rates[2][6][2] = {{{4.9, 4.9}, {4.6, 4.4}, {2.4, 3.6}, {3.4, 3.4}, {2.9, 2.8}, {1.0, 1.8}},
-                                 {{0, 0}, {0, 0}, {0.46, 0.53}, {0, 0}, {0.45, 0.47}, {0.3, 0.45}}};
+  const double rates[2][7][2] = {{{4.9, 4.9}, {4.6, 4.4}, {2.4, 3.6}, {3.4, 3.4}, {3.0, 3.0}, {2.9, 2.8}, {1.0, 1.8}},
+                                 {{0, 0}, {0, 0}, {0.46, 0.53}, {0, 0}, {0, 0}, {0.45, 0.47}, {0.3, 0.45}}};
   const TileSize &s = kTiles[t];
   const bool f32 = dtype == BSR_F32;
   const int64_t tiles = ceil_div(M, (int64_t)s.rows) * ceil_div(N, (int64_t)(gated ? s.cols / 2 : s.cols)) * splits;
@@ -262,7 +262,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool gated) {
     if ((t == kTile32) != (M <= 32) || !has_tile((Tile)t, dtype, gated)) continue;
     const TileSize &s = kTiles[t];
     const int64_t stages = std::max<int64_t>(1, ceil_div(K, (int64_t)(s.row_bytes / elem_bytes(dtype))));
-    for (int64_t n = 1; n <= (t == kTile256 ? 1 : 16) && n * 4 <= std::max<int64_t>(stages, 4); n = t == kTile32 ? n + 1 : 2 * n) {
+    for (int64_t n = 1; n <= (t == kTile256 || t == kTile96Alone ? 1 : 16) && n * 4 <= std::max<int64_t>(stages, 4); n = t == kTile32 ? n + 1 : 2 * n) {
       const double us = estimate_us((Tile)t, M, N, K, dtype, gated, n);
       if (best == 0.0 || us < best) {
         best = us;

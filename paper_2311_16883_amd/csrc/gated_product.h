@@ -1,16 +1,27 @@
 // The matrix products of the gated feed-forward block, for the translation units of their element types.
-//
-// Tiles of the product are computed by workgroups of 4 or 8 waves, a wave 32 .. 128 rows x 64 columns; the forward pass gives a wave 32 columns of
-// the gate and the same 32 of the other projection, so that activation and product happen in its registers.  Operands go from global
-// memory into LDS by the texture path (buffer_load ... lds, 16 bytes a lane), in stages of 64 bytes of the contraction (32 bfloat16, 16
-// binary32), through a ring of four stages: three are on their way while one is multiplied.  A stage is multiplied in two halves, the
-// fragments of one requested while the other is multiplied, across the barrier between stages too; there is one barrier a stage.
-// LDS rows of X are 64 bytes, their 16-byte chunks permuted by the row (chosen by the lane that fetches them) so that the reads of a
-// fragment touch every bank once; W's are 128 bytes of 64 columns, read by transposing loads.
-// The matrix instructions take W's fragment first: a lane then holds four consecutive columns of one row of the result, and
-// two exchanges between the halves of a wave make 16-byte stores of them.
-//
 #pragma once
+
+// [G | U] = X W with act(G) * U made from it, or dX = dGU W^T.  Tiles of the result are computed by workgroups of 4 or 8 waves, a wave
+// 32 .. 128 rows x 64 columns; the forward pass gives a wave 32 columns of the gate and the same 32 of the other projection, so that
+// activation and product happen in its registers.
+//
+// Operands go from global memory into LDS by the texture path (buffer_load ... lds, 16 bytes a lane), in stages of 64 or 128 bytes of the
+// contraction, through a ring of two to four stages: what is not being multiplied is on its way.  128 bytes are whole lines of operands
+// that lie along the contraction: in stages of 64 each line would pass from the second cache to the first twice.  A stage is multiplied in
+// phases of 32 bytes, whose fragments are requested while the phase before is multiplied, across the barrier between stages too; there is
+// one barrier a stage.
+// LDS rows along the contraction are 64 or 128 bytes, their 16-byte chunks permuted by the row (chosen by the lane that fetches them) so
+// that the reads of a fragment touch every bank once; W's in the forward pass are 128 bytes of columns, read by transposing loads.
+// The matrix instructions take B's fragment first: a lane then holds four consecutive columns of one row of the result, and
+// exchanges between the halves of a wave make 16-byte stores of them.
+//
+// Bound by the matrix cores: 8192 x 2048 x [2 x 5504] bfloat16, 369 GFLOP, takes 366 us with GU written (1.01 PFLOP/s), about what a library's
+// product of this size takes that stores [G | U] and nothing else (379 us, 354 with W transposed).  What is lost: the first stages of a tile and its
+// results, in which the matrix cores wait (one workgroup of 256 x 256 fills a compute unit, so nothing runs beside them), and the last
+// round of tiles, which is not full.  Binary32 reaches 121 TFLOP/s of the 154 that a library does.
+// Measured and not kept (this size): 256 x 256 and 128 x 256 tiles in one launch, the last round in the smaller ones: 360 us, but 2048 rows 96 for 93 and
+// 25088 x 384 x [2 x 1024] 72 for 66; wave tiles of 128 x 128 and of 64 x 128; results stored past the caches 495; results in whole
+// 64-byte rows by more exchanges 375.
 
 #include "gated.h"
 
@@ -23,7 +34,6 @@ typedef __attribute__((ext_vector_type(8))) short v8s;
 typedef __attribute__((ext_vector_type(8))) __bf16 v8bf;
 typedef __attribute__((ext_vector_type(4))) float v4f;
 typedef __attribute__((ext_vector_type(16))) float v16f;
-
 
 // One global -> LDS copy: lane l's BYTES land at lds_addr + BYTES * l.  Inline assembly, so that the compiler keeps no account of
 // it (it would wait for all copies in front of the next LDS read); the waits are explicit.
@@ -93,7 +103,7 @@ __device__ __forceinline__ void store_tile(T *out, int64_t ld, int64_t m, int64_
 // A wave's tile is TM x TN fragments of 32 x 32; WM x WN waves; RING stages of ROW bytes of the contraction in LDS.  WHOLE: the contraction
 // and the rows of B end with whole vectors (what it takes where they do not costs the others 2 to 10 %).
 template <typename T, bool GATED, int TM, int TN, int WM, int WN, int RING, int ROW, bool WHOLE, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN, (TM * TN > 8 ? 1 : 2)) void product_kernel(ProductArgs a) {
+__global__ __launch_bounds__(64 * WM * WN, (WM * WN == 4 && RING * 32 * (TM * WM + TN * WN) * ROW > 80 * 1024 ? 1 : 2)) void product_kernel(ProductArgs a) {
   constexpr int kWaves = WM * WN;
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN;            // BN: columns of B in a tile; of a gated tile half belong to G
   constexpr int kStageBytes = (BM + BN) * ROW;
@@ -252,7 +262,7 @@ __global__ __launch_bounds__(64 * WM * WN, (TM * TN > 8 ? 1 : 2)) void product_k
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-  // Multiplies the fragments of half a stage and does `actions` other things between the matrix instructions: a wave issues them
+  // Multiplies the fragments of a phase and does `actions` other things between the matrix instructions: a wave issues them
   // while the matrix core is busy, where all of them together in front would leave it idle (both waves of a SIMD come to that
   // place at the same time).  The order is the program's: the compiler would gather them again.
   auto multiply = [&](const Frags &f, auto actions, auto action) {
@@ -408,6 +418,12 @@ void launch_tile(Tile t, dim3 grid, const ProductArgs &a, hipStream_t s) {
     if constexpr (GATED) {
       if (t == kTileWide) {
         product_kernel<T, GATED, 2, 2, 2, 4, 3, 64, WHOLE, SPLIT><<<grid, 512, 0, s>>>(a);
+        return;
+      }
+    }
+    if constexpr (!GATED && !SPLIT) {
+      if (t == kTile96Alone) {
+        product_kernel<T, GATED, 3, 1, 1, 4, 4, 128, WHOLE, SPLIT><<<grid, 256, 0, s>>>(a);
         return;
       }
     }

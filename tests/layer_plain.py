@@ -131,8 +131,8 @@ def gated(x, w, name, dtype):
     """-> h, bound, gu, bound"""
     D, F = w.shape[0], w.shape[1] // 2
     gu, size = x @ w, np.abs(x) @ np.abs(w)
-    # bfloat16 products are exact and go through D additions; binary32 ones are six products of parts, and 2 U of left out ones
-    e = (D + 1) * U * size if dtype == "bf16" else (6 * D + 4) * U * size
+    # products (exact in binary32 where they are bfloat16's) and D additions
+    e = (D + 1) * U * size
     g, u, eg, eu = gu[:, :F], gu[:, F:], e[:, :F], e[:, F:]
     a, _, ea, _ = act(g, name)
     ea = ea + 1.13 * eg + 16 * U * eg                                            # |act'| <= 1.13

@@ -139,11 +139,11 @@ def test_gated_ff_grad(dtype, M, D, F):
         check(dGU, want, bound, dtype, "dGU")
         d = f64(dGU)
         size = np.abs(d) @ np.abs(f64(w)).T
-        check(dX, d @ f64(w).T, ((2 * F + 1) if dtype == "bf16" else (12 * F + 4)) * P.U * size, dtype, "dX")
+        check(dX, d @ f64(w).T, (2 * F + 1) * P.U * size, dtype, "dX")
         same = src.clone()
         dX2, dGU2 = B.bsr_gated_ff_grad(same, grad, wide, act=name, dGU=same)
         assert dGU2 is same and torch.equal(dGU2, dGU)
-        check(dX2, f64(dX), 2 * ((2 * F + 1) if dtype == "bf16" else (12 * F + 4)) * P.U * size, dtype, "dX in place")
+        check(dX2, f64(dX), 2 * (2 * F + 1) * P.U * size, dtype, "dX in place")
         assert torch.equal(B.bsr_gated_ff_grad(src, grad, None, act=name, want_dX=False), dGU)
 
 
@@ -161,7 +161,31 @@ def test_gated_many_tiles(dtype):
     dX, dGU = B.bsr_gated_ff_grad(gu.cuda(), dh.cuda(), w.cuda(), act="silu")
     d = f64(dGU)
     size = np.abs(d) @ np.abs(f64(w)).T
-    check(dX, d @ f64(w).T, ((2 * F + 1) if dtype == "bf16" else (12 * F + 4)) * P.U * size, dtype, "dX")
+    check(dX, d @ f64(w).T, (2 * F + 1) * P.U * size, dtype, "dX")
+
+
+# Sizes that the larger tiles take, each with its contraction whole and split where that occurs, and with whole vectors or not.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,D,F", [(1706, 32, 2490), (1706, 32, 2496), (1264, 32, 1638), (80, 10447, 1034), (80, 10448, 1040), (1659, 51, 2464),
+                                   (4643, 7294, 8), (4643, 7296, 8), (525, 32, 1865), (4148, 1978, 8), (4148, 1984, 16)])
+def test_gated_ff_in_every_tile(dtype, M, D, F):
+    x, w = randn(1, M, D, dtype=dtype), randn(2, D, 2 * F, dtype=dtype, scale=D ** -0.5)
+    H, GU = B.bsr_gated_ff(x.cuda(), w.cuda(), act="gelu_tanh", want_GU=True)
+    h, e_h, gu, e_gu = P.gated(f64(x), f64(w), "gelu_tanh", dtype)
+    check(GU, gu, e_gu, dtype, "GU")
+    check(H, h, e_h, dtype, "H")
+    assert torch.equal(B.bsr_gated_ff(x.cuda(), w.cuda(), act="gelu_tanh"), H)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,D,F", [(129, 49943, 9), (129, 49944, 16), (1883, 3205, 33), (1883, 3205, 36), (4412, 32, 5253), (4412, 32, 5256), (986, 2962, 33),
+                                   (2132, 32, 2589), (2132, 32, 2592), (515, 3672, 34), (515, 3672, 36), (1003, 2700, 70)])
+def test_gated_ff_grad_in_every_tile(dtype, M, D, F):
+    gu, dh, w = randn(1, M, 2 * F, dtype=dtype), randn(2, M, F, dtype=dtype), randn(3, D, 2 * F, dtype=dtype)
+    dX, dGU = B.bsr_gated_ff_grad(gu.cuda(), dh.cuda(), w.cuda(), act="silu")
+    d = f64(dGU)
+    size = np.abs(d) @ np.abs(f64(w)).T
+    check(dX, d @ f64(w).T, (2 * F + 1) * P.U * size, dtype, "dX")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
