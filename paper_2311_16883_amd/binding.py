@@ -765,7 +765,10 @@ class AdamWBatch:
                     states.append((torch.zeros(p.shape, dtype=torch.uint8, device=p.device),
                                    torch.zeros(p.shape, dtype=torch.uint8, device=p.device),
                                    torch.zeros(2, bsr_adamw_blocks(p.numel()), dtype=torch.uint8, device=p.device)))
-        self.params, self.grads, self.states, self.copies = list(params), list(grads), [tuple(s) for s in states], copies
+        def kept(t):                                  # (an alias: the memory stays, also where a tensor is given other data later)
+            return t.detach() if isinstance(t, torch.Tensor) else t
+        self.params, self.grads = [kept(p) for p in params], [kept(g) for g in grads]
+        self.states, self.copies = [tuple(kept(t) for t in s) for s in states], [kept(c) for c in copies]
         self.items = (_AdamWItem * n)()
         places = []                                   # (first byte, end, whether it is written)
 
@@ -778,7 +781,7 @@ class AdamWBatch:
                 places.append((t.data_ptr(), t.data_ptr() + count * t.element_size(), what != "grads"))
             return _ptr(t)
 
-        for i, (p, g, s, c) in enumerate(zip(self.params, self.grads, self.states, copies)):
+        for i, (p, g, s, c) in enumerate(zip(self.params, self.grads, self.states, self.copies)):
             count = p.numel()
             item = self.items[i]
             item.param, item.grad = flat(p, "params", params[0].dtype, count), flat(g, "grads", grads[0].dtype, count)

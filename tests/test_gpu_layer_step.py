@@ -357,3 +357,15 @@ def test_optimizer_refusals():
         B.bsr_adamw_state_values(codes[0], torch.zeros(2, dtype=torch.uint8, device="cuda"), "m")
     with pytest.raises(ValueError):
         B.bsr_adamw_state_values(codes[0].float(), torch.zeros(3, dtype=torch.uint8, device="cuda"), "m")
+
+
+def test_optimizer_keeps_the_memory_it_was_given():
+    """A param whose data is replaced: the batch goes on with what it was made of."""
+    p, g = torch.nn.Parameter(torch.ones(1000, device="cuda")), torch.ones(1000, device="cuda")
+    batch = B.AdamWBatch([p], [g])
+    p.data = torch.zeros(1000, device="cuda")
+    others = [torch.zeros(1000, device="cuda") for _ in range(8)]
+    B.bsr_adamw_batched(batch, lr=0.5, step=1)
+    torch.cuda.synchronize()
+    assert not any(t.any() for t in others) and not p.data.any()
+    assert (batch.params[0] - 0.5).abs().max() < 1e-6
