@@ -13,8 +13,8 @@
  * buffers (workspaces included) the caller's, work enqueued on `stream`, checks on
  * the host before anything is launched, BSR_ERR_* codes, dtype BSR_F32 or BSR_BF16,
  * matrices row-major with a leading dimension in elements, pointers aligned to their
- * element type.  Sums are binary32, in an order that depends on sizes, leading dimensions
- * and addresses modulo 16 bytes alone, so results are reproducible bit for bit; a bfloat16 result is
+ * element type.  Sums are binary32, in an order that depends on types, sizes, leading dimensions
+ * and addresses modulo 128 bytes alone, so results are reproducible bit for bit; a bfloat16 result is
  * rounded once, to nearest even, from a binary32 value.
  * Outputs must not overlap inputs or each other except where it says so.
  */
@@ -75,7 +75,7 @@ enum {
  * X: [M x D]; H: [M x F]; GU: [M x 2F], G and U rounded to dtype, or NULL where no backward
  * pass follows (H is computed from the unrounded sums either way).
  * act: BSR_ACT_* (BSR_ERR_VALUE otherwise).  D == 0: zeros.
- * Workspace: the function below (host, pure; of X and W it only uses the addresses modulo 16
+ * Workspace: the function below (host, pure; of X and W it only uses the addresses modulo 128
  * bytes; 0 for invalid arguments).
  */
 size_t bsr_gated_ff_workspace_bytes(const void *X, int dtype, int64_t M, int64_t D,
@@ -91,6 +91,7 @@ int bsr_gated_ff(const void *X, int dtype, int64_t M, int64_t D, int64_t ldx,
  *                   rounded dGU where dtype is BSR_BF16 (the matrix cores' operands).
  * dGU [M x 2F] may be GU itself (with lddgu == ldgu).  dX [M x D] may be NULL: dGU alone (W is not
  * read then).  The gradient of W is X^T dGU: bsr_t_dense_matmul of the pruned X.
+ * Workspace: the function below (as above, of dGU and W).
  */
 size_t bsr_gated_ff_grad_workspace_bytes(const void *dGU, int dtype, int64_t M, int64_t F,
                                          int64_t lddgu, const void *W, int64_t D,
@@ -105,8 +106,9 @@ int bsr_gated_ff_grad(const void *GU, int dtype, int64_t M, int64_t F, int64_t l
  *   g = grad_scale * grad;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
  *   param = param * (1 - lr * weight_decay)
  *           - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps).
- * All of it is computed in binary32 (the powers of beta in binary64) from the values before the step and rounded
- * where it is stored; the update takes m and v before they are rounded.
+ * All of it is computed in binary32 (the powers of beta, and moments that are held in 8 bits, in binary64, whose v
+ * and roots have binary32's range) from the values before the step and rounded where it is stored; the update takes
+ * m and v before they are rounded to 8 bits.
  * Moments in binary32: m [n], v [n].  In 8 bits (BSR_MOMENTS_8BIT): m [n] and v [n] are bytes,
  * and scales holds two rows of bsr_adamw_blocks(n) bytes, those of m and those of v, `scales_stride` bytes apart.  128
  * consecutive elements share a scale byte b:

@@ -1,6 +1,8 @@
 // One AdamW step over many tensors, moments in binary32 or in 8 bits.
 //
-// Bound by memory: 28 bytes per element with binary32 weights, gradients and moments, 16 with 8-bit moments.  The tensors of a call
+// Bound by memory: 28 bytes per element with binary32 weights, gradients and moments, 16 with 8-bit moments.  49 million elements of the
+// first kind and bfloat16 copies of the weights: 271 us, 5.4 TB/s; 180 million of the second, bfloat16 gradients and copies: 572 us, 5.0 TB/s.
+// (A large copy: 5.1.)  The tensors of a call
 // are cut into chunks of whole blocks, a chunk to a workgroup; the list of tensors travels in the kernel's arguments, so
 // there is nothing to copy or to keep for the device.  A lane holds four consecutive elements of a block, 32 lanes a block, whose largest magnitudes
 // meet by lane exchanges.
@@ -26,7 +28,8 @@ constexpr int kThreads = 256;
 constexpr int per_lane(size_t param_bytes, bool small) { return param_bytes == 2 && small ? 8 : 4; }
 constexpr int64_t kManyElements = int64_t(4) << 20;    // from here on a workgroup takes four rounds, below one
 // From here on everything is read and written past the caches, which hold none of it until the next step: 49 million elements with binary32 moments
-// 291 -> 271 us (5.4 TB/s), 180 million with 8-bit moments 592 -> 548; stores alone 290 and 580, loads alone 289 and 600; 4.8 million 28.8 -> 30.0.
+// 291 -> 271 us (5.4 TB/s), 180 million with 8-bit moments 592 -> 548 (codes from binary32, as then); stores alone 290
+// and 580, loads alone 289 and 600; 4.8 million 28.8 -> 30.0.
 constexpr int64_t kStreamElements = int64_t(16) << 20;
 constexpr int kItems = 40;                             // tensors per launch: their list is 3.5 KB of arguments
 
@@ -43,7 +46,7 @@ struct Options {
   float lr, b1, c1, b2, c2, eps, grad_scale;           // c = 1 - b
   float first_full, root;                              // 1 / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
   uint32_t key;
-  double beta1, beta2;
+  double beta1, beta2, scale64;
   const float *lr_device, *grad_scale_device;
   const int64_t *step_device;
   uint64_t seed;
@@ -127,12 +130,22 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t most) {
   return b < 32u ? 0u : b > 255u ? 255u : b;
 }
 
-// a >= 0 rounded to one of its two neighbours by u in [0, 2^16): the bits below a code's last are added to and cut off.  (The scale
-// leaves room for it: the largest of a block is not above the largest code.)
+// A number >= 0, cut off to the binary32 number with these bits, rounded to one of its two neighbours by u in [0, 2^16): the bits below a
+// code's last are added to and cut off.  (The scale leaves room for it: the largest of a block is not above the largest code.)
 template <int BITS>
-__device__ __forceinline__ uint32_t encode(float a, uint32_t scale, uint32_t u) {
-  const uint32_t code = (__float_as_uint(ldexpf(a, 15 - (int)scale)) + (u << (7 - BITS))) >> (23 - BITS);
-  return scale == 0u || scale == 255u ? 0u : BITS == 4 ? max(code, min(__float_as_uint(a), 1u)) : code;
+__device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t scale, uint32_t u) {
+  const uint32_t code = (__float_as_uint(ldexpf(__uint_as_float(bits), 15 - (int)scale)) + (u << (7 - BITS))) >> (23 - BITS);
+  return scale == 0u || scale == 255u ? 0u : BITS == 4 ? max(code, min(bits, 1u)) : code;
+}
+
+// A moment m, or the root of v, as the bits of the binary32 number that its magnitude is cut off to; `near`, `root`: the number
+// nearest to it.  What a code's border decides hangs on the last bit: of 49 million elements 40 .. 60 have another code where m and v are made in
+// binary32, 0 .. 3 from binary64, whose multiplies and adds are as fast (180 million elements 548 us and 572, with correctly rounded roots 582).
+__device__ __forceinline__ uint32_t cut_off(double m, float near) {
+  return (__float_as_uint(near) & 0x7FFFFFFFu) - (fabs((double)near) > fabs(m) ? 1u : 0u);
+}
+__device__ __forceinline__ uint32_t root_cut_off(double v, float root) {
+  return __float_as_uint(root) - (__builtin_fma((double)root, (double)root, -v) > 0.0 ? 1u : 0u);
 }
 
 template <typename P, typename G, bool SMALL, bool COPY, bool STREAM>
@@ -151,6 +164,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
   if (o.step_device != nullptr) step_numbers(o, *o.step_device);
   if (o.lr_device != nullptr) o.lr = *o.lr_device;
   if (o.grad_scale_device != nullptr) o.grad_scale = *o.grad_scale_device;
+  const double c1 = 1.0 - o.beta1, c2 = 1.0 - o.beta2;
+  const double grad_scale = o.grad_scale_device != nullptr ? (double)o.grad_scale : o.scale64;
   P *const param = static_cast<P *>(it.param);
   const G *const grad = static_cast<const G *>(it.grad);
   const float keep = 1.0f - o.lr * it.decay, rate = o.lr * o.first_full;
@@ -161,6 +176,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
     P p0[PL];
     G g0[PL];
     float m[PL], root[PL], p[PL];
+    uint32_t cut_m[SMALL ? PL : 1], cut_r[SMALL ? PL : 1];
     load_some<PL, STREAM>(param + i, left, p0);
     load_some<PL, STREAM>(grad + i, left, g0);
     const int64_t block = i / kMomentBlock;
@@ -180,13 +196,21 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
     }
 #pragma unroll
     for (int q = 0; q < PL; ++q) {
-      const float g = elem_to_float<G>(g0[q]) * o.grad_scale;
-      // (rounded product by product: what a code's border decides does not hang on which of them are fused)
-      m[q] = __fadd_rn(__fmul_rn(o.b1, m[q]), __fmul_rn(o.c1, g));
-      const float v = __fadd_rn(SMALL ? __fmul_rn(__fmul_rn(o.b2, root[q]), root[q]) : __fmul_rn(o.b2, root[q]), __fmul_rn(__fmul_rn(o.c2, g), g));
-      const float rt = SMALL ? __fsqrt_rn(v) : __builtin_amdgcn_sqrtf(v);
+      float rt;
+      if constexpr (SMALL) {
+        const double g = (double)elem_to_float<G>(g0[q]) * grad_scale, old = root[q];
+        const double m64 = __builtin_fma(o.beta1, (double)m[q], c1 * g), v = __builtin_fma(o.beta2 * old, old, c2 * g * g);
+        m[q] = (float)m64;
+        rt = __builtin_amdgcn_sqrtf((float)v);
+        cut_m[q] = cut_off(m64, m[q]);
+        cut_r[q] = root_cut_off(v, rt);
+      } else {
+        const float g = elem_to_float<G>(g0[q]) * o.grad_scale;
+        m[q] = o.b1 * m[q] + o.c1 * g;
+        root[q] = o.b2 * root[q] + o.c2 * g * g;
+        rt = __builtin_amdgcn_sqrtf(root[q]);
+      }
       p[q] = elem_to_float<P>(p0[q]) * keep - rate * m[q] * __builtin_amdgcn_rcpf(rt * o.root + o.eps);
-      root[q] = SMALL ? rt : v;
     }
 #pragma unroll
     for (int q = 0; q < PL; ++q) p0[q] = from_float<P>(p[q]);
@@ -201,9 +225,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
       uint32_t most_m = 0u, most_v = 0u;
 #pragma unroll
       for (int q = 0; q < PL; ++q) {
-        const bool there = q < left;
-        most_m = max(most_m, there ? __float_as_uint(m[q]) & 0x7FFFFFFFu : 0u);
-        most_v = max(most_v, there ? __float_as_uint(root[q]) & 0x7FFFFFFFu : 0u);
+        most_m = max(most_m, q < left ? cut_m[q] : 0u);
+        most_v = max(most_v, q < left ? cut_r[q] : 0u);
       }
       const uint32_t sm = scale_of<3>(group_max<kGroup>(most_m)), sv = scale_of<4>(group_max<kGroup>(most_v));
       uint8_t cm[PL], cv[PL];
@@ -212,9 +235,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
 #pragma unroll
       for (int q = 0; q < PL; ++q) {
         const uint32_t h = mix(base + (uint32_t)q * 0x9E3779B1u);
-        const uint32_t c = encode<3>(fabsf(m[q]), sm, h & 0xFFFFu);
+        const uint32_t c = encode<3>(cut_m[q], sm, h & 0xFFFFu);
         cm[q] = (uint8_t)(c | (c != 0u && m[q] < 0.0f ? 128u : 0u));
-        cv[q] = (uint8_t)encode<4>(root[q], sv, h >> 16);
+        cv[q] = (uint8_t)encode<4>(cut_r[q], sv, h >> 16);
       }
       store_some<PL, STREAM>(static_cast<uint8_t *>(it.m) + i, left, cm);
       store_some<PL, STREAM>(static_cast<uint8_t *>(it.v) + i, left, cv);
@@ -268,6 +291,7 @@ int launch_adamw(const bsr_adamw_item *items, int n, int param_dtype, int grad_d
   o.grad_scale = (float)opt.grad_scale;
   o.beta1 = opt.beta1;
   o.beta2 = opt.beta2;
+  o.scale64 = opt.grad_scale;
   o.seed = opt.seed;
   o.lr_device = opt.lr_device;
   o.grad_scale_device = opt.grad_scale_device;
