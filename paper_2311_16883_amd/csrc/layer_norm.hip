@@ -1,12 +1,15 @@
 // Layer norm and its gradient.
 //
 // Both are bound by memory: a row is read once into registers, its sums are made there, and the result is written; a row belongs
-// to 8 .. 64 lanes of a wave, longer ones to the 4 or 16 waves of a workgroup, the longest are read again for every pass over them.
+// to 8 .. 64 lanes of a wave, longer ones to the 4 .. 16 waves of a workgroup, the longest are read again for every pass over them.
+// [25088 x 1536] bfloat16: 28 us, 5.5 TB/s; gradient with those of weight and bias: 46 us, 5.0 TB/s ([25088 x 384]: 16.6 us, most of it in the
+// caches, and the second launch).  A large copy reaches 5.1 TB/s on this card.
 // The variance is the sum of squares of the distances from a first mean, less what that mean is off: rows far from 0 lose
 // nothing.  16 bytes a lane at any alignment; the last vector of a row that is no whole number of vectors ends with the row, and the
 // elements that it shares with the one before count there only.
 // The gradients of weight and bias are sums over all rows.  The workgroups of the backward pass walk down the matrix and keep the sums of
 // their rows in registers, column by column; a second launch adds up the workgroups.  No atomics: the order is that of the rows.
+// (Requesting the next row while one is summed took the registers of other waves: 25088 x 384 18 -> 20 us.)
 #include <algorithm>
 #include <type_traits>
 
