@@ -1,6 +1,7 @@
 """One training step of a small token model whose experts save pruned inputs.
 
     python examples/token_step.py [--tokens 2048] [--vocab 8192] [--dim 256] [--experts 8] [--keep 0.5] [--dtype bf16] [--steps 5]
+                                  [--adamw 8]
 
 The model: token table -> router (k experts of all) -> one linear layer per expert -> weighted return -> logits, learning from the
 largest logits of a teacher.  What is a plain matrix product is torch's; the rest are calls of this library:
@@ -15,6 +16,7 @@ largest logits of a teacher.  What is a plain matrix product is torch's; the res
             bsr_t_dense_matmul_batched      the experts' weight gradients from the BSR tensors
             bsr_expert_combine              gradient of the gather
             bsr_embedding_grad              gradient of the token table
+  step      bsr_adamw_batched               with --adamw: all weights in one call, moments in 8 or 32 bits, bfloat16 copies beside them
 
 One small copy to the host per step: the experts' segments, which size their products.
 """
@@ -114,17 +116,28 @@ def main():
     p.add_argument("--keep", type=float, default=0.5)
     p.add_argument("--dtype", choices=("f32", "bf16"), default="bf16")
     p.add_argument("--steps", type=int, default=5)
-    p.add_argument("--rate", type=float, default=2.0)
+    p.add_argument("--adamw", type=int, choices=(8, 32), help="moments in so many bits; otherwise plain steps down the gradient")
+    p.add_argument("--rate", type=float)
     a = p.parse_args()
+    rate = a.rate if a.rate is not None else 2e-3 if a.adamw else 2.0
     dtype = torch.bfloat16 if a.dtype == "bf16" else torch.float32
     model = make_model(a.vocab, a.dim, a.experts, torch.float32)
     batch = make_batch(a.tokens, a.vocab, a.entries)
+    cast = {n: t.to(dtype) for n, t in model.items()}
+    states = None
     for i in range(a.steps):
-        cast = {n: t.to(dtype) for n, t in model.items()}
         loss, grads = step(cast, batch, k=a.choices, keep=a.keep)
-        for n in ("table", "router", "out"):
-            model[n] -= a.rate * grads[n]
-        model["experts"] -= a.rate * torch.stack(grads["experts"])
+        grads["experts"] = torch.stack(grads["experts"])
+        if a.adamw:
+            copies = list(cast.values()) if a.dtype == "bf16" else None
+            optimizer = B.AdamWBatch(list(model.values()), [grads[n].contiguous() for n in model], bits=a.adamw, states=states, copies=copies,
+                                     weight_decay=0.01)
+            B.bsr_adamw_batched(optimizer, lr=rate, step=i + 1)
+            states = optimizer.states
+        else:
+            for n, t in model.items():
+                t -= rate * grads[n]
+                cast[n].copy_(t)
         print(f"step {i}: loss {float(loss):.4f}", flush=True)
 
 

@@ -369,3 +369,17 @@ def test_optimizer_keeps_the_memory_it_was_given():
     torch.cuda.synchronize()
     assert not any(t.any() for t in others) and not p.data.any()
     assert (batch.params[0] - 0.5).abs().max() < 1e-6
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("more", [[], ["--adamw", "8"], ["--adamw", "32"]])
+def test_example_with_and_without_the_optimizer(monkeypatch, capsys, dtype, more):
+    monkeypatch.setattr("sys.argv", ["token_step.py", "--tokens", "256", "--vocab", "512", "--dim", "64", "--steps", "3", "--dtype", dtype, *more])
+    import importlib.util
+    from pathlib import Path
+    spec = importlib.util.spec_from_file_location("token_step_example", Path(__file__).resolve().parent.parent / "examples" / "token_step.py")
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    example.main()
+    losses = [float(line.split()[-1]) for line in capsys.readouterr().out.splitlines() if line.startswith("step ")]
+    assert len(losses) == 3 and all(np.isfinite(losses)) and losses[0] != losses[2]
