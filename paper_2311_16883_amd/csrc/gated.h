@@ -79,6 +79,8 @@ inline int32_t blocks_for(int64_t threads) { return (int32_t)std::min(ceil_div(t
 
 // gated_bf16.hip, gated_f32.hip: the product and, of a split contraction, the sum of the parts.
 int launch_product_bf16(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s);
+// (M <= 32)
+int launch_gated_rows_bf16(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, hipStream_t s);
 int launch_product_f32(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s);
 
 }  // namespace bsr

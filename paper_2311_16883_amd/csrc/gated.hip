@@ -4,7 +4,9 @@
 //   backward  dGU from GU and dH, then dX = dGU W^T  (both operands contiguous along the contraction)
 //
 // bfloat16 operands whose rows are not whole words are copied into the workspace first, rows padded; then so is the contraction,
-// with zeros.  Where there are few tiles the contraction is split and a second kernel adds the parts up, in order.
+// with zeros.  Where there are few tiles the contraction is split and a second kernel adds the parts up, in order.  Few rows read W once, at the
+// rate of memory: 1 x 2048 x [2 x 5504] bfloat16 11.0 us (4.1 TB/s).  Large products are bound by the matrix cores (8192 rows of the same: 370 us, 1.0
+// PFLOP/s), the slopes by memory (25088 x [2 x 1024]: 40 us, 6.4 TB/s).
 #include "gated.h"
 
 namespace bsr {
@@ -217,7 +219,6 @@ constexpr int kCus = 256;
 // Bytes of GU from which it and dH pass by the caches, which then keep more of dGU for the product (25088 x 384 x [2 x 1024]: 97.3 us, 90.7 so).
 constexpr int64_t kStream = int64_t(64) << 20;
 
-
 int64_t padded(int64_t n, int dtype) {
   const int64_t ve = 16 / elem_bytes(dtype);
   return ceil_div(n, ve) * ve;
@@ -294,6 +295,7 @@ int product_of(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s) {
 struct Layout {
   Plan plan;
   size_t a = 0, b = 0, partial = 0, all = 0;         // bytes of the packed operands (0: taken in place), of the parts, together
+  bool alone = false;                                // forward: up to 32 rows by a kernel of their own
 };
 
 // Rows that gated_few_kernel takes (with four, its sums leave registers for half as many waves: 19 us, the matrix cores 16).
@@ -307,6 +309,18 @@ Layout forward_layout(const GatedArgs &g) {
   const size_t e = (size_t)elem_bytes(g.dtype);
   if (g.D > 0 && !in_place(g.X, g.dtype, g.ldx, g.D)) l.a = align_up((size_t)g.M * (size_t)padded(g.D, g.dtype) * e, 256);
   if (g.D > 0 && !in_place(g.W, g.dtype, g.ldw, g.F)) l.b = align_up((size_t)g.D * 2 * (size_t)padded(g.F, g.dtype) * e, 256);
+  // Up to 32 rows by one launch that reads W once and copies nothing, where a workgroup for each 32 columns has a compute unit for itself and
+  // the contraction is not so long that more of them sharing it are faster (8 rows: 2048 x [2 x 5504] 11.0 us, by tiles 16.3; 1024 x [2 x 1024]
+  // 5.9 and 8.8; 4096 x [2 x 4096] 22.8 and 19.1; 8192 x [2 x 1024] 35 and 12; rows of W that are no whole vectors: 2048 x [2 x 5503] 21.7 and
+  // 31.7, 4096 x [2 x 1501] 34 and 22; 64 x [2 x 64] 5.1 and 4.5).
+  const double copied = l.b != 0 ? 3.0 + 2.0 * (double)l.b / 5e6 : 0.0;
+  const bool vectors = (uintptr_t)g.W % 16 == 0 && g.ldw % 8 == 0 && g.F % 8 == 0;
+  l.alone = g.dtype == BSR_BF16 && g.M <= 32 && (g.D >= 128 || l.b != 0) && ceil_div(g.F, (int64_t)32) <= kCus &&
+            4.9 + (vectors ? 3.4e-3 : 7e-3) * (double)g.D < l.plan.us + copied;
+  if (l.alone) {
+    l.a = l.b = 0;
+    return l;
+  }
   l.partial = partial_bytes(l.plan, g.M, g.F, true);
   l.all = l.a + l.b + l.partial;
   return l;
@@ -365,6 +379,7 @@ int forward(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, vo
     return check_launch();
   }
   const Layout l = forward_layout(g);
+  if (l.alone) return launch_gated_rows_bf16(g, H, ldh, GU, ldgu, s);
   uint8_t *const at = static_cast<uint8_t *>(ws);
   ProductArgs a = {};
   a.A = g.X;

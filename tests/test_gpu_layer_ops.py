@@ -164,10 +164,15 @@ def test_gated_many_tiles(dtype):
     check(dX, d @ f64(w).T, (2 * F + 1) * P.U * size, dtype, "dX")
 
 
-# Sizes that the larger tiles take, each with its contraction whole and split where that occurs, and with whole vectors or not.
+# Sizes that every tile takes, each with its contraction whole and split where that occurs, and with whole vectors or not (the smallest of each).
+TILE_SIZES = [(684, 8, 6412), (580, 8, 6885), (290, 8, 6838), (204, 8, 8257), (2098, 4548, 67), (69, 4944, 2248), (7167, 9, 524), (8916, 8, 437),
+              (4608, 5970, 8), (4608, 5976, 8), (69, 10, 9518), (67, 8, 9439), (1035, 9078, 9), (2118, 3896, 8), (34, 10, 8), (37, 8, 9),
+              (38, 1012, 8), (33, 1344, 8), (10578, 8, 273), (8479, 8, 328), (3407, 2643, 8), (3219, 3108, 12), (45, 8, 8), (39, 253, 8),
+              (47, 256, 8), (1, 12, 8), (1, 117, 8), (1, 152, 8), (20, 9000, 40), (9, 9001, 33), (5, 70, 8300), (32, 64, 8256)]
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,D,F", [(1706, 32, 2490), (1706, 32, 2496), (1264, 32, 1638), (80, 10447, 1034), (80, 10448, 1040), (1659, 51, 2464),
-                                   (4643, 7294, 8), (4643, 7296, 8), (525, 32, 1865), (4148, 1978, 8), (4148, 1984, 16)])
+@pytest.mark.parametrize("M,D,F", TILE_SIZES)
 def test_gated_ff_in_every_tile(dtype, M, D, F):
     x, w = randn(1, M, D, dtype=dtype), randn(2, D, 2 * F, dtype=dtype, scale=D ** -0.5)
     H, GU = B.bsr_gated_ff(x.cuda(), w.cuda(), act="gelu_tanh", want_GU=True)
@@ -177,9 +182,32 @@ def test_gated_ff_in_every_tile(dtype, M, D, F):
     assert torch.equal(B.bsr_gated_ff(x.cuda(), w.cuda(), act="gelu_tanh"), H)
 
 
+@pytest.mark.parametrize("act", ["silu", "relu"])
+@pytest.mark.parametrize("M,D,F,pad,offset", [(1, 130, 3, 0, 0), (3, 128, 32, 0, 0), (4, 1024, 40, 8, 0), (5, 1025, 37, 3, 1), (16, 1040, 96, 0, 0), (17, 2047, 65, 0, 0),
+                                              (31, 2100, 31, 1, 3), (32, 3000, 64, 16, 8), (32, 1500, 7, 0, 0), (7, 77, 33, 5, 0), (29, 400, 8190, 0, 0)])
+def test_up_to_32_rows(act, M, D, F, pad, offset):
+    """Slices and vectors that the contraction or the columns end in, rows behind the last one, NaN around the operands."""
+    x, w = randn(1, M, D, dtype="bf16"), randn(2, D, 2 * F, dtype="bf16", scale=D ** -0.5)
+    H, GU = strided(torch.zeros(M, F, dtype=torch.bfloat16), pad, offset, 7.0), strided(torch.zeros(M, 2 * F, dtype=torch.bfloat16), pad, offset, 7.0)
+    B.bsr_gated_ff(strided(x, pad, offset), strided(w, pad, offset), act=act, H=H, GU=GU)
+    assert around_is_untouched(H, pad, offset, 7.0) and around_is_untouched(GU, pad, offset, 7.0)
+    h, e_h, gu, e_gu = P.gated(f64(x), f64(w), act, "bf16")
+    check(GU, gu, e_gu, "bf16", "GU")
+    check(H, h, e_h, "bf16", "H")
+    # a row does not depend on the others
+    again = B.bsr_gated_ff(strided(torch.cat((x, x))[:min(32, 2 * M)], pad, offset), strided(w, pad, offset), act=act)
+    if M > 2:
+        assert torch.equal(again[:M], H)
+
+
+TILE_GRAD_SIZES = [(3209, 2826, 9), (1922, 4653, 8), (2231, 2694, 9), (2359, 2565, 8), (4964, 8, 2370), (4662, 9, 2432), (112, 20254, 9),
+                   (107, 18935, 8), (4156, 8, 818), (1059, 8, 3404), (8539, 147, 9), (10729, 137, 8), (37, 8, 9), (34, 8, 8), (39, 8, 485),
+                   (38, 9, 488), (1, 8, 9), (1, 8, 8), (1, 8, 198), (1, 8, 232), (3740, 8, 1081), (6597, 9, 564), (36, 9, 129), (52, 9, 114),
+                   (1, 8, 79), (1, 8, 78)]
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,D,F", [(129, 49943, 9), (129, 49944, 16), (1883, 3205, 33), (1883, 3205, 36), (4412, 32, 5253), (4412, 32, 5256), (986, 2962, 33),
-                                   (2132, 32, 2589), (2132, 32, 2592), (515, 3672, 34), (515, 3672, 36), (1003, 2700, 70)])
+@pytest.mark.parametrize("M,D,F", TILE_GRAD_SIZES)
 def test_gated_ff_grad_in_every_tile(dtype, M, D, F):
     gu, dh, w = randn(1, M, 2 * F, dtype=dtype), randn(2, M, F, dtype=dtype), randn(3, D, 2 * F, dtype=dtype)
     dX, dGU = B.bsr_gated_ff_grad(gu.cuda(), dh.cuda(), w.cuda(), act="silu")

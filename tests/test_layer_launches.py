@@ -99,7 +99,28 @@ def test_one_and_two_rows_are_one_launch(recorder):
     for M in (1, 2):
         assert len(kernels(recorder, gated(M, 1000, 700))) == 1
         assert "gated_few_kernel" in kernels(recorder, gated(M, 1000, 701))[0]
-    assert any("product_kernel" in k for k in kernels(recorder, gated(1, 1000, 7)))        # (fewer columns than a vector)
+    assert any("product_kernel" in k for k in kernels(recorder, gated(1, 1000, 3, F32)))    # (fewer columns than a vector)
+
+
+def test_up_to_32_rows_are_one_launch_where_that_is_faster(recorder):
+    for M, D, F in ((3, 1000, 704), (32, 2048, 5504), (16, 1000, 701), (1, 1000, 7)):
+        names = kernels(recorder, gated(M, D, F))
+        assert len(names) == 1 and "gated_rows_kernel" in names[0], names
+    for M, D, F in ((33, 1000, 700), (8, 8192, 1024), (8, 256, 16384), (3, 64, 64)):
+        assert "product_kernel" in kernels(recorder, gated(M, D, F))[0]
+
+
+def test_sizes_of_the_gpu_tests_reach_every_product_kernel(recorder):
+    from test_gpu_layer_ops import GATED_SIZES, TILE_GRAD_SIZES, TILE_SIZES
+    reached = set()
+    for dtype in (BF16, F32):
+        for sizes, call in ((GATED_SIZES + TILE_SIZES, gated), (GATED_SIZES + TILE_GRAD_SIZES, gated_grad)):
+            for size in sizes:
+                reached |= {n for n in kernels(recorder, call(*size, dtype)) if "product_kernel" in n}
+    there = {n for n in subprocess.run(["nm", str(LIB)], capture_output=True, text=True, check=True).stdout.split() if "product_kernel" in n}
+    there = {n for n in there if "__device_stub__" not in n}
+    assert reached and reached <= there
+    assert sorted(there - reached) == []
 
 
 def test_few_rows_of_a_norm_leave_nothing_to_add_up(recorder):
