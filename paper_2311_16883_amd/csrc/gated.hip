@@ -243,13 +243,13 @@ bool has_tile(Tile t, int dtype, bool gated) {
 // of the contraction.  (Whether GU is written has no part in it: H would have other bits with GU than without.)
 double estimate_us(Tile t, int64_t M, int64_t N, int64_t K, int dtype, bool gated, int64_t splits) {
   const double rates[2][7][2] = {{{4.9, 4.9}, {4.6, 4.4}, {2.4, 3.6}, {3.4, 3.4}, {3.0, 3.0}, {2.9, 2.8}, {1.0, 1.8}},
-                                 {{0, 0}, {0, 0}, {0.46, 0.53}, {0, 0}, {0, 0}, {0.45, 0.47}, {0.3, 0.45}}};
+                                 {{0, 0}, {0, 0}, {0.46, 0.53}, {0, 0}, {0, 0}, {0.45, 0.47}, {0.4, 0.45}}};
   const TileSize &s = kTiles[t];
   const bool f32 = dtype == BSR_F32;
   const int64_t tiles = ceil_div(M, (int64_t)s.rows) * ceil_div(N, (int64_t)(gated ? s.cols / 2 : s.cols)) * splits;
   const int64_t each = ceil_div(tiles, (int64_t)kCus);
   const double rate = rates[f32][t][each > 1];
-  const double more = (f32 ? 24.0 : 128.0) * (gated && splits == 1 ? 2.0 : 1.0);
+  const double more = f32 ? (gated && splits == 1 ? 48.0 : 24.0) : t == kTile32 && splits == 1 ? 64.0 : gated && splits == 1 ? 256.0 : 128.0;
   double us = 3.0 + (double)each * s.rows * s.cols * 2.0 * (ceil_div(K, splits) + more) / (rate * 1e6);
   if (splits > 1) us += 4.0 + (double)splits * M * N * (gated ? 2 : 1) * 8.0 / 4e6;
   return us;
@@ -295,29 +295,40 @@ int product_of(const Plan &p, const ProductArgs &a, bool gated, hipStream_t s) {
 struct Layout {
   Plan plan;
   size_t a = 0, b = 0, partial = 0, all = 0;         // bytes of the packed operands (0: taken in place), of the parts, together
-  bool alone = false;                                // forward: up to 32 rows by a kernel of their own
+  enum { kTiles, kFew, kRows } by = kTiles;          // forward: by product_kernel, gated_few_kernel or gated_rows_kernel
 };
 
-// Rows that gated_few_kernel takes (with four, its sums leave registers for half as many waves: 19 us, the matrix cores 16).
+// Rows that gated_few_kernel takes (with four, its sums leave registers for half as many waves: 19 us, the matrix cores 16), and the vectors of
+// columns of its workgroups: whole lines as soon as half of the compute units have some (2048 x [2 x 5504] in 172 workgroups of 64 bytes 11.0 us, in
+// 86 of 128 bytes 12.1, in 344 of 32 bytes 19.4; 4096 x [2 x 11008] in 172 of 128 bytes 38.6 (4.7 TB/s), in 344 of 64 bytes 54).
 constexpr int64_t kFewRows = 2;
-bool few_rows(const GatedArgs &g) { return g.M <= kFewRows && g.F >= 16 / elem_bytes(g.dtype) && g.D > 0; }
+int few_vectors(const GatedArgs &g) { return ceil_div(g.F, 16 / (int64_t)elem_bytes(g.dtype)) >= 4 * kCus ? 8 : 4; }
 
 Layout forward_layout(const GatedArgs &g) {
   Layout l;
-  if (few_rows(g)) return l;
   l.plan = plan_product(g.M, g.F, g.D, g.dtype, true);
   const size_t e = (size_t)elem_bytes(g.dtype);
   if (g.D > 0 && !in_place(g.X, g.dtype, g.ldx, g.D)) l.a = align_up((size_t)g.M * (size_t)padded(g.D, g.dtype) * e, 256);
   if (g.D > 0 && !in_place(g.W, g.dtype, g.ldw, g.F)) l.b = align_up((size_t)g.D * 2 * (size_t)padded(g.F, g.dtype) * e, 256);
-  // Up to 32 rows by one launch that reads W once and copies nothing, where a workgroup for each 32 columns has a compute unit for itself and
-  // the contraction is not so long that more of them sharing it are faster (8 rows: 2048 x [2 x 5504] 11.0 us, by tiles 16.3; 1024 x [2 x 1024]
-  // 5.9 and 8.8; 4096 x [2 x 4096] 22.8 and 19.1; 8192 x [2 x 1024] 35 and 12; rows of W that are no whole vectors: 2048 x [2 x 5503] 21.7 and
-  // 31.7, 4096 x [2 x 1501] 34 and 22; 64 x [2 x 64] 5.1 and 4.5).
-  const double copied = l.b != 0 ? 3.0 + 2.0 * (double)l.b / 5e6 : 0.0;
+  // Few rows by one launch that reads W once and copies nothing, where a compute unit's share of W, which it reads at 36 GB/s, is not so long
+  // that more of them sharing the contraction are faster.  Microseconds by tiles, of gated_few_kernel with one row and two, of gated_rows_kernel:
+  // 2048 x [2 x 5504] 15.4, 10.9, 13.2, 10.7; 1024 x [2 x 1024] 8.8, 5.9, 8.2, 5.8; 4096 x [2 x 11008] 41, 38.6, 41, 51; 4096 x [2 x 4096] 18.8, 21.7, 24, 22;
+  // 8192 x [2 x 1024] 12, 34, 37, 32; rows that are no whole vectors, 2048 x [2 x 5503] 31, 12.8, 14.6, 21.3; 4000 x [2 x 1500] 11, 18.7, 21.6, 29; binary32,
+  // 2048 x [2 x 5504] 24.6, 20.5, 21.3, 11008 x [2 x 2048] 39, 84, 89.
+  const double bytes = 2.0 * (double)g.D * (double)g.F * (double)e;
+  double best = std::max(l.plan.us, 4.0 + bytes / 4.7e6) + (l.b != 0 ? 3.0 + 2.0 * (double)l.b / 5e6 : 0.0);
+  auto consider = [&](decltype(l.by) by, int64_t columns, double per_mb) {       // columns of G of a workgroup
+    const double share = (double)ceil_div(ceil_div(g.F, columns), (int64_t)kCus) * (double)g.D * (double)(2 * columns) * (double)e;
+    const double us = 4.9 + std::max(share / 1e6 * per_mb, bytes / 4.7e6 - 4.9) + (by == Layout::kFew && g.M > 1 ? 2.4 : 0.0);
+    if (us > best) return;
+    best = us;
+    l.by = by;
+  };
+  if (g.D > 0 && g.M <= kFewRows && g.F >= 16 / (int64_t)e) consider(Layout::kFew, few_vectors(g) * 16 / (int64_t)e, 28.0);
   const bool vectors = (uintptr_t)g.W % 16 == 0 && g.ldw % 8 == 0 && g.F % 8 == 0;
-  l.alone = g.dtype == BSR_BF16 && g.M <= 32 && (g.D >= 128 || l.b != 0) && ceil_div(g.F, (int64_t)32) <= kCus &&
-            4.9 + (vectors ? 3.4e-3 : 7e-3) * (double)g.D < l.plan.us + copied;
-  if (l.alone) {
+  if (g.dtype == BSR_BF16 && g.M <= 32 && (g.D >= 128 || l.b != 0) && ceil_div(g.F, (int64_t)32) <= kCus)
+    consider(Layout::kRows, 32, (vectors ? 26.0 : 54.0) * (1.0 + (double)g.M / 64.0));
+  if (l.by != Layout::kTiles) {
     l.a = l.b = 0;
     return l;
   }
@@ -366,20 +377,18 @@ void run_few(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, h
     if (g.M == 1) go(std::integral_constant<int, 1>(), v);
     else go(std::integral_constant<int, 2>(), v);
   };
-  // whole lines as soon as half of the compute units have some: 2048 x [2 x 5504] in 172 workgroups of 64 bytes 11.0 us, in 86 of 128 bytes
-  // 12.1, in 344 of 32 bytes 19.4; 4096 x [2 x 11008] in 172 of 128 bytes 38.6 (4.7 TB/s), in 344 of 64 bytes 54
-  if (vecs >= 4 * kCus) rows(std::integral_constant<int, 8>());
+  if (few_vectors(g) == 8) rows(std::integral_constant<int, 8>());
   else rows(std::integral_constant<int, 4>());
 }
 
 template <typename T>
 int forward(const GatedArgs &g, void *H, int64_t ldh, void *GU, int64_t ldgu, void *ws, hipStream_t s) {
-  if (few_rows(g)) {
+  const Layout l = forward_layout(g);
+  if (l.by == Layout::kFew) {
     run_few<T>(g, H, ldh, GU, ldgu, s);
     return check_launch();
   }
-  const Layout l = forward_layout(g);
-  if (l.alone) return launch_gated_rows_bf16(g, H, ldh, GU, ldgu, s);
+  if (l.by == Layout::kRows) return launch_gated_rows_bf16(g, H, ldh, GU, ldgu, s);
   uint8_t *const at = static_cast<uint8_t *>(ws);
   ProductArgs a = {};
   a.A = g.X;

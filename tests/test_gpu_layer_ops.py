@@ -200,7 +200,7 @@ def test_up_to_32_rows(act, M, D, F, pad, offset):
         assert torch.equal(again[:M], H)
 
 
-TILE_GRAD_SIZES = [(3209, 2826, 9), (1922, 4653, 8), (2231, 2694, 9), (2359, 2565, 8), (4964, 8, 2370), (4662, 9, 2432), (112, 20254, 9),
+TILE_GRAD_SIZES = [(3, 20, 333), (3, 20, 336), (3209, 2826, 9), (1922, 4653, 8), (2231, 2694, 9), (2359, 2565, 8), (4964, 8, 2370), (4662, 9, 2432), (112, 20254, 9),
                    (107, 18935, 8), (4156, 8, 818), (1059, 8, 3404), (8539, 147, 9), (10729, 137, 8), (37, 8, 9), (34, 8, 8), (39, 8, 485),
                    (38, 9, 488), (1, 8, 9), (1, 8, 8), (1, 8, 198), (1, 8, 232), (3740, 8, 1081), (6597, 9, 564), (36, 9, 129), (52, 9, 114),
                    (1, 8, 79), (1, 8, 78)]
