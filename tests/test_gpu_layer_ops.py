@@ -164,11 +164,12 @@ def test_gated_many_tiles(dtype):
     check(dX, d @ f64(w).T, (2 * F + 1) * P.U * size, dtype, "dX")
 
 
-# Sizes that every tile takes, each with its contraction whole and split where that occurs, and with whole vectors or not (the smallest of each).
-TILE_SIZES = [(684, 8, 6412), (580, 8, 6885), (290, 8, 6838), (204, 8, 8257), (2098, 4548, 67), (69, 4944, 2248), (7167, 9, 524), (8916, 8, 437),
-              (4608, 5970, 8), (4608, 5976, 8), (69, 10, 9518), (67, 8, 9439), (1035, 9078, 9), (2118, 3896, 8), (34, 10, 8), (37, 8, 9),
-              (38, 1012, 8), (33, 1344, 8), (10578, 8, 273), (8479, 8, 328), (3407, 2643, 8), (3219, 3108, 12), (45, 8, 8), (39, 253, 8),
-              (47, 256, 8), (1, 12, 8), (1, 117, 8), (1, 152, 8), (20, 9000, 40), (9, 9001, 33), (5, 70, 8300), (32, 64, 8256)]
+# Sizes that every tile takes, each with its contraction whole and split where that occurs, and with whole vectors or not.
+TILE_SIZES = [(1, 8, 10), (1, 2168, 16), (1, 2385, 10), (2, 8, 8), (2, 13, 12), (2, 16, 16), (3, 168, 16), (4, 187, 8), (33, 1990, 12), (35, 9, 8),
+              (36, 16, 16), (39, 348, 8), (41, 8, 10), (45, 16, 16), (65, 1048, 8), (66, 280, 9), (624, 9, 6982), (798, 8, 5217), (3099, 8, 413),
+              (3342, 4608, 8), (3918, 8, 948), (4140, 11042, 14), (4261, 2664, 16), (4793, 3594, 9), (6341, 8, 325), (6552, 1406, 10),
+              (6661, 9, 312), (7059, 9, 399), (8203, 4872, 16), (8291, 22, 433), (10347, 8, 68), (11432, 16, 304), (2098, 4548, 67),
+              (69, 4944, 2248), (80, 10448, 1040), (20, 9000, 40), (9, 9001, 33), (5, 70, 8300), (32, 64, 8256)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -200,10 +201,10 @@ def test_up_to_32_rows(act, M, D, F, pad, offset):
         assert torch.equal(again[:M], H)
 
 
-TILE_GRAD_SIZES = [(3, 20, 333), (3, 20, 336), (3209, 2826, 9), (1922, 4653, 8), (2231, 2694, 9), (2359, 2565, 8), (4964, 8, 2370), (4662, 9, 2432), (112, 20254, 9),
-                   (107, 18935, 8), (4156, 8, 818), (1059, 8, 3404), (8539, 147, 9), (10729, 137, 8), (37, 8, 9), (34, 8, 8), (39, 8, 485),
-                   (38, 9, 488), (1, 8, 9), (1, 8, 8), (1, 8, 198), (1, 8, 232), (3740, 8, 1081), (6597, 9, 564), (36, 9, 129), (52, 9, 114),
-                   (1, 8, 79), (1, 8, 78)]
+TILE_GRAD_SIZES = [(1, 8, 14), (1, 9, 91), (1, 10, 8), (1, 10, 94), (1, 10, 558), (1, 11, 9), (1, 15, 8), (1, 16, 424), (33, 9, 623), (34, 8, 13),
+                   (36, 11, 19), (36, 13, 8), (44, 10, 126), (44, 11, 8), (59, 11, 113), (62, 8, 616), (141, 13218, 11), (1046, 10033, 8),
+                   (1482, 6300, 11), (1556, 3880, 8), (1961, 3371, 8), (2177, 11, 1971), (2584, 2573, 11), (3080, 652, 8), (3642, 12, 2136),
+                   (4200, 759, 8), (4238, 10, 884), (4507, 10, 4071), (5155, 16, 3384), (6191, 8, 677), (7959, 778, 9), (8402, 298, 10)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
