@@ -239,9 +239,11 @@ bool has_tile(Tile t, int dtype, bool gated) {
 
 // Estimated microseconds, from what the kernels were measured to do: TFLOP/s of a compute unit with one workgroup in it and with two
 // (bfloat16: 8192 x 2048 x [2 x 5504] in 256 x 256 tiles 326 us, in 128 x 256 349, in 128 x 128 390; 2048 rows 97, 85, 93; 512 rows 42, 27, 29;
-// 2999 x 3080 x 808 in 96 x 128 tiles, 224 of them, 24, in 128 x 128, 168 of them, alone in their unit 26, otherwise 45).  A tile's beginning and end cost as much as some more
-// of the contraction.  Tiles of 32 rows: one row of 16384 x [2 x 512] 14.9 us in 16 parts, of 40000 x [2 x 64] 26.1 and in 64 parts 13.7, binary32 47 and 103, in
-// 64 parts 20 and 33.  (Whether GU is written has no part in it: H would have other bits with GU than without.)
+// 2999 x 3080 x 808 in 96 x 128 tiles, 224 of them, 24, in 128 x 128, 168 of them, alone in their unit 26, otherwise 45).  A tile's beginning
+// and end cost as much as some more of the contraction, most where nothing runs beside it (16384 x 128 x [2 x 2048] in 256 x 256 tiles 46 us, in 128 x 256 35,
+// in 128 x 128 51; 8192 x 512 x [2 x 2816] 64, 53, 68).  Tiles of 32 rows, in 16 and in up to 64 parts: one row of 16384 x [2 x 512] 14.9 and
+// 12.4 us, of 40000 x [2 x 64] 26.1 and 13.7, binary32 47 and 20, 103 and 33.  (Whether GU is written has no part in it: H would have other bits
+// with GU than without.)
 double estimate_us(Tile t, int64_t M, int64_t N, int64_t K, int dtype, bool gated, int64_t splits) {
   const double rates[2][7][2] = {{{4.9, 4.9}, {4.6, 4.4}, {2.4, 3.6}, {3.4, 3.4}, {3.0, 3.0}, {2.9, 2.8}, {1.0, 1.8}},
                                  {{0, 0}, {0, 0}, {0.46, 0.53}, {0, 0}, {0, 0}, {0.45, 0.47}, {0.43, 0.45}}};
@@ -250,9 +252,10 @@ double estimate_us(Tile t, int64_t M, int64_t N, int64_t K, int dtype, bool gate
   const int64_t tiles = ceil_div(M, (int64_t)s.rows) * ceil_div(N, (int64_t)(gated ? s.cols / 2 : s.cols)) * splits;
   const int64_t each = ceil_div(tiles, (int64_t)kCus);
   const bool whole = t == kTile32 && !f32 && splits == 1;
-  const double rate = whole ? 1.9 : rates[f32][t][each > 1];
-  const double more = f32 ? (gated && splits == 1 ? 48.0 : 24.0)
-                      : whole ? 170.0 : gated && splits == 1 ? 256.0 : 128.0;
+  const bool results = gated && splits == 1;         // activations and two or three results
+  const double rate = whole ? 1.9 : results && t == kTile256 ? 5.4 : rates[f32][t][each > 1];
+  const double with_results[] = {365.0, 140.0, 200.0, 256.0, 0.0, 256.0, 170.0};
+  const double more = f32 ? (results ? 48.0 : 24.0) : whole || results ? with_results[t] : 128.0;
   double us = 3.0 + (double)each * s.rows * s.cols * 2.0 * (ceil_div(K, splits) + more) / (rate * 1e6);
   if (splits > 1) us += 4.0 + (double)splits * (M * N * (gated ? 2 : 1) * 8.0 / 4e6 + 0.025);
   return us;
@@ -267,8 +270,9 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int dtype, bool gated) {
     const TileSize &s = kTiles[t];
     const int64_t stages = std::max<int64_t>(1, ceil_div(K, (int64_t)(s.row_bytes / elem_bytes(dtype))));
     // (more than 16 parts of long contractions only where they have a compute unit each, of bfloat16 two: more of them at a time are slower)
-    const int64_t across = ceil_div(N, (int64_t)(gated ? s.cols / 2 : s.cols));
-    const int64_t most = t == kTile256 || t == kTile96Alone ? 1 : t != kTile32 ? 16 : std::min<int64_t>(64, std::max<int64_t>(16, kCus / (dtype == BSR_F32 ? 1 : 2) / across));
+    const int64_t across = std::max<int64_t>(1, ceil_div(N, (int64_t)(gated ? s.cols / 2 : s.cols)));
+    const int64_t each = kCus / (dtype == BSR_F32 ? 1 : 2) / across;
+    const int64_t most = t == kTile256 || t == kTile96Alone ? 1 : t != kTile32 ? 16 : std::min<int64_t>(64, std::max<int64_t>(16, each));
     for (int64_t n = 1; n <= most && n * 4 <= std::max<int64_t>(stages, 4); n = t == kTile32 && n < 16 ? n + 1 : 2 * n) {
       const double us = estimate_us((Tile)t, M, N, K, dtype, gated, n);
       if (best == 0.0 || us < best) {

@@ -165,7 +165,7 @@ def test_gated_many_tiles(dtype):
 
 
 # Sizes that every tile takes, each with its contraction whole and split where that occurs, and with whole vectors or not.
-TILE_SIZES = [(1, 8, 10), (1, 2168, 16), (1, 2385, 10), (2, 8, 8), (2, 13, 12), (2, 16, 16), (3, 168, 16), (4, 187, 8), (33, 1990, 12), (35, 9, 8),
+TILE_SIZES = [(13260, 1144, 264), (609, 1143, 6534), (84, 105, 8932), (65, 104, 9048), (1, 8, 10), (1, 2168, 16), (1, 2385, 10), (2, 8, 8), (2, 13, 12), (2, 16, 16), (3, 168, 16), (4, 187, 8), (33, 1990, 12), (35, 9, 8),
               (36, 16, 16), (39, 348, 8), (41, 8, 10), (45, 16, 16), (65, 1048, 8), (66, 280, 9), (624, 9, 6982), (798, 8, 5217), (3099, 8, 413),
               (3342, 4608, 8), (3918, 8, 948), (4140, 11042, 14), (4261, 2664, 16), (4793, 3594, 9), (6341, 8, 325), (6552, 1406, 10),
               (6661, 9, 312), (7059, 9, 399), (8203, 4872, 16), (8291, 22, 433), (10347, 8, 68), (11432, 16, 304), (65, 4616, 2082),
