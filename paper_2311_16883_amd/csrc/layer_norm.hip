@@ -537,8 +537,10 @@ int norm_grad_of(const T *X, int64_t M, int64_t D, int64_t ldx, const void *gamm
     const int64_t groups = ceil_div(M, (int64_t)S::kRows);
     auto go = [&](auto with) {
       constexpr bool SUMS = decltype(with)::value;
-      // a few rows more than a workgroup has in hand: one does them all, and nothing is left to add up
-      const int64_t grid = !SUMS ? std::min(groups, kMostWorkgroups) : groups <= 2 ? 1 : walkers(groups, WAVES);
+      // little more than a workgroup has in hand: one does it all, and nothing is left to add up (bfloat16, one workgroup and several: [32 x 1024]
+      // 7.5 us and 10.0, [64 x 337] 7.8 and 10.2, [64 x 1024] 11.1 and 10.0, [16 x 2048] 10.8 and 10.1, [2 x 9920] 13.3 and 10.1)
+      const bool alone = groups <= 1 || (groups <= 8 && D <= 4096 && M * D <= 25000);
+      const int64_t grid = !SUMS ? std::min(groups, kMostWorkgroups) : alone ? 1 : walkers(groups, WAVES);
       Sums out = {grid > 1 ? partial : nullptr, dgamma, dbeta, accumulate};
       if (SUMS) parts = grid;
       layer_norm_grad_kernel<T, decltype(ve)::value, decltype(nv)::value, decltype(lg)::value, WAVES, decltype(ragged)::value, SUMS>

@@ -33,7 +33,7 @@ def test_layer_norm(dtype, params, M, D, pad, offset):
 
 
 @pytest.mark.parametrize("dtype,params", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
-@pytest.mark.parametrize("M,D,pad,offset", NORM_SIZES + [(5000, 24, 0, 0), (2500, 131, 0, 0), (700, 1024, 0, 0)])
+@pytest.mark.parametrize("M,D,pad,offset", NORM_SIZES + [(5000, 24, 0, 0), (2500, 131, 0, 0), (700, 1024, 0, 0), (24, 1024, 0, 0), (61, 337, 3, 1), (300, 80, 0, 0), (2, 9920, 0, 0)])
 def test_layer_norm_grad(dtype, params, M, D, pad, offset):
     x, dy = randn(1, M, D, dtype=dtype, scale=2.0) + 0.5, randn(4, M, D, dtype=dtype)
     gamma = randn(2, D, dtype=params) + 1
