@@ -145,7 +145,7 @@ __device__ __forceinline__ uint32_t cut_off(double m, float near) {
   return (__float_as_uint(near) & 0x7FFFFFFFu) - (fabs((double)near) > fabs(m) ? 1u : 0u);
 }
 __device__ __forceinline__ uint32_t root_cut_off(double v, float root) {
-  return __float_as_uint(root) - (__builtin_fma((double)root, (double)root, -v) > 0.0 ? 1u : 0u);
+  return (__float_as_uint(root) & 0x7FFFFFFFu) - (__builtin_fma((double)root, (double)root, -v) > 0.0 ? 1u : 0u);
 }
 
 template <typename P, typename G, bool SMALL, bool COPY, bool STREAM>
