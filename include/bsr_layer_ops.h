@@ -106,9 +106,10 @@ int bsr_gated_ff_grad(const void *GU, int dtype, int64_t M, int64_t F, int64_t l
  *   g = grad_scale * grad;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
  *   param = param * (1 - lr * weight_decay)
  *           - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps).
- * All of it is computed in binary32 (the powers of beta, and moments that are held in 8 bits, in binary64, whose v
- * and roots have binary32's range) from the values before the step and rounded where it is stored; the update takes
- * m and v before they are rounded to 8 bits.
+ * All of it is computed in binary32 (the powers of beta, and moments that are held in 8 bits, in binary64: v may leave
+ * binary32's range there, its root may not) from the values before the step and rounded where it is stored; the update takes
+ * m and v before they are rounded to 8 bits.  A v below 2^-150 held in binary32 is 0, and the update then m over eps.  Where
+ * sqrt(v / (1 - beta2^step)) + eps is above 2^126 the update may be 0.
  * Moments in binary32: m [n], v [n].  In 8 bits (BSR_MOMENTS_8BIT): m [n] and v [n] are bytes,
  * and scales holds two rows of bsr_adamw_blocks(n) bytes, those of m and those of v, `scales_stride` bytes apart.  128
  * consecutive elements share a scale byte b:
@@ -119,8 +120,8 @@ int bsr_gated_ff_grad(const void *GU, int dtype, int64_t M, int64_t F, int64_t l
  * A number x between two neighbours goes to the upper one with the probability of its distance
  * from the lower one: k = floor(x / step + u), u a multiple of 2^-16 made from (seed, step, the
  * element's number: tensors in order, each from a multiple of 128 on).  (To the nearest, sqrt(v) would
- * stand still: a step changes it by less than half the distance of its codes.)  A positive
- * sqrt(v) does not become 0.
+ * stand still: a step changes it by less than half the distance of its codes.)  A sqrt(v) of 2^-148 or more does not become 0 in a
+ * block that does not.
  */
 enum { BSR_MOMENTS_F32 = 0, BSR_MOMENTS_8BIT = 1 };
 

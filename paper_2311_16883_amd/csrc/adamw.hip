@@ -145,7 +145,20 @@ __device__ __forceinline__ uint32_t cut_off(double m, float near) {
   return (__float_as_uint(near) & 0x7FFFFFFFu) - (fabs((double)near) > fabs(m) ? 1u : 0u);
 }
 __device__ __forceinline__ uint32_t root_cut_off(double v, float root) {
-  return (__float_as_uint(root) & 0x7FFFFFFFu) - (__builtin_fma((double)root, (double)root, -v) > 0.0 ? 1u : 0u);
+  return __float_as_uint(root) - (__builtin_fma((double)root, (double)root, -v) > 0.0 ? 1u : 0u);
+}
+
+// The root of v >= 0 to one unit in its last place.  The square of a binary32 number need not be one, so half of the (even part of the)
+// exponent goes round the root, and the rest of v through it; infinities and NaN become infinities.
+__device__ __forceinline__ float root_of(double v) {
+  const uint64_t bits = (uint64_t)__double_as_longlong(v);
+  const double rest = __longlong_as_double((long long)((bits & 0x001FFFFFFFFFFFFFu) | 0x3FE0000000000000u));       // in [1/2, 2)
+  return ldexpf(__builtin_amdgcn_sqrtf((float)rest), (int)(bits >> 53) - 511);
+}
+// ... of a binary32 v, whose subnormals the root instruction would lose.
+__device__ __forceinline__ float root_of(float v) {
+  const bool small = v < 0x1p-96f;
+  return __builtin_amdgcn_sqrtf(v * (small ? 0x1p64f : 1.0f)) * (small ? 0x1p-32f : 1.0f);
 }
 
 template <typename P, typename G, bool SMALL, bool COPY, bool STREAM>
@@ -180,6 +193,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
     load_some<PL, STREAM>(param + i, left, p0);
     load_some<PL, STREAM>(grad + i, left, g0);
     const int64_t block = i / kMomentBlock;
+    float eps = o.eps;
     if constexpr (SMALL) {
       uint8_t cm[PL], cv[PL];
       load_some<PL, STREAM>(static_cast<const uint8_t *>(it.m) + i, left, cm);
@@ -190,6 +204,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
         m[q] = decode<3>(cm[q], sm);
         root[q] = decode<4>(cv[q], sv);
       }
+      if (sv == 255u) eps = __uint_as_float(0x7FC00000u);      // (root_of does not pass on a NaN)
     } else {
       load_some<PL, STREAM>(static_cast<const float *>(it.m) + i, left, m);
       load_some<PL, STREAM>(static_cast<const float *>(it.v) + i, left, root);
@@ -201,16 +216,16 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
         const double g = (double)elem_to_float<G>(g0[q]) * grad_scale, old = root[q];
         const double m64 = __builtin_fma(o.beta1, (double)m[q], c1 * g), v = __builtin_fma(o.beta2 * old, old, c2 * g * g);
         m[q] = (float)m64;
-        rt = __builtin_amdgcn_sqrtf((float)v);
+        rt = root_of(v);
         cut_m[q] = cut_off(m64, m[q]);
         cut_r[q] = root_cut_off(v, rt);
       } else {
         const float g = elem_to_float<G>(g0[q]) * o.grad_scale;
         m[q] = o.b1 * m[q] + o.c1 * g;
         root[q] = o.b2 * root[q] + o.c2 * g * g;
-        rt = __builtin_amdgcn_sqrtf(root[q]);
+        rt = root_of(root[q]);
       }
-      p[q] = elem_to_float<P>(p0[q]) * keep - rate * m[q] * __builtin_amdgcn_rcpf(rt * o.root + o.eps);
+      p[q] = elem_to_float<P>(p0[q]) * keep - rate * m[q] * __builtin_amdgcn_rcpf(rt * o.root + eps);
     }
 #pragma unroll
     for (int q = 0; q < PL; ++q) p0[q] = from_float<P>(p[q]);
