@@ -10,8 +10,8 @@
 // 8-bit moments: codes of 4 exponent bits in units of a power of two per block, so that scaling is exact and a value fits bfloat16.
 // sqrt(v) is held in place of v: half the range in the exponent, and the update needs the root anyway.  Rounding is to one of the two
 // neighbours with the probability of the distances, by bits of a counter hash: with beta2 = 0.999 a step changes sqrt(v) by 0.05 % of
-// itself, its codes are 3 to 6 % apart, and to nearest it would never move.  A positive root does not become 0, since the first moment
-// beside it may be larger than its smallest code and would be divided by eps.
+// itself, its codes are 3 to 6 % apart, and to nearest it would never move.  A root does not become 0 beside others that do not, since the
+// first moment beside it may be larger than its smallest code and would be divided by eps.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -24,7 +24,7 @@ namespace {
 
 constexpr int kThreads = 256;
 // Consecutive elements of a lane: 16 bytes of the largest kind of number that is read.  (49 million bfloat16 weights and gradients, 8-bit
-// moments: four a lane 134 us, eight 116; moments in binary32: 212 and 219.)
+// moments: four a lane 149 us, eight 132; moments in binary32: 212 and 219.)
 constexpr int per_lane(size_t param_bytes, bool small) { return param_bytes == 2 && small ? 8 : 4; }
 constexpr int64_t kManyElements = int64_t(4) << 20;    // from here on a workgroup takes four rounds, below one
 // From here on everything is read and written past the caches, which hold none of it until the next step: 49 million elements with binary32 moments
@@ -130,20 +130,20 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t most) {
   return b < 32u ? 0u : b > 255u ? 255u : b;
 }
 
-// A number >= 0, cut off to the binary32 number with these bits, rounded to one of its two neighbours by u in [0, 2^16): the bits below a
-// code's last are added to and cut off.  (The scale leaves room for it: the largest of a block is not above the largest code.)
+// How far a block's numbers are moved; those of a block without a scale far enough to be 0.
+constexpr int kAway = -1000;
+__device__ __forceinline__ int shift_of(uint32_t scale) { return scale == 0u ? kAway : 15 - (int)scale; }
+
+// The code of a number >= 0, rounded to one of its two neighbours by u in [0, 2^16): `moved` is the number nearest to it in the codes' place,
+// `above` whether that is above it, and so not what it is cut off to there.  The bits below a code's last are added to and cut off.  (The
+// scale leaves room for it: the largest of a block is not above the largest code.)
 template <int BITS>
-__device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t scale, uint32_t u) {
-  const uint32_t code = (__float_as_uint(ldexpf(__uint_as_float(bits), 15 - (int)scale)) + (u << (7 - BITS))) >> (23 - BITS);
-  return scale == 0u || scale == 255u ? 0u : BITS == 4 ? max(code, min(bits, 1u)) : code;
+__device__ __forceinline__ uint32_t encode(float moved, bool above, uint32_t u) {
+  return (__float_as_uint(moved) - (above ? 1u : 0u) + (u << (7 - BITS))) >> (23 - BITS);
 }
 
-// A moment m, or the root of v, as the bits of the binary32 number that its magnitude is cut off to; `near`, `root`: the number
-// nearest to it.  What a code's border decides hangs on the last bit: of 49 million elements 40 .. 60 have another code where m and v are made in
-// binary32, 0 .. 3 from binary64, whose multiplies and adds are as fast (180 million elements 548 us and 572, with correctly rounded roots 582).
-__device__ __forceinline__ uint32_t cut_off(double m, float near) {
-  return (__float_as_uint(near) & 0x7FFFFFFFu) - (fabs((double)near) > fabs(m) ? 1u : 0u);
-}
+// The root of v cut off to binary32, as bits; `root`: one of the two numbers beside it.  What a code's border decides hangs on the last bit: of 49
+// million elements 40 .. 60 have another code where m and v are made in binary32.  Binary64, whose multiplies and adds are as fast, costs 4 %.
 __device__ __forceinline__ uint32_t root_cut_off(double v, float root) {
   return __float_as_uint(root) - (__builtin_fma((double)root, (double)root, -v) > 0.0 ? 1u : 0u);
 }
@@ -189,7 +189,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
     P p0[PL];
     G g0[PL];
     float m[PL], root[PL], p[PL];
-    uint32_t cut_m[SMALL ? PL : 1], cut_r[SMALL ? PL : 1];
+    double m64[SMALL ? PL : 1];
+    uint32_t cut_r[SMALL ? PL : 1];
     load_some<PL, STREAM>(param + i, left, p0);
     load_some<PL, STREAM>(grad + i, left, g0);
     const int64_t block = i / kMomentBlock;
@@ -214,10 +215,10 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
       float rt;
       if constexpr (SMALL) {
         const double g = (double)elem_to_float<G>(g0[q]) * grad_scale, old = root[q];
-        const double m64 = __builtin_fma(o.beta1, (double)m[q], c1 * g), v = __builtin_fma(o.beta2 * old, old, c2 * g * g);
-        m[q] = (float)m64;
+        m64[q] = __builtin_fma(o.beta1, (double)m[q], c1 * g);
+        const double v = __builtin_fma(o.beta2 * old, old, c2 * g * g);
+        m[q] = (float)m64[q];
         rt = root_of(v);
-        cut_m[q] = cut_off(m64, m[q]);
         cut_r[q] = root_cut_off(v, rt);
       } else {
         const float g = elem_to_float<G>(g0[q]) * o.grad_scale;
@@ -240,20 +241,29 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(List list, int n, int r
       uint32_t most_m = 0u, most_v = 0u;
 #pragma unroll
       for (int q = 0; q < PL; ++q) {
-        most_m = max(most_m, q < left ? cut_m[q] : 0u);
+        most_m = max(most_m, q < left ? __float_as_uint(m[q]) & 0x7FFFFFFFu : 0u);
         most_v = max(most_v, q < left ? cut_r[q] : 0u);
       }
       const uint32_t sm = scale_of<3>(group_max<kGroup>(most_m)), sv = scale_of<4>(group_max<kGroup>(most_v));
+      const int by_m = shift_of(sm), by_r = shift_of(sv);
+      const uint32_t least = sv == 0u ? 0u : 1u;
       uint8_t cm[PL], cv[PL];
       const uint64_t number = (uint64_t)(it.first + i);       // (its high half is that of all)
       const uint32_t base = (uint32_t)number * 0x9E3779B1u + (uint32_t)(number >> 32) * 0x7F4A7C15u + o.key;
 #pragma unroll
       for (int q = 0; q < PL; ++q) {
         const uint32_t h = mix(base + (uint32_t)q * 0x9E3779B1u);
-        const uint32_t c = encode<3>(cut_m[q], sm, h & 0xFFFFu);
+        const float near = ldexpf(fabsf(m[q]), by_m), cut = __uint_as_float(cut_r[q]), near_r = ldexpf(cut, by_r);
+        const uint32_t c = encode<3>(near, (double)ldexpf(near, -by_m) > fabs(m64[q]), h & 0xFFFFu);
         cm[q] = (uint8_t)(c | (c != 0u && m[q] < 0.0f ? 128u : 0u));
-        cv[q] = (uint8_t)encode<4>(cut_r[q], sv, h >> 16);
+        cv[q] = (uint8_t)max(encode<4>(near_r, ldexpf(near_r, -by_r) > cut, h >> 16), min(cut_r[q], least));
       }
+      if (sm == 255u)
+#pragma unroll
+        for (int q = 0; q < PL; ++q) cm[q] = 0;
+      if (sv == 255u)
+#pragma unroll
+        for (int q = 0; q < PL; ++q) cv[q] = 0;
       store_some<PL, STREAM>(static_cast<uint8_t *>(it.m) + i, left, cm);
       store_some<PL, STREAM>(static_cast<uint8_t *>(it.v) + i, left, cv);
       if (threadIdx.x % (kMomentBlock / PL) == 0 && left > 0) {

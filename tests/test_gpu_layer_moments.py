@@ -1,4 +1,5 @@
-"""The optimizer's moments where their numbers come to an end: roots of second moments below and above binary32's range, gradients of any NaN."""
+"""The optimizer's moments where their numbers come to an end: roots of second moments below and above binary32's range, codes beside
+their borders, gradients of any NaN."""
 import math
 
 import numpy as np
@@ -63,6 +64,30 @@ def test_small_second_moments_in_binary32_have_the_roots_of_what_is_held(size, e
     denominator = np.sqrt(f64(v)) / math.sqrt(1 - BETA2) + o["eps"]
     want = -o["lr"] / (1 - 0.9) * f64(m) / denominator
     check(p, want, 16 * U * np.abs(want), what="param")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [3, 4])
+def test_codes_are_cut_off_just_below_their_borders(bits, dtype):
+    """Without an exponent codes are a fixed distance apart: one rounding step below the border, to which u would carry it, a number has the code below."""
+    n, seed, step = 128 * 40, 21, 1
+    u = P.uniform(0, n, seed, step)[0 if bits == 3 else 1]
+    unit = 2.0 ** (0 - 14 - bits)                    # of blocks whose largest number is 1
+    k = np.arange(n) % (1 << bits)
+    border = ((k + 1 - u) * unit).astype(np.float32)             # (exact: at most 4 + 16 bits)
+    x = np.nextafter(border, np.float32(0))
+    x[::128] = 1.0
+    batch = B.AdamWBatch([torch.zeros(n, dtype=dtype, device="cuda")], [torch.from_numpy(x).cuda()], bits=8)
+    # without a past: m is the gradient, and v its square, exactly
+    B.bsr_adamw_batched(batch, lr=1e-3, step=step, beta1=0.0, beta2=0.0, seed=seed)
+    codes, scales = batch.states[0][0 if bits == 3 else 1].cpu().numpy(), batch.states[0][2].cpu().numpy()[0 if bits == 3 else 1]
+    assert (scales == 127).all()
+    value = P.decode(codes, scales, bits)
+    own = np.floor(np.log2(x.astype(float))) - bits
+    distance = 2.0 ** np.maximum(own, -14 - bits)
+    want = np.floor(x.astype(float) / distance + u) * distance
+    want = np.maximum(want, unit) if bits == 4 else want
+    assert np.array_equal(value, want), (int((value != want).sum()), np.argwhere(value != want)[:4].ravel())
 
 
 @pytest.mark.parametrize("dtype,word", [(torch.float32, -1), (torch.float32, 0x7FFFFFFF), (torch.float32, 0x7F800001), (torch.bfloat16, -1), (torch.bfloat16, 0x7FFF)])
