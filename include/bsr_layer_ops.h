@@ -35,7 +35,7 @@ extern "C" {
  * every row, or NULL.  Y (of dtype) may be X itself, with ldy == ldx.
  * eps in [2^-126, 2^126] (BSR_ERR_VALUE).  A row that holds a NaN or an infinity, or whose
  * squares overflow binary32, gives NaN or the values that this arithmetic has; other rows are
- * not touched by it.
+ * not touched by it.  D == 0: nothing is written, stats neither.
  */
 int bsr_layer_norm(const void *X, int dtype, int64_t M, int64_t D, int64_t ldx,
                    const void *gamma, const void *beta, int param_dtype, float eps,

@@ -667,7 +667,7 @@ def bsr_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: 
                    eps: float = 1e-5, Y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
                    want_stats: bool = False, stream=None):
     """-> Y [M x D] (which may be X itself), or (Y, stats float32 [M x 2]: mean and 1 / sqrt(variance + eps) of every row,
-    what bsr_layer_norm_grad needs beside X)."""
+    what bsr_layer_norm_grad needs beside X; 0 and 1 / sqrt(eps) of rows without columns)."""
     r = (_native or _load_native()).layer_norm(X, gamma, beta, eps, Y, stats, want_stats, stream)
     return r if type(r) is not int else _failed(r, X, "bsr_layer_norm")
 

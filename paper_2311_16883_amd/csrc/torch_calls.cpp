@@ -12,10 +12,13 @@
 #include <Python.h>
 
 #include <climits>
+#include <cmath>
 #include <optional>
 #include <string>
 
 #include <ATen/ops/empty.h>
+#include <ATen/ops/fill.h>
+#include <ATen/ops/select.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -729,6 +732,12 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
                             with_stats ? typed<float>(stats.get()) : nullptr, stream.handle());
     });
     if (rc != BSR_OK) return code_result(rc);
+    if (with_stats && x.cols == 0 && x.rows > 0) {          // (the library writes nothing then)
+      const at::AutoDispatchBelowAutograd plain;
+      at::Tensor mean = at::select(stats.get(), 1, 0), rstd = at::select(stats.get(), 1, 1);
+      at::fill_(mean, 0.0);
+      at::fill_(rstd, 1.0 / std::sqrt((double)(float)eps));
+    }
     return with_stats ? Py_BuildValue("(NN)", Y.result(), stats.result()) : Y.result();
   });
 }

@@ -1,0 +1,28 @@
+"""Calls at the edge of what the layer operators take."""
+import pytest
+import torch
+
+from paper_2311_16883_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("eps", [1e-5, 2.0 ** -20])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_statistics_of_rows_without_columns(dtype, eps):
+    want = torch.tensor([0.0, eps]).rsqrt_()
+    want[0] = 0.0
+    x = torch.zeros(5, 0, dtype=dtype, device="cuda")
+    for _ in range(3):
+        given = torch.full((5, 2), 7.0, device="cuda")
+        Y, stats = B.bsr_layer_norm(x, eps=eps, stats=given)
+        assert stats is given and Y.shape == (5, 0)
+        _, made = B.bsr_layer_norm(x, eps=eps, want_stats=True)
+        for s in (given.cpu(), made.cpu()):
+            assert torch.equal(s[:, 0], torch.zeros(5)) and torch.allclose(s[:, 1], want[1].expand(5), rtol=2.0 ** -22, atol=0)
+    stream = torch.cuda.Stream()
+    given = torch.full((5, 2), 7.0, device="cuda")
+    torch.cuda.synchronize()
+    B.bsr_layer_norm(x, eps=eps, stats=given, stream=stream)
+    stream.synchronize()
+    assert torch.equal(given.cpu(), s)
