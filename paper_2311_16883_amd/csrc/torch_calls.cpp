@@ -52,7 +52,7 @@ int64_t integer(PyObject *o) {
   return v;
 }
 
-// A block extent: beyond the range of int it becomes a value that the library refuses.
+// A block extent or a kind of something: beyond the range of int it becomes a value that the library refuses.
 int extent(PyObject *o) {
   const int64_t v = integer(o);
   return v > INT_MAX ? INT_MAX : v < 0 ? -1 : (int)v;
@@ -794,7 +794,7 @@ PyObject *gated_ff(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor &X = tensor(a[0], "X"), &W = tensor(a[1], "W");
     const Dense x = dense2d(X, "X"), w = gated_weights(W, X);
     if (w.rows != x.cols) value_error("W must have a row for each column of X");
-    const int act = (int)integer(a[2]);
+    const int act = extent(a[2]);
     const int64_t F = w.cols / 2;
     const bool save = a[4] != Py_None || truth(a[5]);
     const int code = dtype_code(X);
@@ -822,7 +822,7 @@ PyObject *gated_ff_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor &GU = tensor(a[0], "GU"), &dH = tensor(a[1], "dH");
     const Dense gu = dense2d(GU, "GU"), h = matrix_like(dH, "dH", GU);
     if (gu.cols != 2 * h.cols || gu.rows != h.rows) value_error("GU must have the rows of dH and twice its columns");
-    const int act = (int)integer(a[3]);
+    const int act = extent(a[3]);
     const bool with_x = truth(a[6]);
     if (!with_x && a[5] != Py_None) value_error("dX is not wanted");
     const at::Tensor *W = with_x ? &tensor(a[2], "W") : nullptr;

@@ -26,3 +26,13 @@ def test_statistics_of_rows_without_columns(dtype, eps):
     B.bsr_layer_norm(x, eps=eps, stats=given, stream=stream)
     stream.synchronize()
     assert torch.equal(given.cpu(), s)
+
+
+def test_activations_beyond_an_int_are_refused():
+    x, w = torch.ones(3, 8, device="cuda"), torch.ones(8, 8, device="cuda")
+    gu, dh = torch.ones(3, 8, device="cuda"), torch.ones(3, 4, device="cuda")
+    for act in (1 << 32, -(1 << 32), (1 << 32) + 1, 4, -1):
+        for call in (lambda: B.bsr_gated_ff(x, w, act=act), lambda: B.bsr_gated_ff_grad(gu, dh, w, act=act), lambda: B.bsr_gated_ff_grad(gu, dh, None, act=act, want_dX=False)):
+            with pytest.raises(B.BsrError) as e:
+                call()
+            assert e.value.code == B.BSR_ERR_VALUE
