@@ -126,3 +126,26 @@ def test_sizes_of_the_gpu_tests_reach_every_product_kernel(recorder):
 def test_few_rows_of_a_norm_leave_nothing_to_add_up(recorder):
     assert len(kernels(recorder, norm_grad(8, 384))) == 1
     assert len(kernels(recorder, norm_grad(100, 384))) == 2
+
+
+def norm_grad_alone(M, D, dtype=BF16):
+    """... without the gradients of weight and bias"""
+    name, args = norm_grad(M, D, dtype)
+    return [name, args[:12] + [None, None] + args[14:]]
+
+
+def test_sizes_of_the_gpu_tests_reach_every_norm_kernel_and_those_of_few_rows(recorder):
+    """Sizes whose results the GPU tests compare with the plain implementation."""
+    from test_gpu_layer_ops import NORM_SIZES
+    from test_gpu_layer_widths import FEW_SIZES, WIDE_SIZES
+    calls = []
+    for dtype in (BF16, F32):
+        for M, D, _, _ in NORM_SIZES + WIDE_SIZES:
+            calls += [norm(M, D, dtype), norm_grad(M, D, dtype), norm_grad_alone(M, D, dtype)]
+        calls += [gated(*size, dtype) for size in FEW_SIZES]
+        calls.append(norm_grad(0, 5, dtype))
+    reached = {l["kernel"] for got in run(recorder, "recorded_token_calls.py", *calls) for l in got["launches"]}
+    kinds = ("layer_norm", "gated_few_kernel", "gated_rows_kernel", "clear_sums_kernel")
+    symbols = subprocess.run(["nm", str(LIB)], capture_output=True, text=True, check=True).stdout.split()
+    there = {n for n in symbols if any(k in n for k in kinds) and "_kernel" in n and "__device_stub__" not in n}
+    assert len(there) > 100 and sorted(there - reached) == []
