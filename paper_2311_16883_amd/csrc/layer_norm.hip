@@ -537,9 +537,11 @@ int norm_grad_of(const T *X, int64_t M, int64_t D, int64_t ldx, const void *gamm
     const int64_t groups = ceil_div(M, (int64_t)S::kRows);
     auto go = [&](auto with) {
       constexpr bool SUMS = decltype(with)::value;
-      // little more than a workgroup has in hand: one does it all, and nothing is left to add up (bfloat16, one workgroup and several: [32 x 1024]
-      // 7.5 us and 10.0, [64 x 337] 7.8 and 10.2, [64 x 1024] 11.1 and 10.0, [16 x 2048] 10.8 and 10.1, [2 x 9920] 13.3 and 10.1)
-      const bool alone = groups <= 1 || (groups <= 8 && D <= 4096 && M * D <= 25000);
+      // little more than a workgroup has in hand, of rows that are a wave's or less: one does it all, and nothing is left to add up (one workgroup and
+      // several, in a graph; bfloat16: [25 x 1024] 7.0 us and 7.8, [32 x 1024] 7.7 and 7.6, [36 x 337] 5.7 and 5.9, [48 x 337] 6.7 and 5.9, [256 x 64] 5.2
+      // and 5.9, [400 x 64] 6.2 and 5.9, [8 x 2048] 8.8 and 9.6, [12 x 2048] 10.1 and 9.5; binary32: [128 x 64] 4.3 and 5.2, [256 x 64] 5.7 and 5.3,
+      // [25 x 1024] 6.7 and 6.9; rows of several waves: [8 x 1536] 7.5 and 5.1)
+      const bool alone = groups <= 1 || (WAVES == 1 && groups <= S::kThreads / 128 && M * D <= 25600);
       const int64_t grid = !SUMS ? std::min(groups, kMostWorkgroups) : alone ? 1 : walkers(groups, WAVES);
       Sums out = {grid > 1 ? partial : nullptr, dgamma, dbeta, accumulate};
       if (SUMS) parts = grid;
