@@ -141,7 +141,7 @@ typedef struct {
   int64_t step;                /* 1 for the first */
   uint64_t seed;               /* 8-bit moments: names the random numbers of all steps */
   /* Device pointers to single numbers, or NULL.  Where one is set it is read by the kernels in the place of
-     the number above, so that a captured graph can be replayed with another. */
+     the number above, unchecked, so that a captured graph can be replayed with another. */
   const float *lr_device, *grad_scale_device;
   const int64_t *step_device;
 } bsr_adamw_options;

@@ -736,7 +736,7 @@ class _AdamWItem(C.Structure):
 
 class AdamWBatch:
     """The marshalled tensors of bsr_adamw_batched: build it once for tensors that stay where they are and pass it again every
-    step.  Holds references to them.  params, grads: contiguous tensors of any shape, all params of one dtype and all grads of one;
+    step (another one, with the first's states, where gradients are new tensors: 6 to 8 us a tensor).  Holds references to them.  params, grads: contiguous tensors of any shape, all params of one dtype and all grads of one;
     bits: 32 or 8, the moments' size; states: for every tensor (m, v) float32, or (m, v, scales) uint8 with scales [2 x
     bsr_adamw_blocks(n)] (v holds the codes of its root; see include/bsr_layer_ops.h) -- made as zeros where not given; copies: bfloat16 tensors that receive the new params too
     (None: none); weight_decay: a number, or one for every tensor."""

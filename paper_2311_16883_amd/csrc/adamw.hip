@@ -1,7 +1,7 @@
 // One AdamW step over many tensors, moments in binary32 or in 8 bits.
 //
 // Bound by memory: 28 bytes per element with binary32 weights, gradients and moments, 16 with 8-bit moments.  49 million elements of the
-// first kind and bfloat16 copies of the weights: 271 us, 5.4 TB/s; 180 million of the second, bfloat16 gradients and copies: 572 us, 5.0 TB/s.
+// first kind and bfloat16 copies of the weights: 271 us, 5.4 TB/s; 180 million of the second, bfloat16 gradients and copies: 580 us, 5.0 TB/s.
 // (A large copy: 5.1.)  The tensors of a call
 // are cut into chunks of whole blocks, a chunk to a workgroup; the list of tensors travels in the kernel's arguments, so
 // there is nothing to copy or to keep for the device.  A lane holds four consecutive elements of a block, 32 lanes a block, whose largest magnitudes

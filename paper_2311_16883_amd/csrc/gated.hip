@@ -5,8 +5,8 @@
 //
 // bfloat16 operands whose rows are not whole words are copied into the workspace first, rows padded; then so is the contraction,
 // with zeros.  Where there are few tiles the contraction is split and a second kernel adds the parts up, in order.  Few rows read W once, at the
-// rate of memory: 1 x 2048 x [2 x 5504] bfloat16 11.0 us (4.1 TB/s).  Large products are bound by the matrix cores (8192 rows of the same: 370 us, 1.0
-// PFLOP/s), the slopes by memory (25088 x [2 x 1024]: 40 us, 6.4 TB/s).
+// rate of memory: 1 x 2048 x [2 x 5504] bfloat16 11.0 us (4.1 TB/s).  Large products are bound by the matrix cores (8192 rows of the same: 372 us, 0.99
+// PFLOP/s), the slopes by memory (25088 x [2 x 1024]: 257 MB in 41 us, 6.3 TB/s).
 #include "gated.h"
 
 namespace bsr {
@@ -243,7 +243,10 @@ bool has_tile(Tile t, int dtype, bool gated) {
 // and end cost as much as some more of the contraction, most where nothing runs beside it (16384 x 128 x [2 x 2048] in 256 x 256 tiles 46 us, in 128 x 256 35,
 // in 128 x 128 51; 8192 x 512 x [2 x 2816] 64, 53, 68).  Tiles of 32 rows, in 16 and in up to 64 parts: one row of 16384 x [2 x 512] 14.9 and
 // 12.4 us, of 40000 x [2 x 64] 26.1 and 13.7, binary32 47 and 20, 103 and 33.  (Whether GU is written has no part in it: H would have other bits
-// with GU than without.)
+// with GU than without.)  Tiles of 32 rows are for up to 32: bfloat16 of 33 to 96 rows is no faster in them (48 x 2048 x [2 x 5504] 15.2 us and 20.3,
+// 33 x 8192 x [2 x 1024] 13.6 and 13.8); binary32 takes a tenth more or less (64 x 4096 x [2 x 4096] 49.4 and 50.5, 33 x 2048 x [2 x 5504] 40.5 and 38.8), but
+// small products and gradients of few columns, which more than 16 parts would share, up to half (48 x 411 x [2 x 1003] 14.9 and 11.7, gradient of
+// 48 x 512 x [2 x 8192] 46 and 23).
 double estimate_us(Tile t, int64_t M, int64_t N, int64_t K, int dtype, bool gated, int64_t splits) {
   const double rates[2][7][2] = {{{4.9, 4.9}, {4.6, 4.4}, {2.4, 3.6}, {3.4, 3.4}, {3.0, 3.0}, {2.9, 2.8}, {1.0, 1.8}},
                                  {{0, 0}, {0, 0}, {0.46, 0.53}, {0, 0}, {0, 0}, {0.45, 0.47}, {0.43, 0.45}}};
@@ -469,6 +472,8 @@ int backward(const GatedArgs &g, const void *GU, int64_t ldgu, const void *dH, i
     if (const int rc = check_launch(); rc != BSR_OK) return rc;
   }
   if (!product) return BSR_OK;
+  // The operand is the dGU that was stored, in bfloat16 rounded: the matrix instructions take no wider one, and the weights' gradient takes the same.
+  // (Against binary64 dX is off by 0.235 % of its norm, of which its own rounding makes 0.166 %; both halves of unrounded slopes would be twice the product.)
   ProductArgs a = {};
   a.A = also != nullptr ? also : dGU;
   a.lda = also != nullptr ? pitch : lddgu;

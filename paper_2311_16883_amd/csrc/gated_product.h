@@ -15,10 +15,10 @@
 // The matrix instructions take B's fragment first: a lane then holds four consecutive columns of one row of the result, and
 // exchanges between the halves of a wave make 16-byte stores of them.
 //
-// Bound by the matrix cores: 8192 x 2048 x [2 x 5504] bfloat16, 369 GFLOP, takes 366 us with GU written (1.01 PFLOP/s), about what a library's
+// Bound by the matrix cores: 8192 x 2048 x [2 x 5504] bfloat16, 369 GFLOP, takes 372 us with GU written (0.99 PFLOP/s), about what a library's
 // product of this size takes that stores [G | U] and nothing else (379 us, 354 with W transposed).  What is lost: the first stages of a tile and its
 // results, in which the matrix cores wait (one workgroup of 256 x 256 fills a compute unit, so nothing runs beside them), and the last
-// round of tiles, which is not full.  Binary32 reaches 121 TFLOP/s of the 154 that a library does.
+// round of tiles, which is not full: they are busy for 55 % of the cycles.  Binary32 reaches 121 TFLOP/s of the 154 that a library does.
 // Measured and not kept (this size): 256 x 256 and 128 x 256 tiles in one launch, the last round in the smaller ones: 360 us, but 2048 rows 96 for 93 and
 // 25088 x 384 x [2 x 1024] 72 for 66; wave tiles of 128 x 128 and of 64 x 128; results stored past the caches 495; results in whole
 // 64-byte rows by more exchanges 375.
@@ -265,8 +265,8 @@ __global__ __launch_bounds__(64 * WM * WN, (WM * WN == 4 && RING * 32 * (TM * WM
   // Multiplies the fragments of a phase and does `actions` other things between the matrix instructions: a wave issues them
   // while the matrix core is busy, where all of them together in front would leave it idle (both waves of a SIMD come to that
   // place at the same time).  The order is the program's: the compiler would gather them again.  Where a wave has a SIMD for itself, the last
-  // fragment is requested some matrix instructions before it is waited for (997 x 411 x [2 x 1003] binary32 25.2 -> 23.6 us; in the
-  // largest tile, whose other wave covers that, 0.5 % slower).
+  // fragment is requested some matrix instructions before it is waited for (997 x 411 x [2 x 1003] binary32 26.8 -> 25.8 us; in the
+  // largest tile, whose other wave covers that, 1 % slower).
   constexpr bool kEarly = TM * TN <= 4;
   auto multiply = [&](const Frags &f, auto actions, auto action) {
     constexpr int kActions = decltype(actions)::value, kSteps = sizeof(T) == 2 ? 1 : 4, kAll = TM * TN * kSteps;
